@@ -178,6 +178,7 @@ def library():
         L.rac_predictor_step.restype = ctypes.c_int
         L.rac_status_string.argtypes = [ctypes.c_int]
         L.rac_status_string.restype = ctypes.c_char_p
+        cache.declare(L)
         _lib = L
     return _lib
 
@@ -510,3 +511,9 @@ def rac_predictor_step(cfg: PredictorConfig, weights, cache, pos, h_prev, ref_ou
                                         _dev(workspace, "workspace", 1, rac_predictor_workspace_bytes(cfg)),
                                         _nbytes(workspace) if not isinstance(workspace, int) else
                                         rac_predictor_workspace_bytes(cfg), _stream(stream)), "rac_predictor_step")
+
+
+from . import cache  # noqa: E402  (its functions call the ones above)
+from .cache import *  # noqa: E402,F401,F403
+
+__all__ += cache.__all__

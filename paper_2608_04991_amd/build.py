@@ -23,6 +23,8 @@ ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "rac.hip")
 HOST_SRC = os.path.join(HERE, "csrc", "spans.cpp")   # host-only C++ (reference selection)
 PRED_SRC = os.path.join(HERE, "csrc", "predictor.hip")  # decode-phase reference predictor
+CACHE_SRC = os.path.join(HERE, "csrc", "cache.hip")  # paged key-value cache
+TREE_SRC = os.path.join(HERE, "csrc", "tree.hip")    # attention of drafted trees over it
 INC = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "lib", "librac.so")
 
@@ -50,9 +52,13 @@ def build(verbose: bool = True) -> str:
         jobs.append([HIPCC, *compile_flags, *define, "-c", "-I", INC, "-o", objs[-1], SRC])
         jobs.append([HIPCC, *[f for f in compile_flags if f != "-fPIC"], *define, "--cuda-device-only", "-S",
                      "-I", INC, "-o", asms[-1], SRC])
-    for src in (PRED_SRC, HOST_SRC):
+    for src in (PRED_SRC, HOST_SRC, CACHE_SRC, TREE_SRC):
         objs.append(os.path.join(out, os.path.basename(src) + ".o"))
         jobs.append([HIPCC, *compile_flags, "-c", "-I", INC, "-o", objs[-1], src])
+    for src in (CACHE_SRC, TREE_SRC):
+        asms.append(os.path.join(out, os.path.basename(src) + ".s"))
+        jobs.append([HIPCC, *[f for f in compile_flags if f != "-fPIC"], "--cuda-device-only", "-S", "-I", INC, "-o",
+                     asms[-1], src])
     tmp = LIB + ".tmp"
     try:
         if verbose:

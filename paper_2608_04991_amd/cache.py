@@ -1,0 +1,264 @@
+"""Python binding of include/rac_cache.h: the paged key-value cache and the
+attention of drafted trees.  Re-exported by the package.
+
+    cfg = CacheConfig(layers=1, kv_heads=8, head_dim=128, page_tokens=32, pages=4096, seqs=64, max_pages=512)
+    pool = torch.zeros(rac_cache_pool_bytes(cfg), dtype=torch.uint8, device="cuda")
+    table, lengths, refs = rac_cache_new(cfg)
+    tree = TreeConfig(q_heads=32, rows=q.shape[0], max_rows=64, max_draft=64)
+    ws = torch.empty(rac_tree_attention_workspace(cfg, tree), dtype=torch.uint8, device="cuda")
+    rac_tree_attention(cfg, tree, 0, pool, table, lengths, q, start, k, v, out, ws, mask=mask)
+    rac_cache_commit(cfg, pool, table, lengths, refs, k[None], v[None], start, committed, ws2, path=path)
+
+As in the rest of the package every step runs in HIP kernels; PyTorch supplies
+device memory and the stream.
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+from dataclasses import dataclass
+
+import paper_2608_04991_amd as _rac
+
+__all__ = [
+    "RAC_CACHE_BF16", "RAC_CACHE_FP16", "RAC_CACHE_FP8", "CacheConfig", "TreeConfig", "rac_cache_pool_bytes",
+    "rac_cache_new", "rac_tree_attention_workspace", "rac_tree_attention", "rac_cache_fork",
+    "rac_cache_commit_workspace", "rac_cache_commit", "rac_cache_copy",
+]
+
+RAC_CACHE_BF16 = 0
+RAC_CACHE_FP16 = 1
+RAC_CACHE_FP8 = 2
+
+
+class _CacheConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("layers", "kv_heads", "head_dim", "page_tokens", "pages", "seqs",
+                                              "max_pages", "type")] + \
+               [("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
+
+
+class _TreeConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("q_heads", "rows", "max_rows", "max_draft", "window")] + \
+               [("scale", ctypes.c_float)]
+
+
+class _TreeTensors(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "q_start", "draft_start", "mask", "out", "lse")] + \
+               [(n, ctypes.c_int64) for n in ("q_stride", "kv_stride", "out_stride")] + \
+               [(n, ctypes.c_int32) for n in ("draft_rows", "mask_words")]
+
+
+@dataclass(frozen=True)
+class CacheConfig:
+    layers: int
+    kv_heads: int
+    head_dim: int
+    page_tokens: int
+    pages: int
+    seqs: int
+    max_pages: int
+    type: int = RAC_CACHE_BF16
+    k_scale: float = 1.0
+    v_scale: float = 1.0
+
+    def _c(self) -> _CacheConfig:
+        return _cache_struct(self)
+
+
+@dataclass(frozen=True)
+class TreeConfig:
+    q_heads: int
+    rows: int
+    max_rows: int
+    max_draft: int
+    window: int = 0
+    scale: float = 0.0
+
+    def _c(self) -> _TreeConfig:
+        return _tree_struct(self)
+
+
+# (the library reads the structs during the call only, so one instance per
+# configuration can be passed to every call)
+@functools.lru_cache(maxsize=512)
+def _cache_struct(c: CacheConfig) -> _CacheConfig:
+    return _CacheConfig(c.layers, c.kv_heads, c.head_dim, c.page_tokens, c.pages, c.seqs, c.max_pages, c.type,
+                        c.k_scale, c.v_scale)
+
+
+@functools.lru_cache(maxsize=512)
+def _tree_struct(t: TreeConfig) -> _TreeConfig:
+    return _TreeConfig(t.q_heads, t.rows, t.max_rows, t.max_draft, t.window, t.scale)
+
+
+def declare(L) -> None:
+    """The argument types of the library's cache functions."""
+    cp, tp, vp, i32, i64 = (ctypes.POINTER(_CacheConfig), ctypes.POINTER(_TreeConfig), ctypes.c_void_p,
+                            ctypes.c_int32, ctypes.c_int64)
+    sz = ctypes.c_size_t
+    for name, args, res in (
+            ("rac_cache_pool_bytes", [cp], sz),
+            ("rac_tree_attention_workspace", [cp, tp], sz),
+            ("rac_tree_attention", [cp, tp, i32, vp, vp, vp, ctypes.POINTER(_TreeTensors), vp, sz, vp], ctypes.c_int),
+            ("rac_cache_fork", [cp, vp, vp, vp, vp, vp, vp, vp], ctypes.c_int),
+            ("rac_cache_commit_workspace", [cp], sz),
+            ("rac_cache_commit", [cp, vp, vp, vp, vp, vp, vp, i64, i64, i32, vp, vp, i32, vp, vp, sz, vp],
+             ctypes.c_int),
+            ("rac_cache_copy", [cp, vp, vp, vp, vp, i32, vp], ctypes.c_int)):
+        f = getattr(L, name)
+        f.argtypes = args
+        f.restype = res
+
+
+def _pool(cfg: CacheConfig, pool, what: str = "pool"):
+    """Address of a pool tensor of any element type, checked by its bytes."""
+    if pool is None or isinstance(pool, int):
+        return pool
+    size = pool.element_size()
+    return _rac._dev(pool, what, size, -(-_pool_bytes(cfg, _rac.library()) // size))
+
+
+def _rows(t, what: str, rows: int, heads: int, dim: int):
+    """(address, elements between rows) of a 16-bit [rows][heads][dim] tensor
+    whose heads lie together; its rows may be apart."""
+    if t is None or isinstance(t, int):
+        return t, heads * dim
+    try:
+        if t.is_cuda and t.element_size() == 2 and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dim \
+                and t.shape[0] >= rows:
+            st = t.stride()
+            if t.shape[0] <= 1:
+                st = (heads * dim, st[1], st[2])
+            if st[2] == 1 and (st[1] == dim or heads == 1) and st[0] >= heads * dim:
+                return t.data_ptr(), st[0]
+    except AttributeError:
+        pass
+    raise ValueError(f"{what}: expected a GPU tensor of 2-byte elements, [{rows}][{heads}][{dim}], heads and channels "
+                     "contiguous")
+
+
+def rac_cache_pool_bytes(cfg: CacheConfig) -> int:
+    return _pool_bytes(cfg, _rac.library())
+
+
+@functools.lru_cache(maxsize=512)
+def _pool_bytes(cfg: CacheConfig, lib) -> int:
+    return int(lib.rac_cache_pool_bytes(ctypes.byref(cfg._c())))
+
+
+def rac_cache_new(cfg: CacheConfig, device: str = "cuda"):
+    """(table, lengths, refs) of an empty cache."""
+    import torch
+    return (torch.full((cfg.seqs, cfg.max_pages), -1, dtype=torch.int32, device=device),
+            torch.zeros(cfg.seqs, dtype=torch.int32, device=device),
+            torch.zeros(cfg.pages, dtype=torch.int32, device=device))
+
+
+def rac_tree_attention_workspace(cfg: CacheConfig, tree: TreeConfig) -> int:
+    return _attention_workspace(cfg, tree, _rac.library())
+
+
+@functools.lru_cache(maxsize=512)
+def _attention_workspace(cfg: CacheConfig, tree: TreeConfig, lib) -> int:
+    return int(lib.rac_tree_attention_workspace(ctypes.byref(cfg._c()), ctypes.byref(tree._c())))
+
+
+def rac_tree_attention(cfg: CacheConfig, tree: TreeConfig, layer: int, pool, table, lengths, q, q_start, k, v, out,
+                       workspace, *, draft_start=None, mask=None, lse=None, stream=None) -> None:
+    """Attention of query rows q (16-bit [rows][q_heads][head_dim]) over the
+    committed tokens in the pool and the drafted ones k, v ([draft_rows]
+    [kv_heads][head_dim], or None).  q_start, draft_start: int32 [seqs + 1];
+    mask: int64 [rows][words], the drafted tokens each row sees; lse: fp32
+    [rows][q_heads].  Rows of q, k, v and out may be apart (views of a larger
+    tensor); k and v by the same distance."""
+    dev = _rac._dev
+    R, H, D = tree.rows, cfg.kv_heads, cfg.head_dim
+    drafted = 0 if k is None or isinstance(k, int) else int(k.shape[0])
+    qp, qs = _rows(q, "q", R, tree.q_heads, D)
+    op, os_ = _rows(out, "out", R, tree.q_heads, D)
+    kp, ks = _rows(k, "k", 0, H, D)
+    vp, vs = _rows(v, "v", drafted, H, D)
+    if k is not None and v is not None and drafted > 1 and ks != vs:
+        raise ValueError("k and v: expected the same distance between rows")
+    words = 0
+    if mask is not None:
+        words = mask if isinstance(mask, int) else int(mask.shape[-1])
+    t = _TreeTensors(qp, kp, vp, dev(q_start, "q_start", 4, cfg.seqs + 1),
+                     dev(draft_start, "draft_start", 4, cfg.seqs + 1), dev(mask, "mask", 8, R * words), op,
+                     dev(lse, "lse", 4, R * tree.q_heads), qs, ks, os_, drafted, words)
+    need = _attention_workspace(cfg, tree, _rac.library())
+    _rac._check(_rac.library().rac_tree_attention(
+        ctypes.byref(cfg._c()), ctypes.byref(tree._c()), int(layer), _pool(cfg, pool),
+        dev(table, "table", 4, cfg.seqs * cfg.max_pages), dev(lengths, "lengths", 4, cfg.seqs), ctypes.byref(t),
+        dev(workspace, "workspace", 1, need), need if isinstance(workspace, int) else _rac._nbytes(workspace),
+        _rac._stream(stream)), "rac_tree_attention")
+
+
+def rac_cache_fork(cfg: CacheConfig, parents, table, lengths, refs, keep_from=None, keep_to=None, stream=None) -> None:
+    """Sequence d becomes a view of positions [keep_from[d], keep_to[d]) of what
+    sequence parents[d] held (int32 [seqs] each): fork, reorder, roll back, bound
+    and free sequences, in place."""
+    dev, S = _rac._dev, cfg.seqs
+    _rac._check(_rac.library().rac_cache_fork(
+        ctypes.byref(cfg._c()), dev(parents, "parents", 4, S), dev(keep_from, "keep_from", 4, S),
+        dev(keep_to, "keep_to", 4, S), dev(table, "table", 4, S * cfg.max_pages), dev(lengths, "lengths", 4, S),
+        dev(refs, "refs", 4, cfg.pages), _rac._stream(stream)), "rac_cache_fork")
+
+
+def rac_cache_commit_workspace(cfg: CacheConfig) -> int:
+    return _commit_workspace(cfg, _rac.library())
+
+
+@functools.lru_cache(maxsize=512)
+def _commit_workspace(cfg: CacheConfig, lib) -> int:
+    return int(lib.rac_cache_commit_workspace(ctypes.byref(cfg._c())))
+
+
+def _layers(t, what: str, cfg: CacheConfig):
+    """(address, elements between rows, between layers, rows) of a 16-bit
+    [layers][rows][kv_heads][head_dim] tensor."""
+    H, D = cfg.kv_heads, cfg.head_dim
+    try:
+        if t.is_cuda and t.element_size() == 2 and t.dim() == 4 and t.shape[0] == cfg.layers and t.shape[2] == H \
+                and t.shape[3] == D:
+            st, rows = t.stride(), int(t.shape[1])
+            row = st[1] if rows > 1 else H * D
+            if (st[3] == 1 and (st[2] == D or H == 1)) and row >= H * D:
+                return t.data_ptr(), row, st[0] if cfg.layers > 1 else 0, rows
+            if t.numel() == 0:
+                return t.data_ptr(), H * D, 0, rows
+    except AttributeError:
+        pass
+    raise ValueError(f"{what}: expected a GPU tensor of 2-byte elements, [{cfg.layers}][rows][{H}][{D}], heads and "
+                     "channels contiguous")
+
+
+def rac_cache_commit(cfg: CacheConfig, pool, table, lengths, refs, k, v, draft_start, committed, workspace, *,
+                     path=None, max_path: int | None = None, stream=None) -> None:
+    """Appends the accepted drafted tokens of every sequence to it, in all
+    layers: k, v 16-bit [layers][rows][kv_heads][head_dim], draft_start int32
+    [seqs + 1], path int32 [seqs][max_path] (None: all rows of a sequence, at
+    most max_path); committed int32 [seqs] receives the tokens appended."""
+    dev, S = _rac._dev, cfg.seqs
+    kp, row, layer, rows = _layers(k, "k", cfg)
+    vp, vrow, vlayer, vrows = _layers(v, "v", cfg)
+    if vrows != rows or vrow != row or vlayer != layer:
+        raise ValueError("k and v: expected the same rows, apart by the same distances")
+    if max_path is None:
+        max_path = rows if path is None else int(path.shape[-1])
+    need = _commit_workspace(cfg, _rac.library())
+    _rac._check(_rac.library().rac_cache_commit(
+        ctypes.byref(cfg._c()), _pool(cfg, pool), dev(table, "table", 4, S * cfg.max_pages),
+        dev(lengths, "lengths", 4, S), dev(refs, "refs", 4, cfg.pages), kp, vp, row, layer, rows,
+        dev(draft_start, "draft_start", 4, S + 1), dev(path, "path", 4, S * int(max_path)), int(max_path),
+        dev(committed, "committed", 4, S), dev(workspace, "workspace", 1, need),
+        need if isinstance(workspace, int) else _rac._nbytes(workspace), _rac._stream(stream)), "rac_cache_commit")
+
+
+def rac_cache_copy(cfg: CacheConfig, src_pool, src, dst_pool, dst, n: int | None = None, stream=None) -> None:
+    """Copies page src[i] of src_pool to page dst[i] of dst_pool (int32 arrays)."""
+    count = int(n) if n is not None else int(src.numel())
+    _rac._check(_rac.library().rac_cache_copy(
+        ctypes.byref(cfg._c()), _pool(cfg, src_pool, "src_pool"), _rac._dev(src, "src", 4, count),
+        _pool(cfg, dst_pool, "dst_pool"), _rac._dev(dst, "dst", 4, count), count, _rac._stream(stream)),
+        "rac_cache_copy")

@@ -1,0 +1,382 @@
+// cache.hip - gfx950 kernels and C ABI of the paged key-value cache: forking,
+// committing and copying pages.  The contract is in include/rac_cache.h.
+//
+// All bookkeeping (page tables, lengths, reference counts) stays on the device
+// and gives the same pages whatever order the workgroups run in: counts change
+// by commutative integer atomics, and pages are taken lowest number first.
+#include "cache_common.h"
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// Fork.  A table entry only moves within its column, so a workgroup that owns
+// whole columns can read all of them before it writes any, in place and in one
+// launch: kCols columns of all sequences through LDS.  Lengths move within the
+// first workgroup alone.
+struct ForkArgs {
+    const int32_t* parents;
+    const int32_t* from;
+    const int32_t* to;
+    int32_t* table;
+    int32_t* lengths;
+    int32_t* refs;
+    int32_t seqs, max_pages, pages, log_page;
+};
+
+constexpr int kForkCols = 4;
+constexpr int kForkThreads = 256;
+
+__global__ __launch_bounds__(kForkThreads) void cache_fork_kernel(ForkArgs a) {
+    extern __shared__ int32_t old[];  // [seqs][kForkCols]
+    const int c = (int)threadIdx.x % kForkCols, j = (int)blockIdx.x * kForkCols + c;
+    const bool in = j < a.max_pages;
+    if (in)
+        for (int d = (int)threadIdx.x / kForkCols; d < a.seqs; d += kForkThreads / kForkCols)
+            old[d * kForkCols + c] = a.table[(size_t)d * a.max_pages + j];
+    __syncthreads();
+    if (in) {
+        const int first = j << a.log_page, past = (j + 1) << a.log_page;
+        for (int d = (int)threadIdx.x / kForkCols; d < a.seqs; d += kForkThreads / kForkCols) {
+            const int parent = a.parents[d], was = old[d * kForkCols + c];
+            int now = parent >= 0 && parent < a.seqs ? old[parent * kForkCols + c] : -1;
+            if (a.to && first >= a.to[d]) now = -1;
+            if (a.from && past <= a.from[d]) now = -1;
+            if (now < 0 || now >= a.pages) now = -1;
+            if (now == was) continue;
+            a.table[(size_t)d * a.max_pages + j] = now;
+            if (was >= 0 && was < a.pages) atomicAdd(a.refs + was, -1);
+            if (now >= 0) atomicAdd(a.refs + now, 1);
+        }
+    }
+    if (blockIdx.x != 0) return;
+    __syncthreads();
+    for (int d = (int)threadIdx.x; d < a.seqs; d += kForkThreads) old[d] = a.lengths[d];
+    __syncthreads();
+    for (int d = (int)threadIdx.x; d < a.seqs; d += kForkThreads) {
+        const int parent = a.parents[d];
+        int n = parent >= 0 && parent < a.seqs ? old[parent] : 0;
+        if (a.to && a.to[d] < n) n = a.to[d];
+        a.lengths[d] = n < 0 ? 0 : n;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Commit, first launch: one workgroup decides.  How many tokens and pages each
+// sequence takes, which pages are free (a scan of the counts that ends when
+// the demand is met), and the new table entries, counts and lengths.  The
+// second launch moves the data by the records this one leaves.
+struct CommitRecord {
+    int32_t length;      // before the call
+    int32_t tokens;      // appended
+    int32_t copy_from;   // the shared last page, or -1
+    int32_t copy_to;
+};
+
+struct PlanArgs {
+    int32_t* table;
+    int32_t* lengths;
+    int32_t* refs;
+    const int32_t* start;
+    const int32_t* path;
+    int32_t* committed;
+    CommitRecord* record;  // [seqs]
+    int32_t* free_list;    // [pages]
+    int32_t seqs, max_pages, pages, log_page, draft_rows, max_path;
+};
+
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanWaves = kPlanThreads / 64;
+
+// Rows of a sequence's drafts, whatever start[] holds.
+__device__ __forceinline__ int2 row_range(const int32_t* start, int s, int rows) {
+    const int lo = clamp_int(start[s], 0, rows), hi = clamp_int(start[s + 1], lo, rows);
+    return make_int2(lo, hi - lo);
+}
+
+// Sum over the threads before this one, and over all of them.
+__device__ __forceinline__ int scan_workgroup(int v, int* sums, int* total) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
+    int x = v;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o);
+        x += lane >= o ? y : 0;
+    }
+    __syncthreads();
+    if (lane == 63) sums[w] = x;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int i = 0; i < kPlanWaves; ++i) {
+        before += i < w ? sums[i] : 0;
+        all += sums[i];
+    }
+    *total = all;
+    return before + x - v;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
+    __shared__ int sums[kPlanWaves];
+    const int t = (int)threadIdx.x, page = 1 << a.log_page;
+    constexpr int kPer = 4;  // sequences a thread (4096 / 1024)
+    int tokens[kPer], need[kPer], base[kPer], length[kPer], tail[kPer];
+    bool copies[kPer], fresh[kPer];
+    int demand = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int s = t + i * kPlanThreads;
+        tokens[i] = need[i] = length[i] = 0;
+        tail[i] = -1;
+        copies[i] = fresh[i] = false;
+        if (s < a.seqs) {
+            const int drafted = row_range(a.start, s, a.draft_rows).y;
+            int n = 0;
+            if (a.path) {
+                const int32_t* p = a.path + (size_t)s * a.max_path;
+                while (n < a.max_path && p[n] >= 0 && p[n] < drafted) ++n;
+            } else {
+                n = drafted < a.max_path ? drafted : a.max_path;
+            }
+            const int most = a.max_pages << a.log_page, len = clamp_int(a.lengths[s], 0, most);
+            length[i] = len;
+            if (n > 0 && n <= most - len) {
+                tokens[i] = n;
+                need[i] = ((len + n + page - 1) >> a.log_page) - ((len + page - 1) >> a.log_page);
+                if (len & (page - 1)) {
+                    tail[i] = a.table[(size_t)s * a.max_pages + (len >> a.log_page)];
+                    if (tail[i] < 0 || tail[i] >= a.pages) tail[i] = -1;
+                    copies[i] = tail[i] >= 0 && a.refs[tail[i]] > 1;
+                    fresh[i] = copies[i] || tail[i] < 0;
+                    need[i] += fresh[i];
+                }
+            }
+        }
+        int all;
+        base[i] = demand + scan_workgroup(need[i], sums, &all);
+        demand += all;
+    }
+    // the free pages, lowest first, until the demand is met
+    int found = 0;
+    for (int p0 = 0; p0 < a.pages && found < demand; p0 += kPlanThreads) {
+        const int p = p0 + t;
+        const bool is = p < a.pages && a.refs[p] == 0;
+        int all;
+        const int at = found + scan_workgroup(is, sums, &all);
+        if (is && at < demand) a.free_list[at] = p;
+        found += all;
+    }
+    __syncthreads();  // (the list is read by other threads of this workgroup)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int s = t + i * kPlanThreads;
+        if (s >= a.seqs) continue;
+        CommitRecord r{length[i], tokens[i], -1, -1};
+        if (base[i] + need[i] > found) r.tokens = 0;
+        if (r.tokens > 0) {
+            int32_t* row = a.table + (size_t)s * a.max_pages;
+            int at = ((length[i] + page - 1) >> a.log_page) - (fresh[i] ? 1 : 0);
+            for (int k = 0; k < need[i]; ++k, ++at) {
+                const int p = a.free_list[base[i] + k];
+                row[at] = p;
+                a.refs[p] = 1;
+            }
+            if (copies[i]) {
+                r.copy_from = tail[i];
+                r.copy_to = a.free_list[base[i]];
+                atomicAdd(a.refs + tail[i], -1);
+            }
+            a.lengths[s] = length[i] + r.tokens;
+        }
+        a.record[s] = r;
+        a.committed[s] = r.tokens;
+    }
+}
+
+// Second launch: a workgroup per (sequence, layer).
+struct MoveArgs {
+    uint8_t* pool;
+    const int32_t* table;
+    const uint16_t* k;
+    const uint16_t* v;
+    const int32_t* start;
+    const int32_t* path;
+    const CommitRecord* record;
+    int64_t kv_stride, layer_stride;
+    float k_scale, v_scale;
+    int32_t layers, heads, dim, log_page, max_pages, pages, draft_rows, max_path;
+};
+
+constexpr int kMoveThreads = 256;
+
+// Eight bf16 as eight e4m3 of x / scale.
+__device__ __forceinline__ u32x2 to_fp8(u32x4 x, float scale) {
+    u32x2 o = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float lo = __uint_as_float(x[i] << 16) / scale, hi = __uint_as_float(x[i] & 0xFFFF0000u) / scale;
+        // (a NaN stays one: neither comparison holds)
+        lo = lo > 448.0f ? 448.0f : lo < -448.0f ? -448.0f : lo;
+        hi = hi > 448.0f ? 448.0f : hi < -448.0f ? -448.0f : hi;
+        if (i & 1)
+            o[i >> 1] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(lo, hi, (int)o[i >> 1], true);
+        else
+            o[i >> 1] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(lo, hi, (int)o[i >> 1], false);
+    }
+    return o;
+}
+
+template <bool FP8>
+__global__ __launch_bounds__(kMoveThreads) void cache_move_kernel(MoveArgs a) {
+    const int s = (int)blockIdx.x / a.layers, layer = (int)blockIdx.x % a.layers, t = (int)threadIdx.x;
+    const CommitRecord r = a.record[s];
+    if (r.tokens == 0) return;
+    constexpr int kB = FP8 ? 1 : 2;
+    const int page = 1 << a.log_page;
+    const size_t plane = (size_t)page * a.dim * kB;         // keys or values of one head in a page
+    const size_t side = plane * a.heads, whole = 2 * side;  // of all heads; of both
+    auto at = [&](int p) { return a.pool + ((size_t)p * a.layers + layer) * whole; };
+    if (r.copy_from >= 0) {
+        const int bytes = (r.length & (page - 1)) * a.dim * kB;  // a multiple of 16
+        const uint8_t* from = at(r.copy_from);
+        uint8_t* to = at(r.copy_to);
+        const int per = bytes / 16;
+        for (int i = t; i < per * 2 * a.heads; i += kMoveThreads) {
+            const size_t o = (size_t)(i / per) * plane + (size_t)(i % per) * 16;
+            *reinterpret_cast<u32x4*>(to + o) = *reinterpret_cast<const u32x4*>(from + o);
+        }
+    }
+    const int2 rows = row_range(a.start, s, a.draft_rows);
+    const int per = a.dim / 8, all = r.tokens * 2 * a.heads * per;
+    for (int i = t; i < all; i += kMoveThreads) {
+        const int c = i % per, h = i / per % a.heads, side_of = i / per / a.heads % 2, n = i / per / a.heads / 2;
+        const int node = a.path ? a.path[(size_t)s * a.max_path + n] : n;
+        const uint16_t* from = (side_of ? a.v : a.k) + (size_t)layer * a.layer_stride +
+                               (size_t)(rows.x + node) * a.kv_stride + (size_t)h * a.dim + 8 * c;
+        const int pos = r.length + n, p = a.table[(size_t)s * a.max_pages + (pos >> a.log_page)];
+        if (p < 0 || p >= a.pages) continue;
+        uint8_t* to = at(p) + side_of * side + h * plane + ((size_t)(pos & (page - 1)) * a.dim + 8 * c) * kB;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(from);
+        if constexpr (FP8)
+            *reinterpret_cast<u32x2*>(to) = to_fp8(x, side_of ? a.v_scale : a.k_scale);
+        else
+            *reinterpret_cast<u32x4*>(to) = x;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Copy: a workgroup per kCopyBytes of a page.
+constexpr int kCopyThreads = 256;
+constexpr int kCopyBytes = kCopyThreads * 16 * 4;
+
+struct CopyArgs {
+    const uint8_t* from;
+    uint8_t* to;
+    const int32_t* src;
+    const int32_t* dst;
+    uint64_t page_bytes;
+    int32_t pages, parts;
+};
+
+__global__ __launch_bounds__(kCopyThreads) void cache_copy_kernel(CopyArgs a) {
+    const int i = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x % (unsigned)a.parts);
+    const int s = a.src[i], d = a.dst[i];
+    if (s < 0 || s >= a.pages || d < 0 || d >= a.pages) return;
+    const uint64_t o = (uint64_t)part * kCopyBytes + 16u * threadIdx.x;
+    const uint8_t* from = a.from + (uint64_t)s * a.page_bytes;
+    uint8_t* to = a.to + (uint64_t)d * a.page_bytes;
+    u32x4 x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint64_t at = o + 16u * kCopyThreads * k;
+        if (at < a.page_bytes) x[k] = *reinterpret_cast<const u32x4*>(from + at);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint64_t at = o + 16u * kCopyThreads * k;
+        if (at < a.page_bytes) *reinterpret_cast<u32x4*>(to + at) = x[k];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+
+uint64_t up256(uint64_t v) { return (v + 255u) & ~uint64_t(255); }
+
+template <class A>
+rac_status launch(const void* kernel, unsigned grid, unsigned threads, const A& args, size_t lds, hipStream_t st) {
+    A a = args;
+    void* p[] = {&a};
+    return hipLaunchKernel(kernel, dim3(grid), dim3(threads), p, lds, st) == hipSuccess ? RAC_OK : RAC_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t rac_cache_pool_bytes(const rac_cache_config* cfg) {
+    return cache_valid(cfg) ? (size_t)(cache_page_bytes(cfg) * (uint64_t)cfg->pages) : 0;
+}
+
+rac_status rac_cache_fork(const rac_cache_config* cfg, const int32_t* parents, const int32_t* keep_from,
+                          const int32_t* keep_to, int32_t* table, int32_t* lengths, int32_t* refs,
+                          rac_stream_t stream) {
+    if (!cache_valid(cfg) || !parents || !table || !lengths || !refs) return RAC_ERR_INVALID;
+    if (!aligned(parents, 4) || !aligned(keep_from, 4) || !aligned(keep_to, 4) || !aligned(table, 4) ||
+        !aligned(lengths, 4) || !aligned(refs, 4))
+        return RAC_ERR_ALIGN;
+    const ForkArgs a{parents, keep_from, keep_to, table, lengths, refs, cfg->seqs, cfg->max_pages, cfg->pages,
+                     log2_of(cfg->page_tokens)};
+    const unsigned grid = (unsigned)((cfg->max_pages + kForkCols - 1) / kForkCols);
+    return launch(reinterpret_cast<const void*>(cache_fork_kernel), grid, kForkThreads, a,
+                  (size_t)cfg->seqs * kForkCols * sizeof(int32_t), stream);
+}
+
+size_t rac_cache_commit_workspace(const rac_cache_config* cfg) {
+    if (!cache_valid(cfg)) return 0;
+    return (size_t)(up256((uint64_t)cfg->seqs * sizeof(CommitRecord)) + up256((uint64_t)cfg->pages * 4u));
+}
+
+rac_status rac_cache_commit(const rac_cache_config* cfg, void* pool, int32_t* table, int32_t* lengths, int32_t* refs,
+                            const void* k, const void* v, int64_t kv_stride, int64_t layer_stride, int32_t draft_rows,
+                            const int32_t* draft_start, const int32_t* path, int32_t max_path, int32_t* committed,
+                            void* workspace, size_t workspace_bytes, rac_stream_t stream) {
+    if (!cache_valid(cfg) || draft_rows < 0 || max_path < 0) return RAC_ERR_INVALID;
+    const int64_t row = (int64_t)cfg->kv_heads * cfg->head_dim;
+    if (kv_stride < row || kv_stride % 8 || layer_stride % 8 || layer_stride < 0) return RAC_ERR_INVALID;
+    if (!pool || !table || !lengths || !refs || !draft_start || !committed || !workspace) return RAC_ERR_INVALID;
+    if (draft_rows > 0 && (!k || !v)) return RAC_ERR_INVALID;
+    if (!aligned(pool, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(workspace, 256) || !aligned(table, 4) ||
+        !aligned(lengths, 4) || !aligned(refs, 4) || !aligned(draft_start, 4) || !aligned(path, 4) ||
+        !aligned(committed, 4))
+        return RAC_ERR_ALIGN;
+    if (workspace_bytes < rac_cache_commit_workspace(cfg)) return RAC_ERR_CAPACITY;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    CommitRecord* record = reinterpret_cast<CommitRecord*>(ws);
+    int32_t* list = reinterpret_cast<int32_t*>(ws + up256((uint64_t)cfg->seqs * sizeof(CommitRecord)));
+    const int lp = log2_of(cfg->page_tokens);
+    const PlanArgs plan{table, lengths, refs, draft_start, path, committed, record, list, cfg->seqs, cfg->max_pages,
+                        cfg->pages, lp, draft_rows, max_path};
+    rac_status st = launch(reinterpret_cast<const void*>(cache_plan_kernel), 1, kPlanThreads, plan, 0, stream);
+    if (st != RAC_OK) return st;
+    const MoveArgs move{static_cast<uint8_t*>(pool), table, static_cast<const uint16_t*>(k),
+                        static_cast<const uint16_t*>(v), draft_start, path, record, kv_stride, layer_stride,
+                        cfg->k_scale, cfg->v_scale, cfg->layers, cfg->kv_heads, cfg->head_dim, lp, cfg->max_pages,
+                        cfg->pages, draft_rows, max_path};
+    const void* kernel = cfg->type == RAC_CACHE_FP8 ? reinterpret_cast<const void*>(cache_move_kernel<true>)
+                                                    : reinterpret_cast<const void*>(cache_move_kernel<false>);
+    return launch(kernel, (unsigned)(cfg->seqs * cfg->layers), kMoveThreads, move, 0, stream);
+}
+
+rac_status rac_cache_copy(const rac_cache_config* cfg, const void* src_pool, const int32_t* src, void* dst_pool,
+                          const int32_t* dst, int32_t n, rac_stream_t stream) {
+    if (!cache_valid(cfg) || n < 0 || n > cfg->pages) return RAC_ERR_INVALID;
+    if (n == 0) return RAC_OK;
+    if (!src_pool || !src || !dst_pool || !dst) return RAC_ERR_INVALID;
+    if (!aligned(src_pool, 16) || !aligned(dst_pool, 16) || !aligned(src, 4) || !aligned(dst, 4)) return RAC_ERR_ALIGN;
+    const uint64_t bytes = cache_page_bytes(cfg), parts = (bytes + kCopyBytes - 1) / kCopyBytes;
+    if (parts * (uint64_t)n * kCopyThreads >= (uint64_t(1) << 32)) return RAC_ERR_UNSUPPORTED;
+    const CopyArgs a{static_cast<const uint8_t*>(src_pool), static_cast<uint8_t*>(dst_pool), src, dst, bytes,
+                     cfg->pages, (int32_t)parts};
+    return launch(reinterpret_cast<const void*>(cache_copy_kernel), (unsigned)(parts * (uint64_t)n), kCopyThreads, a, 0,
+                  stream);
+}
+
+}  // extern "C"

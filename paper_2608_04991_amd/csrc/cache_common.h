@@ -1,0 +1,42 @@
+// What the kernels of the paged cache and of the tree attention share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "rac_cache.h"
+
+namespace {
+
+inline bool cache_valid(const rac_cache_config* c) {
+    if (!c || c->layers < 1 || c->layers > 1024 || c->kv_heads < 1 || c->kv_heads > 1024) return false;
+    if (c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16) return false;
+    if (c->page_tokens < 8 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1))) return false;
+    if (c->pages < 1 || c->pages > (1 << 24) || c->seqs < 1 || c->seqs > 4096 || c->max_pages < 1) return false;
+    if ((int64_t)c->max_pages * c->page_tokens > (1 << 30)) return false;
+    if (c->type != RAC_CACHE_BF16 && c->type != RAC_CACHE_FP16 && c->type != RAC_CACHE_FP8) return false;
+    return c->type != RAC_CACHE_FP8 || (c->k_scale > 0.0f && c->k_scale < __builtin_inff() && c->v_scale > 0.0f &&
+                                        c->v_scale < __builtin_inff());
+}
+
+inline int cache_elem_bytes(const rac_cache_config* c) { return c->type == RAC_CACHE_FP8 ? 1 : 2; }
+
+// Bytes of one page: all layers, keys and values.
+inline uint64_t cache_page_bytes(const rac_cache_config* c) {
+    return (uint64_t)c->layers * 2u * (uint64_t)c->kv_heads * (uint64_t)c->page_tokens * (uint64_t)c->head_dim *
+           (uint64_t)cache_elem_bytes(c);
+}
+
+inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+inline int log2_of(int v) { return __builtin_ctz((unsigned)v); }
+
+__device__ __forceinline__ int clamp_int(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+}  // namespace
