@@ -21,8 +21,12 @@ struct TreeArgs {
     int64_t q_stride, kv_stride, out_stride;
     int32_t layers, layer, heads, group, dim, log_page, pages, seqs, max_pages;
     int32_t rows, max_rows, draft_rows, max_draft, window, mask_words;
-    float scale;    // of the scores
+    float scale2;   // of the scores, times log2(e)
     float k_scale, v_scale;
+    int32_t target;     // parts wanted, a power of two (0: sequences are not split)
+    int32_t min_chunk;  // fewest key tiles of a part
+    float* parts;       // [slots] partial results
+    int32_t slots;
 };
 
 // What a sequence brings to the call, whatever the device arrays hold.
@@ -98,16 +102,543 @@ __device__ __forceinline__ Sight sight_of(const TreeArgs& a, const Seq& s, int i
     return r;
 }
 
-// The sequence that query row `row` belongs to, or -1.
-__device__ __forceinline__ int seq_of_row(const TreeArgs& a, int row) {
-    int lo = 0, hi = a.seqs;  // the last s with q_start[s] <= row
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (a.q_start[mid] <= row) lo = mid; else hi = mid;
-    }
-    return lo;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <int TYPE>
+__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (TYPE == RAC_CACHE_FP16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// Two floats in the 16-bit type, round to nearest even.
+template <int TYPE>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    if constexpr (TYPE == RAC_CACHE_FP16)
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, f16x2));
+    else
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+
+// Orders a wavefront's LDS writes before its later reads by other lanes.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The four lanes l, l ^ 16, l ^ 32, l ^ 48 of a query row.
+__device__ __forceinline__ float max_row(float v) {
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __builtin_fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __builtin_fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_row(float v) {
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// ---------------------------------------------------------------------------
+// The work.  Query rows of one key-value head are the (node, query head) pairs
+// of a sequence, node by node; a workgroup takes M of them and a run of key
+// tiles.  Keys come in tiles of kTile: the committed ones from the first that
+// the window reaches, then the drafted ones.
+constexpr int kTile = 32;
+constexpr int kWaves = 4;
+
+struct Work {
+    int seq, head, row_tile;
+    int chunk, chunks;  // the part of the key tiles, and how many parts there are
+    int slot;           // where its partial result goes
+    Seq q;
+};
+
+__device__ __forceinline__ int committed_tile0(const TreeArgs& a, const Seq& q) {
+    const int from = a.window > 0 && q.length > a.window ? q.length - a.window : 0;
+    return from / kTile;
+}
+
+// Key tiles of a sequence.
+__device__ __forceinline__ int key_tiles(const TreeArgs& a, const Seq& q) {
+    return (q.length + kTile - 1) / kTile - committed_tile0(a, q) + (q.n + kTile - 1) / kTile;
+}
+
+__device__ __forceinline__ int64_t sum_wave(int64_t v) {
+    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// Parts of at most this many key tiles, so that all parts together are about
+// a.target and of like size whatever the lengths.
+__device__ __forceinline__ int chunk_tiles(const TreeArgs& a, int rows_per_tile) {
+    if (a.target == 0) return 1 << 30;
+    const int lane = (int)threadIdx.x & 63;
+    int64_t total = 0;
+    for (int s0 = 0; s0 < a.seqs; s0 += 64) {
+        if (s0 + lane < a.seqs) {
+            const Seq q = seq_of(a, s0 + lane);
+            total += (int64_t)((q.m * a.group + rows_per_tile - 1) / rows_per_tile) * key_tiles(a, q);
+        }
+    }
+    total = sum_wave(total) * a.heads;
+    const int64_t c = (total + a.target - 1) >> (31 - __builtin_clz(a.target));
+    return __builtin_amdgcn_readfirstlane(c < a.min_chunk ? a.min_chunk : (int)(c < (1 << 30) ? c : (1 << 30)));
+}
+
+// Which work workgroup `block` has; false: none.  Every wavefront finds it by
+// itself (a lane a sequence), so that no barrier is needed.
+__device__ __forceinline__ bool find_work(const TreeArgs& a, int rows_per_tile, int block, Work& w) {
+    const int lane = (int)threadIdx.x & 63;
+    const int most = chunk_tiles(a, rows_per_tile);
+    int base = 0, slots = 0;
+    for (int s0 = 0; s0 < a.seqs; s0 += 64) {
+        Seq q{0, 0, 0, 0, 0};
+        int tiles = 0, chunks = 1;
+        if (s0 + lane < a.seqs) {
+            q = seq_of(a, s0 + lane);
+            tiles = (q.m * a.group + rows_per_tile - 1) / rows_per_tile;
+            const int keys = key_tiles(a, q);
+            chunks = keys > most ? (keys + most - 1) / most : 1;
+        }
+        const int units = tiles * chunks * a.heads;
+        int upto = units, slots_upto = chunks > 1 ? units : 0;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(upto, o), y = __shfl_up(slots_upto, o);
+            upto += lane >= o ? x : 0;
+            slots_upto += lane >= o ? y : 0;
+        }
+        const uint64_t past = __ballot(block < base + upto);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+            int i = block - (base + of(upto - units));
+            w.seq = s0 + at;
+            w.chunks = of(chunks);
+            const int n = of(tiles);
+            w.slot = slots + of(slots_upto - units) + i;
+            w.head = i % a.heads;
+            i /= a.heads;
+            w.chunk = i % w.chunks;
+            w.row_tile = n - 1 - i / w.chunks;  // (the last rows of a causal sequence see most)
+            w.q = Seq{of(q.q0), of(q.m), of(q.d0), of(q.n), of(q.length)};
+            // (ranges that overlap, as a broken q_start has them, may ask for more parts than there is room for)
+            return w.chunks == 1 || (uint32_t)w.slot < (uint32_t)a.slots;
+        }
+        base += __builtin_amdgcn_readlane(upto, 63);
+        slots += __builtin_amdgcn_readlane(slots_upto, 63);
+    }
+    return false;
+}
+
+// ---------------------------------------------------------------------------
+// LDS: a tile of 16-bit keys or values is kTile rows of DP / 8 pieces of 16
+// bytes; piece c of a row sits at c ^ swizzle(row), so that 16 lanes that read
+// the same piece of 16 rows, or write the pieces of one row, touch every bank
+// once.
+template <int DP>
+__device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t c) {
+    if constexpr (DP == 64)
+        return row * 8u + (c ^ ((row >> 1) & 7u));
+    else
+        return row * (DP / 8) + (c ^ (row & 15u));
+}
+
+// Four of eight keys of channel 16 dt + lane % 16: the transposing read takes
+// from the 16 lanes of a group the four 8-byte parts of four rows.
+template <int DP>
+__device__ __forceinline__ u32x2 read_column(const u32x4* tile, uint32_t lane, uint32_t dt, uint32_t half) {
+    const uint32_t row = 16u * half + 4u * (lane >> 4) + ((lane >> 2) & 3u), c = 2u * dt + ((lane >> 1) & 1u);
+    const u32x2* at = reinterpret_cast<const u32x2*>(tile + piece_at<DP>(row, c)) + (lane & 1u);
+    typedef __attribute__((address_space(3))) s16x4* lds;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)at));
+}
+
+// What a wavefront keeps of its TM x 16 query rows.  With keys (values) as the
+// first operand of the matrix cores, lane l holds everything of row l % 16:
+// scores of keys 16 t + 4 (l / 16) + i, outputs of channels 16 t + 4 (l / 16) +
+// i; the weights of the former are the second operand of the latter as they
+// lie, if the values' keys are taken in the same order.
+template <int TYPE, int DP, int TM>
+struct Rows {
+    u32x4 q[TM][DP / 32];
+    f32x4 o[TM][DP / 16];
+    float m[TM];  // reference of the exponentials, log2: at most 8 below the largest score so far
+    float l[TM];  // sum of the weights over this lane's keys
+    bool alone;   // a value that some row must not see is an infinity or NaN: the rows are redone one by one
+
+    __device__ __forceinline__ void start() {
+        alone = false;
+#pragma unroll
+        for (int r = 0; r < TM; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.0f;
+#pragma unroll
+            for (int t = 0; t < DP / 16; ++t) o[r][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    }
+
+    // One tile.  kl, vl: the tile in LDS; c: factor of the scores, with log2(e)
+    // in it; vs: factor of the values.  plain: every row sees every key; else
+    // bits[r] has the keys that this lane's row of r sees, and `there` the keys
+    // whose values are loaded (the others are zeros).
+    __device__ __forceinline__ void tile(const u32x4* kl, const u32x4* vl, float c, float vs, bool plain,
+                                         const uint32_t (&bits)[TM], uint32_t there) {
+        const uint32_t lane = threadIdx.x & 63u;
+        f32x4 s[TM][2];
+#pragma unroll
+        for (int r = 0; r < TM; ++r) s[r][0] = s[r][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const u32x4 k = kl[piece_at<DP>(16u * h + (lane & 15u), 4u * t + (lane >> 4))];
+#pragma unroll
+                for (int r = 0; r < TM; ++r) s[r][h] = mma<TYPE>(k, q[r][t], s[r][h]);
+            }
+        }
+        bool mixed = false;
+        if (!plain) {
+            const uint32_t first = 4u * (lane >> 4);
+#pragma unroll
+            for (int r = 0; r < TM; ++r) {
+                mixed |= bits[r] != there;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        s[r][h][i] = (bits[r] >> (16u * h + first + i)) & 1u ? s[r][h][i] : -INFINITY;
+            }
+            mixed = __any(mixed);
+        }
+        float top[TM];
+        bool grow = false;
+#pragma unroll
+        for (int r = 0; r < TM; ++r) {
+            const float x = __builtin_fmaxf(__builtin_fmaxf(s[r][0][0], s[r][0][1]), __builtin_fmaxf(s[r][0][2], s[r][0][3]));
+            const float y = __builtin_fmaxf(__builtin_fmaxf(s[r][1][0], s[r][1][1]), __builtin_fmaxf(s[r][1][2], s[r][1][3]));
+            top[r] = __builtin_fmaxf(x, y) * c;
+            grow |= top[r] > m[r] + 8.0f;
+        }
+        if (__any(grow)) {  // (seldom: the reference need not be the maximum, only near it)
+#pragma unroll
+            for (int r = 0; r < TM; ++r) {
+                const float now = __builtin_fmaxf(m[r], max_row(top[r]));
+                const float keep = now == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[r] - now);
+                m[r] = now;
+                l[r] = l[r] * keep;
+#pragma unroll
+                for (int t = 0; t < DP / 16; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[r][t][i] = o[r][t][i] * keep;
+            }
+        }
+        u32x4 p[TM];
+#pragma unroll
+        for (int r = 0; r < TM; ++r) {
+            const float ref = m[r] == -INFINITY ? 0.0f : m[r];
+            float e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][i / 4][i % 4], c, -ref));
+            l[r] = l[r] + (((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (TYPE == RAC_CACHE_FP8)
+                    p[r][i] = pack2<TYPE>(e[2 * i] * vs, e[2 * i + 1] * vs);
+                else
+                    p[r][i] = pack2<TYPE>(e[2 * i], e[2 * i + 1]);
+            }
+        }
+        if (mixed) {
+            // some row must not see some value: a weight of 0 hides it unless
+            // it is an infinity or NaN (all exponent bits set)
+            constexpr uint32_t kExp = TYPE == RAC_CACHE_FP16 ? 0x7C00u : 0x7F80u;
+            bool odd = false;
+            for (uint32_t t = 0; t < DP / 16; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const u32x2 v = read_column<DP>(vl, lane, t, h);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        odd |= (v[i] & kExp) == kExp || (v[i] & (kExp << 16)) == (kExp << 16);
+                }
+            alone |= __any(odd);
+        }
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t) {
+            const u32x2 lo = read_column<DP>(vl, lane, t, 0), hi = read_column<DP>(vl, lane, t, 1);
+            const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+            for (int r = 0; r < TM; ++r) o[r][t] = mma<TYPE>(v, p[r], o[r][t]);
+        }
+    }
+};
+
+// Where a row lives (its node and query head), and what it sees.
+struct RowAt {
+    int node, head;
+    Sight see;
+};
+
+__device__ __forceinline__ RowAt row_at(const TreeArgs& a, const Work& w, int row) {
+    const int last = w.q.m * a.group - 1;
+    row = row < last ? row : last;  // (rows past the last repeat it and are not stored)
+    RowAt r;
+    r.node = row / a.group;
+    r.head = w.head * a.group + row % a.group;
+    r.see = sight_of(a, w.q, r.node);
+    return r;
+}
+
+// The arguments once more.  What only the start, the end or a rare path needs is
+// read when it is needed: a kernel that keeps all of it in scalar registers over
+// its loop has too few of them.
+__device__ __forceinline__ TreeArgs args_again() {
+    TreeArgs a;
+#ifdef __HIP_DEVICE_COMPILE__
+    uint64_t p = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    __builtin_memcpy(&a, (const void*)(const __attribute__((address_space(4))) void*)p, sizeof a);
+#endif
+    return a;
+}
+
+// The key axis of a workgroup, as its loop needs it.
+struct Axis {
+    const uint8_t* pool;   // keys of this layer and head in page 0
+    uint64_t page_stride;  // bytes
+    uint32_t side;         // bytes from a page's keys to its values
+    const int32_t* row;    // the sequence's table entries
+    const uint16_t* k;     // drafted keys and values of this sequence and head
+    const uint16_t* v;
+    int64_t kv_stride;
+    int max_pages, log_page, pages, dim, length, n;
+    // the tiles that the rows see at all: committed ones [ca, ca + committed), then drafted ones from da on
+    int ca, committed, da, count;
+};
+
+template <int TYPE>
+__device__ __forceinline__ Axis axis_of(const TreeArgs& a, const Work& w, int from, int first, int end) {
+    constexpr int kB = TYPE == RAC_CACHE_FP8 ? 1 : 2;
+    const uint64_t plane = ((uint64_t)a.dim << a.log_page) * kB;
+    Axis x;
+    x.pool = a.pool + ((uint64_t)a.layer * 2 * a.heads + w.head) * plane;
+    x.page_stride = plane * a.heads * 2 * a.layers;
+    x.side = (uint32_t)(plane * a.heads);
+    x.row = a.table + (size_t)w.seq * a.max_pages;
+    const int64_t o = w.q.d0 * a.kv_stride + (int64_t)w.head * a.dim;
+    x.k = a.k + o;
+    x.v = a.v + o;
+    x.kv_stride = a.kv_stride;
+    x.max_pages = a.max_pages;
+    x.log_page = a.log_page;
+    x.pages = a.pages;
+    x.dim = a.dim;
+    x.length = w.q.length;
+    x.n = w.q.n;
+    const int c0 = committed_tile0(a, w.q), all = key_tiles(a, w.q), n = (w.q.length + kTile - 1) / kTile - c0;
+    const int each = all / w.chunks, more = all % w.chunks;
+    const int lo = w.chunk * each + (w.chunk < more ? w.chunk : more), hi = lo + each + (w.chunk < more);
+    x.ca = c0 + (lo < n ? lo : n);
+    x.da = lo > n ? lo - n : 0;
+    int cb = c0 + (hi < n ? hi : n), db = hi > n ? hi - n : 0;
+    if (x.ca < from / kTile) x.ca = from / kTile;
+    if (x.da < first / kTile) x.da = first / kTile;
+    const int e = (end + kTile - 1) / kTile;
+    if (db > e) db = e;
+    x.committed = cb > x.ca ? cb - x.ca : 0;
+    x.count = x.committed + (db > x.da ? db - x.da : 0);
+    return x;
+}
+
+// The table entries of eight keys each.
+struct Pages {
+    int p[4];
+};
+
+__device__ __forceinline__ Pages pages_of(const Axis& x, int tile) {
+    using cptr = const __attribute__((address_space(4))) int32_t*;  // read-only in this launch: scalar loads
+    Pages r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int at = (tile * kTile + 8 * i) >> x.log_page;
+        r.p[i] = ((cptr)x.row)[at < x.max_pages ? at : x.max_pages - 1];
+    }
+    return r;
+}
+
+// One tile's keys and values (or the rows [ROW0, ROW0 + ROWS) of it) on their
+// way from memory to LDS, through registers: neighbouring lanes take the 16-byte
+// pieces of a row.
+template <int TYPE, int DP, int ROWS>
+struct Load {
+    static constexpr int kPieces = DP / 8, kRowsAtOnce = 64 / kPieces, kLoads = ROWS / kRowsAtOnce;       // 16 bits
+    static constexpr int kPieces8 = DP / 16, kRowsAtOnce8 = 64 / kPieces8, kLoads8 = ROWS / kRowsAtOnce8;  // 8 bits
+    u32x4 k[kLoads], v[kLoads];
+    bool narrow;
+
+    // `valid`: the keys of the tile that exist.
+    __device__ __forceinline__ void committed(const Axis& ax, int tile, const Pages& pg, uint32_t valid, int row0) {
+        const uint32_t lane = threadIdx.x & 63u;
+        constexpr int kB = TYPE == RAC_CACHE_FP8 ? 1 : 2;
+        constexpr int kN = TYPE == RAC_CACHE_FP8 ? kLoads8 : kLoads, kR = TYPE == RAC_CACHE_FP8 ? kRowsAtOnce8 : kRowsAtOnce;
+        constexpr uint32_t kP = TYPE == RAC_CACHE_FP8 ? kPieces8 : kPieces;
+        narrow = TYPE == RAC_CACHE_FP8;
+        const uint32_t c = lane % kP, in = lane / kP;
+        // (eight aligned rows lie in one page: its address is the same in all
+        // lanes, but for the second eight of sixteen)
+        const uint32_t inner = (kR > 8 ? in & 7u : in) * (uint32_t)(ax.dim * kB) + c * 16u;
+        const auto at = [&](int g, int row) {
+            return ax.pool + (uint64_t)(uint32_t)pg.p[g] * ax.page_stride +
+                   ((uint32_t)(tile * kTile + row) & ((1u << ax.log_page) - 1u)) * (uint32_t)(ax.dim * kB);
+        };
+        const bool whole = valid == ~0u && ax.dim == DP;
+#pragma unroll
+        for (int x = 0; x < kN; ++x) {
+            const int g = x * kR / 8, row = row0 + x * kR;  // (ROWS == 16: row0 is 0 or 16)
+            const uint8_t* from = ROWS == 16 && row0 ? at((g + 2) & 3, row) : at(g & 3, row);
+            if constexpr (kR > 8) {
+                const uint8_t* other = ROWS == 16 && row0 ? at((g + 3) & 3, row + 8) : at((g + 1) & 3, row + 8);
+                from = in >= 8u ? other : from;
+            }
+            if (whole) {
+                k[x] = *reinterpret_cast<const u32x4*>(from + inner);
+                v[x] = *reinterpret_cast<const u32x4*>(from + inner + ax.side);
+            } else {
+                k[x] = v[x] = u32x4{0u, 0u, 0u, 0u};
+                if (c * (16 / kB) < (uint32_t)ax.dim && (valid >> (row + in)) & 1u) {
+                    k[x] = *reinterpret_cast<const u32x4*>(from + inner);
+                    v[x] = *reinterpret_cast<const u32x4*>(from + inner + ax.side);
+                }
+            }
+        }
+    }
+
+    __device__ __forceinline__ void drafted(const Axis& ax, int tile, uint32_t valid, int row0) {
+        const uint32_t lane = threadIdx.x & 63u, c = lane % kPieces, in = lane / kPieces;
+        narrow = false;
+#pragma unroll
+        for (int x = 0; x < kLoads; ++x) {
+            const uint32_t row = row0 + x * kRowsAtOnce + in;
+            k[x] = v[x] = u32x4{0u, 0u, 0u, 0u};
+            if (c * 8u < (uint32_t)ax.dim && (valid >> row) & 1u) {
+                const int64_t o = (int64_t)(tile * kTile + (int)row) * ax.kv_stride + 8u * c;
+                k[x] = *reinterpret_cast<const u32x4*>(ax.k + o);
+                v[x] = *reinterpret_cast<const u32x4*>(ax.v + o);
+            }
+        }
+    }
+
+    // clean: infinities and NaNs among the values become zeros.
+    __device__ __forceinline__ void put(u32x4* kl, u32x4* vl, int row0, bool clean) {
+        const uint32_t lane = threadIdx.x & 63u;
+        if (TYPE == RAC_CACHE_FP8 && narrow) {
+            const uint32_t c = lane % kPieces8, in = lane / kPieces8;
+#pragma unroll
+            for (int x = 0; x < kLoads8; ++x) {
+                const uint32_t row = row0 + x * kRowsAtOnce8 + in;
+#pragma unroll
+                for (uint32_t y = 0; y < 2; ++y) {
+                    const uint32_t at = piece_at<DP>(row, 2u * c + y);
+                    u32x4 wide = widen8(v[x][2 * y], v[x][2 * y + 1]);
+                    if (clean) wide = finite(wide);
+                    kl[at] = widen8(k[x][2 * y], k[x][2 * y + 1]);
+                    vl[at] = wide;
+                }
+            }
+            return;
+        }
+        const uint32_t c = lane % kPieces, in = lane / kPieces;
+#pragma unroll
+        for (int x = 0; x < kLoads; ++x) {
+            const uint32_t at = piece_at<DP>(row0 + x * kRowsAtOnce + in, c);
+            if (clean) v[x] = finite(v[x]);
+            kl[at] = k[x];
+            vl[at] = v[x];
+        }
+    }
+
+    static __device__ __forceinline__ u32x4 finite(u32x4 x) {
+        constexpr uint32_t kExp = TYPE == RAC_CACHE_FP16 ? 0x7C00u : 0x7F80u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] &= (x[i] & kExp) == kExp ? 0xFFFF0000u : ~0u;
+            x[i] &= (x[i] & (kExp << 16)) == (kExp << 16) ? 0xFFFFu : ~0u;
+        }
+        return x;
+    }
+
+    // Eight e4m3 as bf16 (exact).
+    static __device__ __forceinline__ u32x4 widen8(uint32_t a, uint32_t b) {
+        u32x4 r;
+        r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false));
+        r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true));
+        r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false));
+        r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true));
+        return r;
+    }
+};
+
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+
+// The keys of committed tile `tile` that exist.
+__device__ __forceinline__ uint32_t committed_there(const Axis& x, int tile, const Pages& pg) {
+    uint32_t r = low_bits(x.length - tile * kTile);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if ((uint32_t)pg.p[i] >= (uint32_t)x.pages) r &= ~(0xFFu << (8 * i));
+    return r;
+}
+
+// What the rows of a workgroup see, in LDS: it is read for few tiles.
+struct Seen {
+    int from, first, end, mask_row;
+};
+
+__device__ __forceinline__ uint32_t bits_of(const Seen& r, bool past, int tile) {
+    if (past) return ~low_bits(r.from - tile * kTile);
+    uint32_t b = low_bits(r.end - tile * kTile) & ~low_bits(r.first - tile * kTile);
+    const TreeArgs a = args_again();
+    if (a.mask && b)  // (a mask reaches r.end)
+        b &= reinterpret_cast<const uint32_t*>(a.mask + (size_t)r.mask_row * a.mask_words)[tile];
+    return b;
+}
+
+__device__ __forceinline__ int min_wave(int v) {
+    for (int o = 1; o < 16; o <<= 1) { const int x = __shfl_xor(v, o); v = x < v ? x : v; }
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int max_wave(int v) {
+    for (int o = 1; o < 16; o <<= 1) { const int x = __shfl_xor(v, o); v = x > v ? x : v; }
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+// A partial result: [M][DP] outputs, M references, M sums.
+__device__ __forceinline__ float* partial(const TreeArgs& a, int slot, int M, int DP) {
+    return a.parts + (size_t)slot * (M * (DP + 2));
+}
+
+__device__ __forceinline__ uint16_t* out_at(const TreeArgs& a, const Work& w, int node, int head) {
+    return a.out + (int64_t)(w.q.q0 + node) * a.out_stride + (int64_t)head * a.dim;
+}
+
+// Of a reference (log2) and a sum of weights.
+__device__ __forceinline__ float lse_of(float m, float l) {
+    return l == 0.0f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f;
+}
+
+// A row by itself, over the same keys: a lane per key for the scores, a lane per
+// channel for the values, of which only those that the row sees are read.  Where
+// a tile holds infinities or NaNs that some row must not see, the tiles are
+// taken again with zeros in their place, and a row that does see one gets its
+// result from here.
 template <int TYPE>
 __device__ __forceinline__ float widen(const uint8_t* p, int i, bool page) {
     if (TYPE == RAC_CACHE_FP8 && page) return __builtin_amdgcn_cvt_f32_fp8((int)p[i], 0);
@@ -117,88 +648,428 @@ __device__ __forceinline__ float widen(const uint8_t* p, int i, bool page) {
 }
 
 template <int TYPE>
-__device__ __forceinline__ uint16_t narrow(float v) {
-    if (TYPE == RAC_CACHE_FP16) return __builtin_bit_cast(uint16_t, (_Float16)v);
-    return __builtin_bit_cast(uint16_t, (__bf16)v);
-}
-
-// One wavefront per (row, query head): a lane per key for the scores, a lane
-// per channel for the values.
-template <int TYPE>
-__global__ __launch_bounds__(64) void tree_row_kernel(TreeArgs a) {
-    __shared__ float qs[256], ps[64];
-    __shared__ uint64_t at[64];
-    const int hq = a.heads * a.group, lane = (int)threadIdx.x;
-    const int row = (int)blockIdx.x / hq, h = (int)blockIdx.x % hq, kvh = h / a.group;
-    const int s = seq_of_row(a, row);
-    const Seq q = seq_of(a, s);
-    const int i = row - q.q0;
-    if (i < 0 || i >= q.m) return;
-    const Sight see = sight_of(a, q, i);
-    const uint64_t* words = a.mask ? a.mask + (size_t)row * a.mask_words : nullptr;
-    for (int c = lane; c < a.dim; c += 64)
-        qs[c] = widen<TYPE>(reinterpret_cast<const uint8_t*>(a.q + row * a.q_stride + (int64_t)h * a.dim), c, false) * a.scale;
+__device__ __forceinline__ void row_alone(const TreeArgs& a, const Work& w, const Axis& ax, int row, float* part, int in,
+                                          int M, int DP) {
+    const int lane = (int)threadIdx.x & 63;
+    const RowAt at = row_at(a, w, row);
+    const uint8_t* q = reinterpret_cast<const uint8_t*>(a.q + (int64_t)(w.q.q0 + at.node) * a.q_stride + (int64_t)at.head * a.dim);
     const int kb = TYPE == RAC_CACHE_FP8 ? 1 : 2;
     const uint64_t plane = ((uint64_t)a.dim << a.log_page) * kb;
     float top = -INFINITY, total = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int part = 0; part < 2; ++part) {  // committed, then drafted
-        const int end = part ? see.end : q.length;
-        for (int j0 = part ? see.first : see.from; j0 < end; j0 += 64) {
+    for (int side = 0; side < 2; ++side) {  // committed, then drafted
+        int j0 = (side ? ax.da : ax.ca) * kTile, j1 = j0 + (side ? ax.count - ax.committed : ax.committed) * kTile;
+        const int from = side ? at.see.first : at.see.from, end = side ? at.see.end : w.q.length;
+        j0 = j0 < from ? from : j0;
+        j1 = j1 < end ? j1 : end;
+        for (; j0 < j1; j0 += 64) {
             const int j = j0 + lane;
-            bool seen = j < end;
+            bool seen = j < j1;
             const uint8_t *kp = nullptr, *vp = nullptr;
-            if (seen && part == 0) {
-                const int p = a.table[(size_t)s * a.max_pages + (j >> a.log_page)];
+            if (seen && side == 0) {
+                const int p = a.table[(size_t)w.seq * a.max_pages + (j >> a.log_page)];
                 seen = p >= 0 && p < a.pages;
                 if (seen) {
-                    const uint64_t b = (((uint64_t)p * a.layers + a.layer) * 2 * a.heads + kvh) * plane +
-                                       (uint64_t)((j & ((1 << a.log_page) - 1)) * a.dim * kb);
-                    kp = a.pool + b;
+                    kp = a.pool + (((uint64_t)p * a.layers + a.layer) * 2 * a.heads + w.head) * plane +
+                         (uint64_t)((j & ((1 << a.log_page) - 1)) * a.dim * kb);
                     vp = kp + a.heads * plane;
                 }
             } else if (seen) {
-                seen = !words || ((words[j >> 6] >> (j & 63)) & 1);
-                const int64_t o = (q.d0 + j) * a.kv_stride + (int64_t)kvh * a.dim;
+                seen = !a.mask || ((a.mask[(size_t)(w.q.q0 + at.node) * a.mask_words + (j >> 6)] >> (j & 63)) & 1);
+                const int64_t o = (int64_t)(w.q.d0 + j) * a.kv_stride + (int64_t)w.head * a.dim;
                 kp = reinterpret_cast<const uint8_t*>(a.k + o);
                 vp = reinterpret_cast<const uint8_t*>(a.v + o);
             }
             float sc = 0.0f;
-            __syncthreads();
             if (seen)
-                for (int c = 0; c < a.dim; ++c) sc = __builtin_fmaf(qs[c], widen<TYPE>(kp, c, part == 0), sc);
-            if (TYPE == RAC_CACHE_FP8 && part == 0) sc = sc * a.k_scale;
+                for (int c = 0; c < a.dim; ++c)
+                    sc = __builtin_fmaf(widen<TYPE>(q, c, false), widen<TYPE>(kp, c, side == 0), sc);
+            sc = sc * (TYPE == RAC_CACHE_FP8 && side == 0 ? a.scale2 * a.k_scale : a.scale2);
             const uint64_t live = __ballot(seen);
             float m = seen ? sc : -INFINITY;
             for (int o = 1; o < 64; o <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, o));
             m = __builtin_fmaxf(m, top);
-            const float ref = m == -INFINITY ? 0.0f : m;
-            const float p = seen ? __expf(sc - ref) : 0.0f, keep = __expf(top - ref);
-            float sum = p;
+            const float ref = m == -INFINITY ? 0.0f : m, keep = __builtin_amdgcn_exp2f(top - ref);
+            float p = seen ? __builtin_amdgcn_exp2f(sc - ref) : 0.0f, sum = p;
             for (int o = 1; o < 64; o <<= 1) sum = sum + __shfl_xor(sum, o);
             total = __builtin_fmaf(total, keep, sum);
             top = m;
-            ps[lane] = TYPE == RAC_CACHE_FP8 && part == 0 ? p * a.v_scale : p;
-            at[lane] = reinterpret_cast<uint64_t>(vp);
-            __syncthreads();
+            if (TYPE == RAC_CACHE_FP8 && side == 0) p = p * a.v_scale;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int c = lane + 64 * x;
-                if (c >= a.dim) break;
-                float f = acc[x] * keep;
-                for (uint64_t rest = live; rest; rest &= rest - 1) {
-                    const int y = __builtin_ctzll(rest);
-                    f = __builtin_fmaf(ps[y], widen<TYPE>(reinterpret_cast<const uint8_t*>(at[y]), c, part == 0), f);
-                }
-                acc[x] = f;
+            for (int x = 0; x < 4; ++x) acc[x] = acc[x] * keep;
+            for (uint64_t rest = live; rest; rest &= rest - 1) {
+                const int y = __builtin_ctzll(rest);
+                const float py = __shfl(p, y);
+                const uint8_t* vy = reinterpret_cast<const uint8_t*>(__shfl((unsigned long long)vp, y));
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    if (lane + 64 * x < a.dim) acc[x] = __builtin_fmaf(py, widen<TYPE>(vy, lane + 64 * x, side == 0), acc[x]);
             }
         }
     }
-    const bool none = total == 0.0f;
+    bool odd = !(__builtin_fabsf(total) < INFINITY);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) odd |= !(__builtin_fabsf(acc[x]) < INFINITY);
+    if (!__any(odd)) return;
+#pragma unroll
     for (int x = 0; x < 4; ++x) {
         const int c = lane + 64 * x;
-        if (c < a.dim) a.out[row * a.out_stride + (int64_t)h * a.dim + c] = narrow<TYPE>(none ? 0.0f : acc[x] / total);
+        if (part) {
+            if (c < DP) part[in * DP + c] = acc[x];
+        } else if (c < a.dim) {
+            out_at(a, w, at.node, at.head)[c] = (uint16_t)pack2<TYPE>(acc[x] / total, 0.0f);
+        }
     }
-    if (a.lse && lane == 0) a.lse[(size_t)row * hq + h] = none ? -INFINITY : top + logf(total);
+    if (part && lane == 0) {
+        part[M * DP + in] = top;
+        part[M * DP + M + in] = total;
+    }
+}
+
+// The queries of a wavefront's rows, and what they see: into registers and LDS.
+// Returns the extremes: first committed position any (every) row sees from, the
+// first drafted token, and the end of the drafted ones.
+struct Reach {
+    int from_lo, from_hi, first, end;
+};
+
+template <int TYPE, int DP, int TM>
+__device__ __forceinline__ Reach take_rows(const TreeArgs& a, const Work& w, int row0, Rows<TYPE, DP, TM>& rows, Seen* seen) {
+    const uint32_t lane = threadIdx.x & 63u;
+    Reach x{1 << 30, 0, 1 << 30, 0};
+#pragma unroll
+    for (int r = 0; r < TM; ++r) {
+        const RowAt at = row_at(a, w, row0 + 16 * r + (int)(lane & 15u));
+        if (lane < 16u) seen[16 * r + lane] = Seen{at.see.from, at.see.first, at.see.end, w.q.q0 + at.node};
+        x.from_lo = at.see.from < x.from_lo ? at.see.from : x.from_lo;
+        x.from_hi = at.see.from > x.from_hi ? at.see.from : x.from_hi;
+        x.first = at.see.first < x.first ? at.see.first : x.first;
+        x.end = at.see.end > x.end ? at.see.end : x.end;
+        const uint16_t* q = a.q + (int64_t)(w.q.q0 + at.node) * a.q_stride + (int64_t)at.head * a.dim;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) {
+            const int c = 32 * t + 8 * (int)(lane >> 4);
+            rows.q[r][t] = u32x4{0u, 0u, 0u, 0u};
+            if (c < a.dim) rows.q[r][t] = *reinterpret_cast<const u32x4*>(q + c);
+        }
+    }
+    return Reach{min_wave(x.from_lo), max_wave(x.from_hi), min_wave(x.first), max_wave(x.end)};
+}
+
+// Few rows: all wavefronts hold the same 16 TM rows and take key tiles in
+// turn, each through LDS of its own, without a barrier until they join.
+template <int TYPE, int DP, int TM>
+__global__ __launch_bounds__(64 * kWaves, TYPE != RAC_CACHE_FP8 && TM * DP <= 128 ? 2 : 1) void tree_few_kernel(TreeArgs a) {
+    constexpr int M = 16 * TM, kTileP = kTile * DP / 8, kPad = DP + 4;
+    constexpr int kStage = 2 * kTileP * 16 * kWaves, kJoin = kWaves * 16 * kPad * 4;
+    __shared__ alignas(16) uint8_t mem[kStage > kJoin ? kStage : kJoin];
+    __shared__ float wm[kWaves][M], wl[kWaves][M];
+    __shared__ Seen seen[kWaves][M];
+    const uint32_t lane = threadIdx.x & 63u;
+    const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
+    Rows<TYPE, DP, TM> rows;
+    Axis ax;
+    int from_hi;
+    {
+        Work w;
+        if (!find_work(a, M, (int)blockIdx.x, w)) return;
+        const Reach x = take_rows(a, w, w.row_tile * M, rows, seen[wv]);
+        from_hi = x.from_hi;
+        ax = axis_of<TYPE>(a, w, x.from_lo, x.first, x.end);
+    }
+    u32x4* const kl = reinterpret_cast<u32x4*>(mem) + wv * 2 * kTileP;
+    u32x4* const vl = kl + kTileP;
+    Load<TYPE, DP, kTile> ld;
+    const float c16 = a.scale2, c8 = a.scale2 * a.k_scale, v8 = a.v_scale;
+    bool clean = false;
+again:
+    rows.start();
+    uint32_t there = 0;
+    Pages pg{};
+    auto load = [&](int i) {
+        if (i < ax.committed) {
+            there = committed_there(ax, ax.ca + i, pg);
+            ld.committed(ax, ax.ca + i, pg, there, 0);
+        } else {
+            there = low_bits(ax.n - (ax.da + i - ax.committed) * kTile);
+            ld.drafted(ax, ax.da + i - ax.committed, there, 0);
+        }
+    };
+    auto fetch = [&](int i) { if (i < ax.committed) pg = pages_of(ax, ax.ca + i); };
+    fetch(wv);
+    if (wv < ax.count) load(wv);
+    fetch(wv + kWaves);
+    for (int i = wv; i < ax.count; i += kWaves) {
+        ld.put(kl, vl, 0, clean);
+        const uint32_t now = there;
+        if (i + kWaves < ax.count) load(i + kWaves);
+        fetch(i + 2 * kWaves);
+        wave_sync();
+        uint32_t bits[TM];
+        const bool past = i < ax.committed;
+        const int tile = past ? ax.ca + i : ax.da + i - ax.committed;
+        const bool plain = past && now == ~0u && tile * kTile >= from_hi;
+        if (!plain) {
+#pragma unroll
+            for (int r = 0; r < TM; ++r) bits[r] = now & bits_of(seen[wv][16 * r + (lane & 15u)], past, tile);
+        }
+        const bool narrow = TYPE == RAC_CACHE_FP8 && past;
+        rows.tile(kl, vl, narrow ? c8 : c16, narrow ? v8 : 1.0f, plain, bits, now);
+        wave_sync();
+    }
+    if (!clean && __syncthreads_or(rows.alone)) {
+        clean = true;
+        goto again;
+    }
+    // join the wavefronts
+#pragma unroll
+    for (int r = 0; r < TM; ++r) {
+        const float l = sum_row(rows.l[r]);
+        if (lane < 16u) {
+            wm[wv][16 * r + lane] = rows.m[r];
+            wl[wv][16 * r + lane] = l;
+        }
+    }
+    __syncthreads();
+    const TreeArgs b = args_again();
+    Work w;
+    find_work(b, M, (int)blockIdx.x, w);
+    float* const sums = reinterpret_cast<float*>(mem);
+    float* const part = w.chunks > 1 ? partial(b, w.slot, M, DP) : nullptr;
+#pragma unroll
+    for (int r = 0; r < TM; ++r) {
+        const int in = 16 * r + (int)(lane & 15u);
+        float top = wm[0][in];
+#pragma unroll
+        for (int x = 1; x < kWaves; ++x) top = __builtin_fmaxf(top, wm[x][in]);
+        const float f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(rows.m[r] - top);
+        if (r) __syncthreads();
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t)
+            *reinterpret_cast<f32x4*>(sums + (wv * 16 + (lane & 15u)) * kPad + 16 * t + 4 * (lane >> 4)) =
+                f32x4{rows.o[r][t][0] * f, rows.o[r][t][1] * f, rows.o[r][t][2] * f, rows.o[r][t][3] * f};
+        __syncthreads();
+        for (int e = (int)threadIdx.x; e < 16 * DP / 4; e += 64 * kWaves) {
+            const int row = e / (DP / 4), c = 4 * (e % (DP / 4)), ir = 16 * r + row;
+            f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+            float best = wm[0][ir], l = 0.0f;
+#pragma unroll
+            for (int x = 1; x < kWaves; ++x) best = __builtin_fmaxf(best, wm[x][ir]);
+#pragma unroll
+            for (int x = 0; x < kWaves; ++x) {
+                const f32x4 y = *reinterpret_cast<const f32x4*>(sums + (x * 16 + row) * kPad + c);
+                v = f32x4{v[0] + y[0], v[1] + y[1], v[2] + y[2], v[3] + y[3]};
+                l = l + wl[x][ir] * (best == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(wm[x][ir] - best));
+            }
+            const int all = w.row_tile * M + ir;
+            if (all >= w.q.m * b.group) continue;
+            if (part) {
+                *reinterpret_cast<f32x4*>(part + ir * DP + c) = v;
+                if (c == 0) {
+                    part[M * DP + ir] = best;
+                    part[M * DP + M + ir] = l;
+                }
+                continue;
+            }
+            const int node = all / b.group, head = w.head * b.group + all % b.group;
+            const bool none = l == 0.0f;
+            if (c < b.dim)
+                *reinterpret_cast<u32x2*>(out_at(b, w, node, head) + c) =
+                    none ? u32x2{0u, 0u} : u32x2{pack2<TYPE>(v[0] / l, v[1] / l), pack2<TYPE>(v[2] / l, v[3] / l)};
+            if (c == 0 && b.lse) b.lse[(size_t)(w.q.q0 + node) * b.heads * b.group + head] = lse_of(best, l);
+        }
+    }
+    if (clean) {
+        __syncthreads();
+        for (int in = wv; in < M && w.row_tile * M + in < w.q.m * b.group; in += kWaves)
+            row_alone<TYPE>(b, w, ax, w.row_tile * M + in, part, in, M, DP);
+    }
+}
+
+// Many rows: each wavefront holds 16 TM rows of its own, and all share the
+// keys and values of two tiles at a time in LDS, two such pairs in turn.
+template <int TYPE, int DP, int TM>
+__global__ __launch_bounds__(64 * kWaves, TM * DP <= 256 && DP < 256 ? 2 : 1) void tree_many_kernel(TreeArgs a) {
+    constexpr int M = 16 * TM * kWaves, kTileP = kTile * DP / 8;
+    __shared__ u32x4 mem[2][2][2][kTileP];  // pair, tile, keys or values
+    __shared__ uint32_t exist[2][2];         // the keys of a tile that exist
+    __shared__ Seen seen[kWaves][16 * TM];
+    __shared__ Reach reach[kWaves];
+    const uint32_t lane = threadIdx.x & 63u;
+    const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
+    Rows<TYPE, DP, TM> rows;
+    Axis ax;
+    Reach x;
+    bool busy;  // whether this wavefront has rows
+    {
+        Work w;
+        if (!find_work(a, M, (int)blockIdx.x, w)) return;
+        const int row0 = w.row_tile * M + 16 * TM * wv;
+        busy = row0 < w.q.m * a.group;
+        x = take_rows(a, w, row0, rows, seen[wv]);
+        if (lane == 0u) reach[wv] = x;
+        __syncthreads();
+        Reach all = reach[0];
+#pragma unroll
+        for (int y = 1; y < kWaves; ++y) {
+            const Reach z = reach[y];
+            all.from_lo = z.from_lo < all.from_lo ? z.from_lo : all.from_lo;
+            all.first = z.first < all.first ? z.first : all.first;
+            all.end = z.end > all.end ? z.end : all.end;
+        }
+        const auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+        ax = axis_of<TYPE>(a, w, u(all.from_lo), u(all.first), u(all.end));
+    }
+    // (this wavefront brings half a tile of every pair)
+    const int half = 16 * (wv & 1), which = wv >> 1;
+    Load<TYPE, DP, 16> ld;
+    const float c16 = a.scale2, c8 = a.scale2 * a.k_scale, v8 = a.v_scale;
+    bool clean = false;
+again:
+    rows.start();
+    Pages pg{};
+    uint32_t there = 0;
+    auto load = [&](int i) {  // (a pair's second tile may be missing: zeros that are not used)
+        if (i < ax.committed) {
+            there = committed_there(ax, ax.ca + i, pg);
+            ld.committed(ax, ax.ca + i, pg, there, half);
+        } else {
+            there = i < ax.count ? low_bits(ax.n - (ax.da + i - ax.committed) * kTile) : 0u;
+            ld.drafted(ax, ax.da + i - ax.committed, there, half);
+        }
+    };
+    auto fetch = [&](int i) { if (i < ax.committed) pg = pages_of(ax, ax.ca + i); };
+    fetch(which);
+    load(which);
+    fetch(which + 2);
+    for (int i = 0; i < ax.count; i += 2) {
+        u32x4(&buf)[2][2][kTileP] = mem[(i >> 1) & 1];
+        ld.put(buf[which][0], buf[which][1], half, clean);
+        if (half == 0 && lane == 0u) exist[(i >> 1) & 1][which] = there;
+        if (i + 2 < ax.count) load(i + 2 + which);
+        fetch(i + 4 + which);
+        __syncthreads();
+#pragma unroll 1
+        for (int y = 0; y < 2; ++y) {
+            const int j = i + y;
+            if (j >= ax.count || !busy) break;
+            const bool past = j < ax.committed;
+            const int tile = past ? ax.ca + j : ax.da + j - ax.committed;
+            // what no row of this wavefront sees is passed over
+            if (past ? (tile + 1) * kTile <= x.from_lo : tile * kTile >= x.end || (tile + 1) * kTile <= x.first) continue;
+            const uint32_t now = __builtin_amdgcn_readfirstlane(exist[(i >> 1) & 1][y]);
+            uint32_t bits[TM];
+            const bool plain = past && now == ~0u && tile * kTile >= x.from_hi;
+            if (!plain) {
+#pragma unroll
+                for (int r = 0; r < TM; ++r) bits[r] = now & bits_of(seen[wv][16 * r + (lane & 15u)], past, tile);
+            }
+            const bool narrow = TYPE == RAC_CACHE_FP8 && past;
+            rows.tile(buf[y][0], buf[y][1], narrow ? c8 : c16, narrow ? v8 : 1.0f, plain, bits, now);
+        }
+    }
+    if (!clean && __syncthreads_or(rows.alone)) {
+        clean = true;
+        goto again;
+    }
+    const TreeArgs b = args_again();
+    Work w;
+    find_work(b, M, (int)blockIdx.x, w);
+    float* const part = w.chunks > 1 ? partial(b, w.slot, M, DP) : nullptr;
+#pragma unroll
+    for (int r = 0; r < TM; ++r) {
+        const float l = sum_row(rows.l[r]);
+        const int in = 16 * (TM * wv + r) + (int)(lane & 15u), all = w.row_tile * M + in;
+        if (all >= w.q.m * b.group) continue;
+        const int node = all / b.group, head = w.head * b.group + all % b.group;
+        const bool none = l == 0.0f;
+        uint16_t* const out = out_at(b, w, node, head);
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t) {
+            const int c = 16 * t + 4 * (int)(lane >> 4);
+            const f32x4 v = rows.o[r][t];
+            if (part)
+                *reinterpret_cast<f32x4*>(part + in * DP + c) = v;
+            else if (c < b.dim)
+                *reinterpret_cast<u32x2*>(out + c) =
+                    none ? u32x2{0u, 0u} : u32x2{pack2<TYPE>(v[0] / l, v[1] / l), pack2<TYPE>(v[2] / l, v[3] / l)};
+        }
+        if (lane < 16u) {
+            if (part) {
+                part[M * DP + in] = rows.m[r];
+                part[M * DP + M + in] = l;
+            } else if (b.lse) {
+                b.lse[(size_t)(w.q.q0 + node) * b.heads * b.group + head] = lse_of(rows.m[r], l);
+            }
+        }
+    }
+    if (clean) {
+        __syncthreads();
+        const int r0 = 16 * TM * wv;
+        for (int in = r0; in < r0 + 16 * TM && w.row_tile * M + in < w.q.m * b.group; ++in)
+            row_alone<TYPE>(b, w, ax, w.row_tile * M + in, part, in, M, DP);
+    }
+}
+
+// Joins the parts of the sequences that were split: a wavefront per (row,
+// query head), four channels a lane.
+template <int TYPE>
+__global__ __launch_bounds__(64 * kWaves) void tree_join_kernel(TreeArgs a, int M, int DP) {
+    const int lane = (int)threadIdx.x & 63, hq = a.heads * a.group;
+    const int unit = (int)blockIdx.x * kWaves + (int)threadIdx.x / 64, row = unit / hq, h = unit % hq;
+    if (row >= a.rows) return;
+    const int most = chunk_tiles(a, M);
+    int slots = 0;
+    for (int s0 = 0; s0 < a.seqs; s0 += 64) {
+        Seq q{0, 0, 0, 0, 0};
+        int chunks = 1, tiles = 0;
+        if (s0 + lane < a.seqs) {
+            q = seq_of(a, s0 + lane);
+            tiles = (q.m * a.group + M - 1) / M;
+            const int keys = key_tiles(a, q);
+            chunks = keys > most ? (keys + most - 1) / most : 1;
+        }
+        const int mine = chunks > 1 ? tiles * chunks * a.heads : 0;
+        int upto = mine;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(upto, o);
+            upto += lane >= o ? x : 0;
+        }
+        const uint64_t has = __ballot(row >= q.q0 && row < q.q0 + q.m);
+        if (has) {
+            const int at = __builtin_ctzll(has);
+            const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+            chunks = of(chunks);
+            if (chunks == 1) return;
+            tiles = of(tiles);
+            const int r = (row - of(q.q0)) * a.group + h % a.group, kvh = h / a.group;
+            const int first = slots + of(upto - mine) + ((tiles - 1 - r / M) * chunks) * a.heads + kvh, in = r % M;
+            if ((uint32_t)(first + (chunks - 1) * a.heads) >= (uint32_t)a.slots) return;
+            // the largest reference, a lane a part
+            float top = -INFINITY;
+            for (int c = lane; c < chunks; c += 64)
+                top = __builtin_fmaxf(top, partial(a, first + c * a.heads, M, DP)[M * DP + in]);
+            for (int o = 1; o < 64; o <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o));
+            float l = 0.0f;
+            f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int c = 0; c < chunks; ++c) {
+                const float* p = partial(a, first + c * a.heads, M, DP);
+                const float f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(p[M * DP + in] - top);
+                l = __builtin_fmaf(p[M * DP + M + in], f, l);
+                if (4 * lane < DP) {
+                    const f32x4 x = *reinterpret_cast<const f32x4*>(p + in * DP + 4 * lane);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf(x[i], f, v[i]);
+                }
+            }
+            const bool none = l == 0.0f;
+            if (4 * lane < a.dim)
+                *reinterpret_cast<u32x2*>(a.out + (int64_t)row * a.out_stride + (int64_t)h * a.dim + 4 * lane) =
+                    none ? u32x2{0u, 0u} : u32x2{pack2<TYPE>(v[0] / l, v[1] / l), pack2<TYPE>(v[2] / l, v[3] / l)};
+            if (lane == 0 && a.lse) a.lse[(size_t)row * hq + h] = lse_of(top, l);
+            return;
+        }
+        slots += __builtin_amdgcn_readlane(upto, 63);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -210,12 +1081,78 @@ bool tree_valid(const rac_cache_config* c, const rac_tree_config* t) {
            t->scale >= 0.0f && t->scale < __builtin_inff();
 }
 
+// Which kernel a call takes, how its work is split, and what that needs.
+struct Choice {
+    const void* kernel;
+    int m, dp;          // query rows a workgroup, channels (padded)
+    int target, slots;  // parts wanted, room for partial results
+    int64_t grid;
+    uint64_t bytes;
+};
+
+constexpr int kMinChunk = 8;  // key tiles
+
+template <int TYPE, int DP>
+void choose_form(int rows, Choice& c) {
+    c.dp = DP;
+    if (rows <= 16 && DP < 256) {
+        c.m = 16;
+        c.kernel = reinterpret_cast<const void*>(tree_few_kernel<TYPE, DP < 256 ? DP : 128, 1>);
+    } else if (rows <= 32 && DP < 256) {
+        c.m = 32;
+        c.kernel = reinterpret_cast<const void*>(tree_few_kernel<TYPE, DP < 256 ? DP : 128, 2>);
+    } else if (rows <= 64 || DP == 256) {
+        c.m = 64;
+        c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP, 1>);
+    } else if (rows <= 128 || DP == 128) {
+        c.m = 128;
+        c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP < 256 ? DP : 128, 2>);
+    } else {
+        c.m = 256;
+        c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, 64, 4>);
+    }
+}
+
+template <int TYPE>
+void choose_type(int dim, int rows, Choice& c) {
+    if (dim <= 64)
+        choose_form<TYPE, 64>(rows, c);
+    else if (dim <= 128)
+        choose_form<TYPE, 128>(rows, c);
+    else
+        choose_form<TYPE, 256>(rows, c);
+}
+
+Choice choose(const rac_cache_config* cfg, const rac_tree_config* tree) {
+    Choice c{};
+    const int group = tree->q_heads / cfg->kv_heads;
+    const int64_t of_seq = tree->max_rows < tree->rows ? tree->max_rows : tree->rows;
+    const int rows = (int)(of_seq * group);
+    if (cfg->type == RAC_CACHE_BF16)
+        choose_type<RAC_CACHE_BF16>(cfg->head_dim, rows, c);
+    else if (cfg->type == RAC_CACHE_FP16)
+        choose_type<RAC_CACHE_FP16>(cfg->head_dim, rows, c);
+    else
+        choose_type<RAC_CACHE_FP8>(cfg->head_dim, rows, c);
+    // the longest key axis there can be
+    int64_t keys = (int64_t)cfg->max_pages * cfg->page_tokens;
+    if (tree->window > 0 && tree->window < keys) keys = tree->window + kTile;
+    const int64_t most = (keys + kTile - 1) / kTile + ((int64_t)tree->max_draft + kTile - 1) / kTile;
+    c.target = most > kMinChunk ? (c.m <= 64 ? 512 : 256) : 0;
+    // (a sequence that is split has fewer than twice its keys over the part's size parts)
+    c.slots = 2 * c.target;
+    c.bytes = 256 + (uint64_t)c.slots * (uint64_t)c.m * (uint64_t)(c.dp + 2) * 4u;
+    const int64_t seqs = cfg->seqs < tree->rows ? cfg->seqs : tree->rows;
+    c.grid = c.target + (((int64_t)tree->rows * group + c.m - 1) / c.m + seqs) * cfg->kv_heads;
+    return c;
+}
+
 }  // namespace
 
 extern "C" {
 
 size_t rac_tree_attention_workspace(const rac_cache_config* cfg, const rac_tree_config* tree) {
-    return tree_valid(cfg, tree) ? 256 : 0;
+    return tree_valid(cfg, tree) ? (size_t)choose(cfg, tree).bytes : 0;
 }
 
 rac_status rac_tree_attention(const rac_cache_config* cfg, const rac_tree_config* tree, int32_t layer,
@@ -266,15 +1203,26 @@ rac_status rac_tree_attention(const rac_cache_config* cfg, const rac_tree_config
     a.max_draft = tree->max_draft;
     a.window = tree->window;
     a.mask_words = t->mask_words;
-    a.scale = tree->scale > 0.0f ? tree->scale : 1.0f / sqrtf((float)cfg->head_dim);
+    a.scale2 = (tree->scale > 0.0f ? tree->scale : 1.0f / sqrtf((float)cfg->head_dim)) * 1.4426950408889634f;
     a.k_scale = cfg->k_scale;
     a.v_scale = cfg->v_scale;
-    const void* kernel = cfg->type == RAC_CACHE_BF16   ? reinterpret_cast<const void*>(tree_row_kernel<RAC_CACHE_BF16>)
-                         : cfg->type == RAC_CACHE_FP16 ? reinterpret_cast<const void*>(tree_row_kernel<RAC_CACHE_FP16>)
-                                                       : reinterpret_cast<const void*>(tree_row_kernel<RAC_CACHE_FP8>);
+    const Choice c = choose(cfg, tree);
+    a.target = c.target;
+    a.min_chunk = kMinChunk;
+    a.parts = static_cast<float*>(workspace);
+    a.slots = c.slots;
     if ((int64_t)tree->rows * tree->q_heads >= (int64_t(1) << 26)) return RAC_ERR_UNSUPPORTED;
     void* p[] = {&a};
-    return hipLaunchKernel(kernel, dim3((unsigned)(tree->rows * tree->q_heads)), dim3(64), p, 0, stream) == hipSuccess
+    if (hipLaunchKernel(c.kernel, dim3((unsigned)c.grid), dim3(64 * kWaves), p, 0, stream) != hipSuccess)
+        return RAC_ERR_HIP;
+    if (c.target == 0) return RAC_OK;
+    int m = c.m, dp = c.dp;
+    void* j[] = {&a, &m, &dp};
+    const int64_t units = (int64_t)tree->rows * tree->q_heads;
+    const void* join = cfg->type == RAC_CACHE_FP16 ? reinterpret_cast<const void*>(tree_join_kernel<RAC_CACHE_FP16>)
+                                                   : reinterpret_cast<const void*>(tree_join_kernel<RAC_CACHE_BF16>);
+    return hipLaunchKernel(join, dim3((unsigned)((units + kWaves - 1) / kWaves)), dim3(64 * kWaves), j, 0, stream) ==
+                   hipSuccess
                ? RAC_OK
                : RAC_ERR_HIP;
 }
