@@ -100,7 +100,8 @@ typedef struct {
     const uint64_t* mask;       /* [rows][mask_words], or NULL                     */
     void* out;                  /* [rows][q_heads][head_dim], rows out_stride apart*/
     float* lse;                 /* [rows][q_heads], or NULL                        */
-    int64_t q_stride, kv_stride, out_stride; /* elements, multiples of 8           */
+    int64_t q_stride, kv_stride, out_stride; /* elements, multiples of 8; kv_stride */
+                                /* at most 2^25                                    */
     int32_t draft_rows;
     int32_t mask_words;         /* 0 without a mask                                */
 } rac_tree_tensors;

@@ -93,26 +93,6 @@ __device__ __forceinline__ int2 row_range(const int32_t* start, int s, int rows)
     return make_int2(lo, hi - lo);
 }
 
-// Sum over the threads before this one, and over all of them.
-__device__ __forceinline__ int scan_workgroup(int v, int* sums, int* total) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
-    int x = v;
-    for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(x, o);
-        x += lane >= o ? y : 0;
-    }
-    __syncthreads();
-    if (lane == 63) sums[w] = x;
-    __syncthreads();
-    int before = 0, all = 0;
-    for (int i = 0; i < kPlanWaves; ++i) {
-        before += i < w ? sums[i] : 0;
-        all += sums[i];
-    }
-    *total = all;
-    return before + x - v;
-}
-
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
     __shared__ int sums[kPlanWaves];
     const int t = (int)threadIdx.x, page = 1 << a.log_page;
@@ -150,7 +130,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
             }
         }
         int all;
-        base[i] = demand + scan_workgroup(need[i], sums, &all);
+        base[i] = demand + scan_workgroup<kPlanWaves>(need[i], sums, &all);
         demand += all;
     }
     // the free pages, lowest first, until the demand is met
@@ -159,7 +139,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
         const int p = p0 + t;
         const bool is = p < a.pages && a.refs[p] == 0;
         int all;
-        const int at = found + scan_workgroup(is, sums, &all);
+        const int at = found + scan_workgroup<kPlanWaves>(is, sums, &all);
         if (is && at < demand) a.free_list[at] = p;
         found += all;
     }

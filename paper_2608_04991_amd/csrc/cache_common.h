@@ -35,6 +35,28 @@ inline int log2_of(int v) { return __builtin_ctz((unsigned)v); }
 
 __device__ __forceinline__ int clamp_int(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
 
+// Sum over the threads of a workgroup of WAVES wavefronts before this one, and
+// over all of them (sums: LDS).
+template <int WAVES>
+__device__ __forceinline__ int scan_workgroup(int v, int* sums, int* total) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
+    int x = v;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o);
+        x += lane >= o ? y : 0;
+    }
+    __syncthreads();
+    if (lane == 63) sums[w] = x;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int i = 0; i < WAVES; ++i) {
+        before += i < w ? sums[i] : 0;
+        all += sums[i];
+    }
+    *total = all;
+    return before + x - v;
+}
+
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));

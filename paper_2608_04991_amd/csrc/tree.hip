@@ -6,6 +6,11 @@
 
 namespace {
 
+// Where the workgroups of a sequence, and its partial results, begin.
+struct SeqPlan {
+    int32_t base, slot, chunks;
+};
+
 struct TreeArgs {
     const uint8_t* pool;
     const int32_t* table;
@@ -27,6 +32,8 @@ struct TreeArgs {
     int32_t min_chunk;  // fewest key tiles of a part
     float* parts;       // [slots] partial results
     int32_t slots;
+    SeqPlan* plan;      // [seqs + 1], or null: every workgroup finds its work by itself
+    int32_t m;          // query rows a workgroup
 };
 
 // What a sequence brings to the call, whatever the device arrays hold.
@@ -171,71 +178,153 @@ __device__ __forceinline__ int key_tiles(const TreeArgs& a, const Seq& q) {
     return (q.length + kTile - 1) / kTile - committed_tile0(a, q) + (q.n + kTile - 1) / kTile;
 }
 
-__device__ __forceinline__ int64_t sum_wave(int64_t v) {
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-    return v;
+// How a sequence is cut: tiles of M query rows, and parts of its key tiles.
+struct Cut {
+    int tiles, chunks;
+};
+
+__device__ __forceinline__ Cut cut_of(const TreeArgs& a, const Seq& q, int most) {
+    const int keys = key_tiles(a, q);
+    return Cut{(q.m * a.group + a.m - 1) / a.m, keys > most ? (keys + most - 1) / most : 1};
 }
 
 // Parts of at most this many key tiles, so that all parts together are about
-// a.target and of like size whatever the lengths.
-__device__ __forceinline__ int chunk_tiles(const TreeArgs& a, int rows_per_tile) {
+// a.target and of like size whatever the lengths.  total: (tiles of rows) x
+// (tiles of keys) of all sequences, for one head.
+__device__ __forceinline__ int chunk_tiles(const TreeArgs& a, int64_t total) {
     if (a.target == 0) return 1 << 30;
-    const int lane = (int)threadIdx.x & 63;
-    int64_t total = 0;
-    for (int s0 = 0; s0 < a.seqs; s0 += 64) {
-        if (s0 + lane < a.seqs) {
-            const Seq q = seq_of(a, s0 + lane);
-            total += (int64_t)((q.m * a.group + rows_per_tile - 1) / rows_per_tile) * key_tiles(a, q);
-        }
-    }
-    total = sum_wave(total) * a.heads;
-    const int64_t c = (total + a.target - 1) >> (31 - __builtin_clz(a.target));
-    return __builtin_amdgcn_readfirstlane(c < a.min_chunk ? a.min_chunk : (int)(c < (1 << 30) ? c : (1 << 30)));
+    const int64_t c = (total * a.heads + a.target - 1) >> (31 - __builtin_clz(a.target));
+    return c < a.min_chunk ? a.min_chunk : (int)(c < (1 << 30) ? c : (1 << 30));
 }
 
-// Which work workgroup `block` has; false: none.  Every wavefront finds it by
-// itself (a lane a sequence), so that no barrier is needed.
-__device__ __forceinline__ bool find_work(const TreeArgs& a, int rows_per_tile, int block, Work& w) {
+__device__ __forceinline__ int scan_wave(int v) {  // sum over the lanes up to this one
     const int lane = (int)threadIdx.x & 63;
-    const int most = chunk_tiles(a, rows_per_tile);
-    int base = 0, slots = 0;
-    for (int s0 = 0; s0 < a.seqs; s0 += 64) {
-        Seq q{0, 0, 0, 0, 0};
-        int tiles = 0, chunks = 1;
-        if (s0 + lane < a.seqs) {
-            q = seq_of(a, s0 + lane);
-            tiles = (q.m * a.group + rows_per_tile - 1) / rows_per_tile;
-            const int keys = key_tiles(a, q);
-            chunks = keys > most ? (keys + most - 1) / most : 1;
-        }
-        const int units = tiles * chunks * a.heads;
-        int upto = units, slots_upto = chunks > 1 ? units : 0;
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(upto, o), y = __shfl_up(slots_upto, o);
-            upto += lane >= o ? x : 0;
-            slots_upto += lane >= o ? y : 0;
-        }
-        const uint64_t past = __ballot(block < base + upto);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
-            int i = block - (base + of(upto - units));
-            w.seq = s0 + at;
-            w.chunks = of(chunks);
-            const int n = of(tiles);
-            w.slot = slots + of(slots_upto - units) + i;
-            w.head = i % a.heads;
-            i /= a.heads;
-            w.chunk = i % w.chunks;
-            w.row_tile = n - 1 - i / w.chunks;  // (the last rows of a causal sequence see most)
-            w.q = Seq{of(q.q0), of(q.m), of(q.d0), of(q.n), of(q.length)};
-            // (ranges that overlap, as a broken q_start has them, may ask for more parts than there is room for)
-            return w.chunks == 1 || (uint32_t)w.slot < (uint32_t)a.slots;
-        }
-        base += __builtin_amdgcn_readlane(upto, 63);
-        slots += __builtin_amdgcn_readlane(slots_upto, 63);
+    for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_up(v, o);
+        v += lane >= o ? x : 0;
     }
-    return false;
+    return v;
+}
+
+// Up to 64 sequences need no launch ahead: a lane a sequence, each wavefront
+// finds the cuts by itself.  (A launch ahead of 8 sequences takes longer than
+// that; beyond 64 each wavefront would read all sequences again and again: 200
+// sequences in a window of 1000 took 117 us instead of the 53 with a plan.)
+struct LaneSeq {
+    Seq q;
+    Cut c;
+    int base, slot;
+};
+
+__device__ __forceinline__ LaneSeq lane_seq(const TreeArgs& a) {
+    const int lane = (int)threadIdx.x & 63;
+    LaneSeq r{Seq{0, 0, 0, 0, 0}, Cut{0, 1}, 0, 0};
+    int64_t total = 0;
+    if (lane < a.seqs) {
+        r.q = seq_of(a, lane);
+        total = (int64_t)cut_of(a, r.q, 1 << 30).tiles * key_tiles(a, r.q);
+    }
+    int most = 1 << 30;
+    if (a.target) {
+        for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
+        most = chunk_tiles(a, total);
+    }
+    if (lane < a.seqs) r.c = cut_of(a, r.q, most);
+    const int units = r.c.tiles * r.c.chunks * a.heads, split = r.c.chunks > 1 ? units : 0;
+    r.base = scan_wave(units) - units;
+    r.slot = a.target ? scan_wave(split) - split : 0;
+    return r;
+}
+
+// The last of n ascending values that is at most x; a wavefront looks at 64
+// at a time (at(0) <= x).
+template <class At>
+__device__ __forceinline__ int last_at_most(int n, int x, At at) {
+    const int lane = (int)threadIdx.x & 63;
+    int lo = 0;
+    while (n > 64) {
+        const int step = (n + 63) / 64;
+        const int k = __popcll(__ballot(lane * step < n && at(lo + lane * step) <= x)) - 1;
+        lo += k * step;
+        n = n - k * step < step ? n - k * step : step;
+    }
+    return lo + __popcll(__ballot(lane < n && at(lo + lane) <= x)) - 1;
+}
+
+// Which work workgroup `block` has; false: none.
+__device__ __forceinline__ bool find_work(const TreeArgs& a, int block, Work& w) {
+    int i, tiles;
+    if (a.plan) {
+        if (block >= a.plan[a.seqs].base) return false;
+        w.seq = __builtin_amdgcn_readfirstlane(last_at_most(a.seqs, block, [&](int s) { return a.plan[s].base; }));
+        const SeqPlan p = a.plan[w.seq];
+        w.q = seq_of(a, w.seq);
+        tiles = cut_of(a, w.q, 1 << 30).tiles;
+        w.chunks = p.chunks;
+        i = block - p.base;
+        w.slot = p.slot + i;
+    } else {
+        const LaneSeq l = lane_seq(a);
+        const uint64_t past = __ballot(block < l.base + l.c.tiles * l.c.chunks * a.heads);
+        if (!past) return false;
+        const int at = __builtin_ctzll(past);
+        const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+        w.seq = at;
+        w.q = Seq{of(l.q.q0), of(l.q.m), of(l.q.d0), of(l.q.n), of(l.q.length)};
+        tiles = of(l.c.tiles);
+        w.chunks = of(l.c.chunks);
+        i = block - of(l.base);
+        w.slot = of(l.slot) + i;
+    }
+    if (i < 0) return false;
+    w.head = i % a.heads;
+    i /= a.heads;
+    w.chunk = i % w.chunks;
+    w.row_tile = tiles - 1 - i / w.chunks;  // (the last rows of a causal sequence see most)
+    // (ranges that overlap, as a broken q_start has them, may ask for more parts than there is room for)
+    return w.row_tile >= 0 && (w.chunks == 1 || (uint32_t)w.slot < (uint32_t)a.slots);
+}
+
+// The plan of more sequences: one workgroup.
+constexpr int kPlanThreads = 1024;
+
+__global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreeArgs a) {
+    constexpr int kPer = 4;  // sequences a thread (4096 / 1024)
+    __shared__ int sums[kPlanThreads / 64];
+    __shared__ int64_t totals[kPlanThreads / 64];
+    const int t = (int)threadIdx.x;
+    Seq q[kPer];
+    int64_t total = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int s = t + i * kPlanThreads;
+        q[i] = Seq{0, 0, 0, 0, 0};
+        if (s < a.seqs) {
+            q[i] = seq_of(a, s);
+            total += (int64_t)cut_of(a, q[i], 1 << 30).tiles * key_tiles(a, q[i]);
+        }
+    }
+    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
+    if ((t & 63) == 0) totals[t / 64] = total;
+    __syncthreads();
+    total = 0;
+    for (int i = 0; i < kPlanThreads / 64; ++i) total += totals[i];
+    const int most = chunk_tiles(a, total);
+    int base = 0, slot = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int s = t + i * kPlanThreads;
+        if (i * kPlanThreads > a.seqs) break;
+        const Cut c = s < a.seqs ? cut_of(a, q[i], most) : Cut{0, 1};
+        const int units = c.tiles * c.chunks * a.heads, split = c.chunks > 1 ? units : 0;
+        int all_units, all_split;
+        const int b = base + scan_workgroup<kPlanThreads / 64>(units, sums, &all_units);
+        const int l = slot + scan_workgroup<kPlanThreads / 64>(split, sums, &all_split);
+        if (s <= a.seqs) a.plan[s] = SeqPlan{b, l, c.chunks};
+        base += all_units;
+        slot += all_split;
+    }
+    if (t == 0 && a.seqs == kPer * kPlanThreads) a.plan[a.seqs] = SeqPlan{base, slot, 1};
 }
 
 // ---------------------------------------------------------------------------
@@ -285,39 +374,49 @@ struct Rows {
         }
     }
 
-    // One tile.  kl, vl: the tile in LDS; c: factor of the scores, with log2(e)
-    // in it; vs: factor of the values.  plain: every row sees every key; else
-    // bits[r] has the keys that this lane's row of r sees, and `there` the keys
-    // whose values are loaded (the others are zeros).
-    __device__ __forceinline__ void tile(const u32x4* kl, const u32x4* vl, float c, float vs, bool plain,
-                                         const uint32_t (&bits)[TM], uint32_t there) {
+    // Scores of the tile of keys in LDS.
+    __device__ __forceinline__ void scores(const u32x4* kl, f32x4 (&s)[TM][2]) const {
         const uint32_t lane = threadIdx.x & 63u;
-        f32x4 s[TM][2];
+        constexpr int kAtOnce = TM > 1 ? 2 : DP / 32 < 4 ? DP / 32 : 4;
 #pragma unroll
         for (int r = 0; r < TM; ++r) s[r][0] = s[r][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int t = 0; t < DP / 32; ++t) {
+        for (int t0 = 0; t0 < DP / 32; t0 += kAtOnce) {
+            u32x4 k[kAtOnce][2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const u32x4 k = kl[piece_at<DP>(16u * h + (lane & 15u), 4u * t + (lane >> 4))];
+            for (int t = 0; t < kAtOnce; ++t)
 #pragma unroll
-                for (int r = 0; r < TM; ++r) s[r][h] = mma<TYPE>(k, q[r][t], s[r][h]);
-            }
+                for (int h = 0; h < 2; ++h) k[t][h] = kl[piece_at<DP>(16u * h + (lane & 15u), 4u * (t0 + t) + (lane >> 4))];
+#pragma unroll
+            for (int t = 0; t < kAtOnce; ++t)
+#pragma unroll
+                for (int r = 0; r < TM; ++r)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) s[r][h] = mma<TYPE>(k[t][h], q[r][t0 + t], s[r][h]);
         }
+    }
+
+    // The same of a tile that not every row sees all of: bits[r] has the keys
+    // that this lane's row of r sees, `there` the keys whose values are loaded
+    // (the others are zeros).  Returns whether some row must not see a loaded value.
+    __device__ __forceinline__ bool hide(f32x4 (&s)[TM][2], const uint32_t (&bits)[TM], uint32_t there) const {
+        const uint32_t first = 4u * ((threadIdx.x & 63u) >> 4);
         bool mixed = false;
-        if (!plain) {
-            const uint32_t first = 4u * (lane >> 4);
 #pragma unroll
-            for (int r = 0; r < TM; ++r) {
-                mixed |= bits[r] != there;
+        for (int r = 0; r < TM; ++r) {
+            mixed |= bits[r] != there;
+            const uint32_t b = bits[r] >> first;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        s[r][h][i] = (bits[r] >> (16u * h + first + i)) & 1u ? s[r][h][i] : -INFINITY;
-            }
-            mixed = __any(mixed);
+                for (int i = 0; i < 4; ++i) s[r][h][i] = b & (1u << (16 * h + i)) ? s[r][h][i] : -INFINITY;
         }
+        return __any(mixed);
+    }
+
+    // Scores to weights, in the type and order that the values' product takes.
+    // c: factor of the scores, with log2(e) in it; vs: factor of the values.
+    __device__ __forceinline__ void weights(const f32x4 (&s)[TM][2], float c, float vs, u32x4 (&p)[TM]) {
         float top[TM];
         bool grow = false;
 #pragma unroll
@@ -340,7 +439,6 @@ struct Rows {
                     for (int i = 0; i < 4; ++i) o[r][t][i] = o[r][t][i] * keep;
             }
         }
-        u32x4 p[TM];
 #pragma unroll
         for (int r = 0; r < TM; ++r) {
             const float ref = m[r] == -INFINITY ? 0.0f : m[r];
@@ -356,28 +454,39 @@ struct Rows {
                     p[r][i] = pack2<TYPE>(e[2 * i], e[2 * i + 1]);
             }
         }
-        if (mixed) {
-            // some row must not see some value: a weight of 0 hides it unless
-            // it is an infinity or NaN (all exponent bits set)
-            constexpr uint32_t kExp = TYPE == RAC_CACHE_FP16 ? 0x7C00u : 0x7F80u;
-            bool odd = false;
-            for (uint32_t t = 0; t < DP / 16; ++t)
+    }
+
+    // Adds the values of the tile in LDS by their weights.
+    __device__ __forceinline__ void values(const u32x4* vl, const u32x4 (&p)[TM]) {
+        const uint32_t lane = threadIdx.x & 63u;
+        constexpr int kAtOnce = TM > 1 || DP == 64 ? 4 : 8;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const u32x2 v = read_column<DP>(vl, lane, t, h);
+        for (int t0 = 0; t0 < DP / 16; t0 += kAtOnce) {
+            u32x4 v[kAtOnce];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        odd |= (v[i] & kExp) == kExp || (v[i] & (kExp << 16)) == (kExp << 16);
-                }
-            alone |= __any(odd);
+            for (int t = 0; t < kAtOnce; ++t) {
+                const u32x2 lo = read_column<DP>(vl, lane, t0 + t, 0), hi = read_column<DP>(vl, lane, t0 + t, 1);
+                v[t] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+            }
+#pragma unroll
+            for (int t = 0; t < kAtOnce; ++t)
+#pragma unroll
+                for (int r = 0; r < TM; ++r) o[r][t0 + t] = mma<TYPE>(v[t], p[r], o[r][t0 + t]);
         }
+    }
+
+    // Some row must not see some value of the tile: a weight of 0 hides it
+    // unless it is an infinity or NaN (all exponent bits set).
+    __device__ __forceinline__ void look(const u32x4* vl) {
+        constexpr uint32_t kExp = TYPE == RAC_CACHE_FP16 ? 0x7C00u : 0x7F80u;
+        bool odd = false;
+#pragma unroll 2
+        for (uint32_t i = threadIdx.x & 63u; i < kTile * DP / 8; i += 64u) {
+            const u32x4 v = vl[i];
 #pragma unroll
-        for (int t = 0; t < DP / 16; ++t) {
-            const u32x2 lo = read_column<DP>(vl, lane, t, 0), hi = read_column<DP>(vl, lane, t, 1);
-            const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
-#pragma unroll
-            for (int r = 0; r < TM; ++r) o[r][t] = mma<TYPE>(v, p[r], o[r][t]);
+            for (int y = 0; y < 4; ++y) odd |= (v[y] & kExp) == kExp || (v[y] & (kExp << 16)) == (kExp << 16);
         }
+        alone |= __any(odd);
     }
 };
 
@@ -474,105 +583,121 @@ __device__ __forceinline__ Pages pages_of(const Axis& x, int tile) {
     return r;
 }
 
-// One tile's keys and values (or the rows [ROW0, ROW0 + ROWS) of it) on their
-// way from memory to LDS, through registers: neighbouring lanes take the 16-byte
+// A tile's keys or values (or the rows [row0, row0 + ROWS) of it) on their way
+// from memory to LDS, through registers: neighbouring lanes take the 16-byte
 // pieces of a row.
 template <int TYPE, int DP, int ROWS>
 struct Load {
     static constexpr int kPieces = DP / 8, kRowsAtOnce = 64 / kPieces, kLoads = ROWS / kRowsAtOnce;       // 16 bits
     static constexpr int kPieces8 = DP / 16, kRowsAtOnce8 = 64 / kPieces8, kLoads8 = ROWS / kRowsAtOnce8;  // 8 bits
-    u32x4 k[kLoads], v[kLoads];
-    bool narrow;
+    static constexpr int kN = TYPE == RAC_CACHE_FP8 ? kLoads8 : kLoads;
+    u32x4 x[kN];
 
-    // `valid`: the keys of the tile that exist.
-    __device__ __forceinline__ void committed(const Axis& ax, int tile, const Pages& pg, uint32_t valid, int row0) {
+    // Tile i of the axis, keys or values.  Every address lies in the pool or the
+    // drafted rows whatever the tile lacks: what does not exist becomes zeros when
+    // it is put.  (One sequence of loads: with one each for committed and drafted
+    // tiles the registers of both are live, 37 more.)
+    __device__ __forceinline__ void tile(const Axis& ax, int i, const Pages& pg, int row0, bool values) {
         const uint32_t lane = threadIdx.x & 63u;
-        constexpr int kB = TYPE == RAC_CACHE_FP8 ? 1 : 2;
-        constexpr int kN = TYPE == RAC_CACHE_FP8 ? kLoads8 : kLoads, kR = TYPE == RAC_CACHE_FP8 ? kRowsAtOnce8 : kRowsAtOnce;
+        constexpr int kB = TYPE == RAC_CACHE_FP8 ? 1 : 2, kR = TYPE == RAC_CACHE_FP8 ? kRowsAtOnce8 : kRowsAtOnce;
         constexpr uint32_t kP = TYPE == RAC_CACHE_FP8 ? kPieces8 : kPieces;
-        narrow = TYPE == RAC_CACHE_FP8;
-        const uint32_t c = lane % kP, in = lane / kP;
+        const uint32_t in = lane / kP, row_bytes = (uint32_t)(ax.dim * kB);
+        const uint32_t c = (lane % kP * 16u < row_bytes ? lane % kP : 0u) * 16u;
+        const bool past = i < ax.committed;
+        const int tile = past ? ax.ca + i : ax.da + i - ax.committed;
         // (eight aligned rows lie in one page: its address is the same in all
         // lanes, but for the second eight of sixteen)
-        const uint32_t inner = (kR > 8 ? in & 7u : in) * (uint32_t)(ax.dim * kB) + c * 16u;
-        const auto at = [&](int g, int row) {
-            return ax.pool + (uint64_t)(uint32_t)pg.p[g] * ax.page_stride +
-                   ((uint32_t)(tile * kTile + row) & ((1u << ax.log_page) - 1u)) * (uint32_t)(ax.dim * kB);
-        };
-        const bool whole = valid == ~0u && ax.dim == DP;
+        const uint32_t inner = (kR > 8 ? in & 7u : in) * row_bytes;
+        const uint8_t* const pool = ax.pool + (values ? ax.side : 0u);
+        const uint8_t* eight[ROWS / 8];
 #pragma unroll
-        for (int x = 0; x < kN; ++x) {
-            const int g = x * kR / 8, row = row0 + x * kR;  // (ROWS == 16: row0 is 0 or 16)
-            const uint8_t* from = ROWS == 16 && row0 ? at((g + 2) & 3, row) : at(g & 3, row);
-            if constexpr (kR > 8) {
-                const uint8_t* other = ROWS == 16 && row0 ? at((g + 3) & 3, row + 8) : at((g + 1) & 3, row + 8);
-                from = in >= 8u ? other : from;
+        for (int g = 0; g < ROWS / 8; ++g) {
+            int p = ROWS == 16 && row0 ? pg.p[(g + 2) & 3] : pg.p[g & 3];
+            p = (uint32_t)p < (uint32_t)ax.pages ? p : 0;
+            eight[g] = pool + (uint64_t)(uint32_t)p * ax.page_stride +
+                       ((uint32_t)(tile * kTile + row0 + 8 * g) & ((1u << ax.log_page) - 1u)) * row_bytes;
+        }
+        const uint8_t* const draft = reinterpret_cast<const uint8_t*>((values ? ax.v : ax.k) + (int64_t)tile * kTile * ax.kv_stride);
+        const int last = ax.n - 1 - tile * kTile;
+#pragma unroll
+        for (int y = 0; y < kN; ++y) {
+            const uint8_t* at = eight[y * kR / 8] + (uint32_t)(y * kR % 8) * row_bytes;
+            if constexpr (kR > 8) at = in >= 8u ? eight[(y * kR / 8 + 1) % (ROWS / 8)] : at;
+            uint32_t off = inner;
+            if constexpr (TYPE != RAC_CACHE_FP8) {
+                const int row = row0 + y * kR + (int)in;
+                at = past ? at : draft;
+                off = past ? off : (uint32_t)(row < last ? row : last) * (uint32_t)(2 * ax.kv_stride);
             }
-            if (whole) {
-                k[x] = *reinterpret_cast<const u32x4*>(from + inner);
-                v[x] = *reinterpret_cast<const u32x4*>(from + inner + ax.side);
-            } else {
-                k[x] = v[x] = u32x4{0u, 0u, 0u, 0u};
-                if (c * (16 / kB) < (uint32_t)ax.dim && (valid >> (row + in)) & 1u) {
-                    k[x] = *reinterpret_cast<const u32x4*>(from + inner);
-                    v[x] = *reinterpret_cast<const u32x4*>(from + inner + ax.side);
-                }
+            x[y] = *reinterpret_cast<const u32x4*>(at + (off + c));
+        }
+    }
+    // Half a tile of drafted keys or values: with 8-bit pages the registers hold
+    // no more, and these few last tiles come when they are put.
+    __device__ __forceinline__ void drafted(const Axis& ax, const uint16_t* base, int tile, int row0) {
+        const uint32_t lane = threadIdx.x & 63u, in = lane / kPieces;
+        const uint32_t c = lane % kPieces * 8u < (uint32_t)ax.dim ? lane % kPieces : 0u;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            int row = tile * kTile + row0 + i * kRowsAtOnce + (int)in;
+            row = row < ax.n ? row : ax.n - 1;
+            x[i] = *reinterpret_cast<const u32x4*>(base + (int64_t)row * ax.kv_stride + 8u * c);
+        }
+    }
+    // valid: the keys of the tile that exist.  clean: infinities and NaNs become zeros.
+    __device__ __forceinline__ void put_drafted(u32x4* lds, const Axis& ax, const uint16_t* base, int tile, uint32_t valid, int row0,
+                                                bool clean) {
+        if constexpr (TYPE != RAC_CACHE_FP8) {
+            put_wide(lds, ax, valid, row0, clean);
+        } else {
+            constexpr int kRows = kLoads8 * kRowsAtOnce;
+#pragma unroll 1
+            for (int r = 0; r < ROWS; r += kRows) {
+                drafted(ax, base, tile, row0 + r);
+                put_wide(lds, ax, valid, row0 + r, clean);
             }
         }
     }
-
-    __device__ __forceinline__ void drafted(const Axis& ax, int tile, uint32_t valid, int row0) {
-        const uint32_t lane = threadIdx.x & 63u, c = lane % kPieces, in = lane / kPieces;
-        narrow = false;
+    __device__ __forceinline__ void put_committed(u32x4* lds, const Axis& ax, uint32_t valid, int row0, bool clean) {
+        if constexpr (TYPE != RAC_CACHE_FP8) {
+            put_wide(lds, ax, valid, row0, clean);
+        } else {
+            const uint32_t lane = threadIdx.x & 63u, c = lane % kPieces8, in = lane / kPieces8;
+            if (valid != ~0u || ax.dim != DP)
 #pragma unroll
-        for (int x = 0; x < kLoads; ++x) {
-            const uint32_t row = row0 + x * kRowsAtOnce + in;
-            k[x] = v[x] = u32x4{0u, 0u, 0u, 0u};
-            if (c * 8u < (uint32_t)ax.dim && (valid >> row) & 1u) {
-                const int64_t o = (int64_t)(tile * kTile + (int)row) * ax.kv_stride + 8u * c;
-                k[x] = *reinterpret_cast<const u32x4*>(ax.k + o);
-                v[x] = *reinterpret_cast<const u32x4*>(ax.v + o);
-            }
-        }
-    }
-
-    // clean: infinities and NaNs among the values become zeros.
-    __device__ __forceinline__ void put(u32x4* kl, u32x4* vl, int row0, bool clean) {
-        const uint32_t lane = threadIdx.x & 63u;
-        if (TYPE == RAC_CACHE_FP8 && narrow) {
-            const uint32_t c = lane % kPieces8, in = lane / kPieces8;
+                for (int i = 0; i < kLoads8; ++i)
+                    x[i] &= (c * 16u < (uint32_t)ax.dim && (valid >> (row0 + i * kRowsAtOnce8 + in)) & 1u) ? ~0u : 0u;
 #pragma unroll
-            for (int x = 0; x < kLoads8; ++x) {
-                const uint32_t row = row0 + x * kRowsAtOnce8 + in;
+            for (int i = 0; i < kLoads8; ++i)
 #pragma unroll
                 for (uint32_t y = 0; y < 2; ++y) {
-                    const uint32_t at = piece_at<DP>(row, 2u * c + y);
-                    u32x4 wide = widen8(v[x][2 * y], v[x][2 * y + 1]);
-                    if (clean) wide = finite(wide);
-                    kl[at] = widen8(k[x][2 * y], k[x][2 * y + 1]);
-                    vl[at] = wide;
+                    u32x4 w = widen8(x[i][2 * y], x[i][2 * y + 1]);
+                    if (clean) w = finite(w);
+                    lds[piece_at<DP>(row0 + i * kRowsAtOnce8 + in, 2u * c + y)] = w;
                 }
-            }
-            return;
-        }
-        const uint32_t c = lane % kPieces, in = lane / kPieces;
-#pragma unroll
-        for (int x = 0; x < kLoads; ++x) {
-            const uint32_t at = piece_at<DP>(row0 + x * kRowsAtOnce + in, c);
-            if (clean) v[x] = finite(v[x]);
-            kl[at] = k[x];
-            vl[at] = v[x];
         }
     }
+    __device__ __forceinline__ void put_wide(u32x4* lds, const Axis& ax, uint32_t valid, int row0, bool clean) {
+        const uint32_t lane = threadIdx.x & 63u, c = lane % kPieces, in = lane / kPieces;
+        if (valid != ~0u || ax.dim != DP)
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                x[i] &= (c * 8u < (uint32_t)ax.dim && (valid >> (row0 + i * kRowsAtOnce + in)) & 1u) ? ~0u : 0u;
+        if (clean)
+#pragma unroll
+            for (int i = 0; i < kN; ++i) x[i] = finite(x[i]);
+#pragma unroll
+        for (int i = 0; i < kN; ++i) lds[piece_at<DP>(row0 + i * kRowsAtOnce + in, c)] = x[i];
+    }
 
-    static __device__ __forceinline__ u32x4 finite(u32x4 x) {
+    static __device__ __forceinline__ u32x4 finite(u32x4 v) {
         constexpr uint32_t kExp = TYPE == RAC_CACHE_FP16 ? 0x7C00u : 0x7F80u;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            x[i] &= (x[i] & kExp) == kExp ? 0xFFFF0000u : ~0u;
-            x[i] &= (x[i] & (kExp << 16)) == (kExp << 16) ? 0xFFFFu : ~0u;
+            v[i] &= (v[i] & kExp) == kExp ? 0xFFFF0000u : ~0u;
+            v[i] &= (v[i] & (kExp << 16)) == (kExp << 16) ? 0xFFFFu : ~0u;
         }
-        return x;
+        return v;
     }
 
     // Eight e4m3 as bf16 (exact).
@@ -725,6 +850,12 @@ __device__ __forceinline__ void row_alone(const TreeArgs& a, const Work& w, cons
     }
 }
 
+__device__ __forceinline__ Work uniform(const Work& w) {
+    const auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    return Work{u(w.seq), u(w.head), u(w.row_tile), u(w.chunk), u(w.chunks), u(w.slot),
+                Seq{u(w.q.q0), u(w.q.m), u(w.q.d0), u(w.q.n), u(w.q.length)}};
+}
+
 // The queries of a wavefront's rows, and what they see: into registers and LDS.
 // Returns the extremes: first committed position any (every) row sees from, the
 // first drafted token, and the end of the drafted ones.
@@ -756,14 +887,16 @@ __device__ __forceinline__ Reach take_rows(const TreeArgs& a, const Work& w, int
 }
 
 // Few rows: all wavefronts hold the same 16 TM rows and take key tiles in
-// turn, each through LDS of its own, without a barrier until they join.
+// turn, each through LDS of its own (first the keys, then, in the same place,
+// the values), without a barrier until they join.
 template <int TYPE, int DP, int TM>
-__global__ __launch_bounds__(64 * kWaves, TYPE != RAC_CACHE_FP8 && TM * DP <= 128 ? 2 : 1) void tree_few_kernel(TreeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, TM == 1 && (DP == 64 || TYPE == RAC_CACHE_FP8) ? 3 : 2) void tree_few_kernel(TreeArgs a) {
     constexpr int M = 16 * TM, kTileP = kTile * DP / 8, kPad = DP + 4;
-    constexpr int kStage = 2 * kTileP * 16 * kWaves, kJoin = kWaves * 16 * kPad * 4;
+    constexpr int kStage = kTileP * 16 * kWaves, kJoin = kWaves * 16 * kPad * 4;
     __shared__ alignas(16) uint8_t mem[kStage > kJoin ? kStage : kJoin];
     __shared__ float wm[kWaves][M], wl[kWaves][M];
     __shared__ Seen seen[kWaves][M];
+    __shared__ Work work;
     const uint32_t lane = threadIdx.x & 63u;
     const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
     Rows<TYPE, DP, TM> rows;
@@ -771,55 +904,73 @@ __global__ __launch_bounds__(64 * kWaves, TYPE != RAC_CACHE_FP8 && TM * DP <= 12
     int from_hi;
     {
         Work w;
-        if (!find_work(a, M, (int)blockIdx.x, w)) return;
+        if (!find_work(a, (int)blockIdx.x, w)) return;
+        if (threadIdx.x == 0u) work = w;
         const Reach x = take_rows(a, w, w.row_tile * M, rows, seen[wv]);
         from_hi = x.from_hi;
         ax = axis_of<TYPE>(a, w, x.from_lo, x.first, x.end);
     }
-    u32x4* const kl = reinterpret_cast<u32x4*>(mem) + wv * 2 * kTileP;
-    u32x4* const vl = kl + kTileP;
-    Load<TYPE, DP, kTile> ld;
+    u32x4* const tile_lds = reinterpret_cast<u32x4*>(mem) + wv * kTileP;
+    Load<TYPE, DP, kTile> lk, lv;
     const float c16 = a.scale2, c8 = a.scale2 * a.k_scale, v8 = a.v_scale;
-    bool clean = false;
-again:
-    rows.start();
-    uint32_t there = 0;
-    Pages pg{};
-    auto load = [&](int i) {
-        if (i < ax.committed) {
-            there = committed_there(ax, ax.ca + i, pg);
-            ld.committed(ax, ax.ca + i, pg, there, 0);
-        } else {
-            there = low_bits(ax.n - (ax.da + i - ax.committed) * kTile);
-            ld.drafted(ax, ax.da + i - ax.committed, there, 0);
+    auto pass = [&](bool clean) {
+        rows.start();
+        uint32_t there = 0;
+        Pages pg{};
+        // the keys of tile i that exist
+        auto exist = [&](int i) {
+            return i < ax.committed ? committed_there(ax, ax.ca + i, pg) : low_bits(ax.n - (ax.da + i - ax.committed) * kTile);
+        };
+        auto fetch = [&](int i) { if (i < ax.committed) pg = pages_of(ax, ax.ca + i); };
+        fetch(wv);
+        if (wv < ax.count) {
+            there = exist(wv);
+            if (TYPE != RAC_CACHE_FP8 || wv < ax.committed) {
+                lk.tile(ax, wv, pg, 0, false);
+                lv.tile(ax, wv, pg, 0, true);
+            }
+        }
+        fetch(wv + kWaves);
+        for (int i = wv; i < ax.count; i += kWaves) {
+            const bool past = i < ax.committed, narrow = TYPE == RAC_CACHE_FP8 && past;
+            const int tile = past ? ax.ca + i : ax.da + i - ax.committed;
+            const uint32_t now = there;
+            if (past)
+                lk.put_committed(tile_lds, ax, now, 0, false);
+            else
+                lk.put_drafted(tile_lds, ax, ax.k, tile, now, 0, false);
+            if (i + kWaves < ax.count) {
+                there = exist(i + kWaves);
+                if (TYPE != RAC_CACHE_FP8 || i + kWaves < ax.committed) lk.tile(ax, i + kWaves, pg, 0, false);
+            }
+            wave_sync();
+            f32x4 s[TM][2];
+            rows.scores(tile_lds, s);
+            wave_sync();
+            if (past)
+                lv.put_committed(tile_lds, ax, now, 0, clean);
+            else
+                lv.put_drafted(tile_lds, ax, ax.v, tile, now, 0, clean);
+            if (i + kWaves < (TYPE == RAC_CACHE_FP8 ? ax.committed : ax.count)) lv.tile(ax, i + kWaves, pg, 0, true);
+            fetch(i + 2 * kWaves);
+            bool mixed = false;
+            if (!(past && now == ~0u && tile * kTile >= from_hi)) {
+                uint32_t bits[TM];
+#pragma unroll
+                for (int r = 0; r < TM; ++r) bits[r] = now & bits_of(seen[wv][16 * r + (lane & 15u)], past, tile);
+                mixed = rows.hide(s, bits, now);
+            }
+            u32x4 p[TM];
+            rows.weights(s, narrow ? c8 : c16, narrow ? v8 : 1.0f, p);
+            wave_sync();
+            if (mixed) rows.look(tile_lds);
+            rows.values(tile_lds, p);
+            wave_sync();
         }
     };
-    auto fetch = [&](int i) { if (i < ax.committed) pg = pages_of(ax, ax.ca + i); };
-    fetch(wv);
-    if (wv < ax.count) load(wv);
-    fetch(wv + kWaves);
-    for (int i = wv; i < ax.count; i += kWaves) {
-        ld.put(kl, vl, 0, clean);
-        const uint32_t now = there;
-        if (i + kWaves < ax.count) load(i + kWaves);
-        fetch(i + 2 * kWaves);
-        wave_sync();
-        uint32_t bits[TM];
-        const bool past = i < ax.committed;
-        const int tile = past ? ax.ca + i : ax.da + i - ax.committed;
-        const bool plain = past && now == ~0u && tile * kTile >= from_hi;
-        if (!plain) {
-#pragma unroll
-            for (int r = 0; r < TM; ++r) bits[r] = now & bits_of(seen[wv][16 * r + (lane & 15u)], past, tile);
-        }
-        const bool narrow = TYPE == RAC_CACHE_FP8 && past;
-        rows.tile(kl, vl, narrow ? c8 : c16, narrow ? v8 : 1.0f, plain, bits, now);
-        wave_sync();
-    }
-    if (!clean && __syncthreads_or(rows.alone)) {
-        clean = true;
-        goto again;
-    }
+    pass(false);
+    const bool clean = __syncthreads_or(rows.alone);
+    if (clean) pass(true);
     // join the wavefronts
 #pragma unroll
     for (int r = 0; r < TM; ++r) {
@@ -831,8 +982,7 @@ again:
     }
     __syncthreads();
     const TreeArgs b = args_again();
-    Work w;
-    find_work(b, M, (int)blockIdx.x, w);
+    const Work w = uniform(work);
     float* const sums = reinterpret_cast<float*>(mem);
     float* const part = w.chunks > 1 ? partial(b, w.slot, M, DP) : nullptr;
 #pragma unroll
@@ -894,6 +1044,7 @@ __global__ __launch_bounds__(64 * kWaves, TM * DP <= 256 && DP < 256 ? 2 : 1) vo
     __shared__ uint32_t exist[2][2];         // the keys of a tile that exist
     __shared__ Seen seen[kWaves][16 * TM];
     __shared__ Reach reach[kWaves];
+    __shared__ Work work;
     const uint32_t lane = threadIdx.x & 63u;
     const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
     Rows<TYPE, DP, TM> rows;
@@ -902,7 +1053,8 @@ __global__ __launch_bounds__(64 * kWaves, TM * DP <= 256 && DP < 256 ? 2 : 1) vo
     bool busy;  // whether this wavefront has rows
     {
         Work w;
-        if (!find_work(a, M, (int)blockIdx.x, w)) return;
+        if (!find_work(a, (int)blockIdx.x, w)) return;
+        if (threadIdx.x == 0u) work = w;
         const int row0 = w.row_tile * M + 16 * TM * wv;
         busy = row0 < w.q.m * a.group;
         x = take_rows(a, w, row0, rows, seen[wv]);
@@ -921,21 +1073,19 @@ __global__ __launch_bounds__(64 * kWaves, TM * DP <= 256 && DP < 256 ? 2 : 1) vo
     }
     // (this wavefront brings half a tile of every pair)
     const int half = 16 * (wv & 1), which = wv >> 1;
-    Load<TYPE, DP, 16> ld;
+    Load<TYPE, DP, 16> lk, lv;
     const float c16 = a.scale2, c8 = a.scale2 * a.k_scale, v8 = a.v_scale;
     bool clean = false;
 again:
     rows.start();
     Pages pg{};
     uint32_t there = 0;
-    auto load = [&](int i) {  // (a pair's second tile may be missing: zeros that are not used)
-        if (i < ax.committed) {
-            there = committed_there(ax, ax.ca + i, pg);
-            ld.committed(ax, ax.ca + i, pg, there, half);
-        } else {
-            there = i < ax.count ? low_bits(ax.n - (ax.da + i - ax.committed) * kTile) : 0u;
-            ld.drafted(ax, ax.da + i - ax.committed, there, half);
-        }
+    auto load = [&](int i) {  // (a pair's second tile may be missing: what is put there is not used)
+        if (i >= ax.count) return;
+        there = i < ax.committed ? committed_there(ax, ax.ca + i, pg) : low_bits(ax.n - (ax.da + i - ax.committed) * kTile);
+        if (TYPE == RAC_CACHE_FP8 && i >= ax.committed) return;
+        lk.tile(ax, i, pg, half, false);
+        lv.tile(ax, i, pg, half, true);
     };
     auto fetch = [&](int i) { if (i < ax.committed) pg = pages_of(ax, ax.ca + i); };
     fetch(which);
@@ -943,7 +1093,14 @@ again:
     fetch(which + 2);
     for (int i = 0; i < ax.count; i += 2) {
         u32x4(&buf)[2][2][kTileP] = mem[(i >> 1) & 1];
-        ld.put(buf[which][0], buf[which][1], half, clean);
+        if (i + which < ax.committed) {
+            lk.put_committed(buf[which][0], ax, there, half, false);
+            lv.put_committed(buf[which][1], ax, there, half, clean);
+        } else if (i + which < ax.count) {
+            const int tile = ax.da + i + which - ax.committed;
+            lk.put_drafted(buf[which][0], ax, ax.k, tile, there, half, false);
+            lv.put_drafted(buf[which][1], ax, ax.v, tile, there, half, clean);
+        }
         if (half == 0 && lane == 0u) exist[(i >> 1) & 1][which] = there;
         if (i + 2 < ax.count) load(i + 2 + which);
         fetch(i + 4 + which);
@@ -957,14 +1114,18 @@ again:
             // what no row of this wavefront sees is passed over
             if (past ? (tile + 1) * kTile <= x.from_lo : tile * kTile >= x.end || (tile + 1) * kTile <= x.first) continue;
             const uint32_t now = __builtin_amdgcn_readfirstlane(exist[(i >> 1) & 1][y]);
-            uint32_t bits[TM];
-            const bool plain = past && now == ~0u && tile * kTile >= x.from_hi;
-            if (!plain) {
+            f32x4 s[TM][2];
+            rows.scores(buf[y][0], s);
+            if (!(past && now == ~0u && tile * kTile >= x.from_hi)) {
+                uint32_t bits[TM];
 #pragma unroll
                 for (int r = 0; r < TM; ++r) bits[r] = now & bits_of(seen[wv][16 * r + (lane & 15u)], past, tile);
+                if (rows.hide(s, bits, now)) rows.look(buf[y][1]);
             }
             const bool narrow = TYPE == RAC_CACHE_FP8 && past;
-            rows.tile(buf[y][0], buf[y][1], narrow ? c8 : c16, narrow ? v8 : 1.0f, plain, bits, now);
+            u32x4 p[TM];
+            rows.weights(s, narrow ? c8 : c16, narrow ? v8 : 1.0f, p);
+            rows.values(buf[y][1], p);
         }
     }
     if (!clean && __syncthreads_or(rows.alone)) {
@@ -972,8 +1133,7 @@ again:
         goto again;
     }
     const TreeArgs b = args_again();
-    Work w;
-    find_work(b, M, (int)blockIdx.x, w);
+    const Work w = uniform(work);
     float* const part = w.chunks > 1 ? partial(b, w.slot, M, DP) : nullptr;
 #pragma unroll
     for (int r = 0; r < TM; ++r) {
@@ -1010,66 +1170,104 @@ again:
     }
 }
 
-// Joins the parts of the sequences that were split: a wavefront per (row,
-// query head), four channels a lane.
-template <int TYPE>
-__global__ __launch_bounds__(64 * kWaves) void tree_join_kernel(TreeArgs a, int M, int DP) {
-    const int lane = (int)threadIdx.x & 63, hq = a.heads * a.group;
-    const int unit = (int)blockIdx.x * kWaves + (int)threadIdx.x / 64, row = unit / hq, h = unit % hq;
+// Joins the parts of the sequences that were split.  DP / 4 lanes take a (row,
+// query head) pair, four channels each; with SPLIT (few pairs, so many parts)
+// a workgroup's wavefronts share the parts of the same pairs.
+template <int TYPE, int DP, bool SPLIT>
+__global__ __launch_bounds__(64 * kWaves) void tree_join_kernel(TreeArgs a) {
+    constexpr int kLanes = DP / 4, kPairs = 64 / kLanes, kAtOnce = 8;
+    __shared__ f32x4 sums[SPLIT ? kWaves : 1][64];
+    __shared__ float wm[SPLIT ? kWaves : 1][kPairs], wl[SPLIT ? kWaves : 1][kPairs];
+    const int lane = (int)threadIdx.x & 63, wv = (int)threadIdx.x / 64, hq = a.heads * a.group;
+    const int groups = (hq + kPairs - 1) / kPairs;  // of the heads of a row
+    const int unit = SPLIT ? (int)blockIdx.x : (int)blockIdx.x * kWaves + wv;
+    const int row = __builtin_amdgcn_readfirstlane(unit / groups);
     if (row >= a.rows) return;
-    const int most = chunk_tiles(a, M);
-    int slots = 0;
-    for (int s0 = 0; s0 < a.seqs; s0 += 64) {
-        Seq q{0, 0, 0, 0, 0};
-        int chunks = 1, tiles = 0;
-        if (s0 + lane < a.seqs) {
-            q = seq_of(a, s0 + lane);
-            tiles = (q.m * a.group + M - 1) / M;
-            const int keys = key_tiles(a, q);
-            chunks = keys > most ? (keys + most - 1) / most : 1;
-        }
-        const int mine = chunks > 1 ? tiles * chunks * a.heads : 0;
-        int upto = mine;
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(upto, o);
-            upto += lane >= o ? x : 0;
-        }
-        const uint64_t has = __ballot(row >= q.q0 && row < q.q0 + q.m);
-        if (has) {
-            const int at = __builtin_ctzll(has);
-            const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
-            chunks = of(chunks);
-            if (chunks == 1) return;
-            tiles = of(tiles);
-            const int r = (row - of(q.q0)) * a.group + h % a.group, kvh = h / a.group;
-            const int first = slots + of(upto - mine) + ((tiles - 1 - r / M) * chunks) * a.heads + kvh, in = r % M;
-            if ((uint32_t)(first + (chunks - 1) * a.heads) >= (uint32_t)a.slots) return;
-            // the largest reference, a lane a part
-            float top = -INFINITY;
-            for (int c = lane; c < chunks; c += 64)
-                top = __builtin_fmaxf(top, partial(a, first + c * a.heads, M, DP)[M * DP + in]);
-            for (int o = 1; o < 64; o <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o));
-            float l = 0.0f;
-            f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-            for (int c = 0; c < chunks; ++c) {
-                const float* p = partial(a, first + c * a.heads, M, DP);
-                const float f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(p[M * DP + in] - top);
-                l = __builtin_fmaf(p[M * DP + M + in], f, l);
-                if (4 * lane < DP) {
-                    const f32x4 x = *reinterpret_cast<const f32x4*>(p + in * DP + 4 * lane);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf(x[i], f, v[i]);
-                }
-            }
-            const bool none = l == 0.0f;
-            if (4 * lane < a.dim)
-                *reinterpret_cast<u32x2*>(a.out + (int64_t)row * a.out_stride + (int64_t)h * a.dim + 4 * lane) =
-                    none ? u32x2{0u, 0u} : u32x2{pack2<TYPE>(v[0] / l, v[1] / l), pack2<TYPE>(v[2] / l, v[3] / l)};
-            if (lane == 0 && a.lse) a.lse[(size_t)row * hq + h] = lse_of(top, l);
-            return;
-        }
-        slots += __builtin_amdgcn_readlane(upto, 63);
+    Seq q;
+    int chunks, slot;
+    if (a.plan) {
+        const int s = __builtin_amdgcn_readfirstlane(last_at_most(a.seqs, row, [&](int i) { return i ? a.q_start[i] : -1; }));
+        chunks = a.plan[s].chunks;
+        if (chunks == 1) return;
+        q = seq_of(a, s);
+        slot = a.plan[s].slot;
+    } else {
+        const LaneSeq l = lane_seq(a);
+        const uint64_t has = __ballot(row >= l.q.q0 && row < l.q.q0 + l.q.m);
+        if (!has) return;
+        const int at = __builtin_ctzll(has);
+        const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+        chunks = of(l.c.chunks);
+        if (chunks == 1) return;
+        q = Seq{of(l.q.q0), of(l.q.m), of(l.q.d0), of(l.q.n), of(l.q.length)};
+        slot = of(l.slot);
     }
+    const int tiles = cut_of(a, q, 1 << 30).tiles;
+    if (row < q.q0 || row >= q.q0 + q.m || (uint32_t)(slot + tiles * chunks * a.heads) > (uint32_t)a.slots) return;
+    const int pair = lane / kLanes, h = unit % groups * kPairs + pair, c4 = lane % kLanes;
+    const int hc = h < hq ? h : hq - 1, r = (row - q.q0) * a.group + hc % a.group;
+    const int in = r % a.m;
+    // parts of a row tile are a.heads slots apart
+    const size_t stride = (size_t)a.m * (DP + 2);
+    const float* const base = a.parts + ((size_t)slot + (size_t)((tiles - 1 - r / a.m) * chunks) * a.heads + hc / a.group) * stride;
+    const size_t step = stride * a.heads;
+    float top = -INFINITY, l = 0.0f;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int first = SPLIT ? wv : 0, by = SPLIT ? kWaves : 1;
+    for (int c = first; c < chunks; c += by * kAtOnce) {
+        f32x4 x[kAtOnce];
+        float m[kAtOnce], s[kAtOnce], now = top;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const bool is = c + i * by < chunks;
+            const float* p = base + (size_t)(is ? c + i * by : c) * step;
+            x[i] = *reinterpret_cast<const f32x4*>(p + (size_t)in * DP + 4 * c4);
+            m[i] = is ? p[a.m * DP + in] : -INFINITY;
+            s[i] = p[a.m * DP + a.m + in];
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) now = __builtin_fmaxf(now, m[i]);
+        const float ref = now == -INFINITY ? 0.0f : now, keep = __builtin_amdgcn_exp2f(top - ref);
+        l = l * keep;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = v[i] * keep;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (c + i * by >= chunks) break;
+            const float f = __builtin_amdgcn_exp2f(m[i] - ref);
+            l = __builtin_fmaf(s[i], f, l);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) v[y] = __builtin_fmaf(x[i][y], f, v[y]);
+        }
+        top = now;
+    }
+    if constexpr (SPLIT) {
+        sums[wv][lane] = v;
+        if (c4 == 0) {
+            wm[wv][pair] = top;
+            wl[wv][pair] = l;
+        }
+        __syncthreads();
+        if (wv != 0) return;
+        top = wm[0][pair];
+#pragma unroll
+        for (int x = 1; x < kWaves; ++x) top = __builtin_fmaxf(top, wm[x][pair]);
+        v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        l = 0.0f;
+#pragma unroll
+        for (int x = 0; x < kWaves; ++x) {
+            const float f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(wm[x][pair] - top);
+            l = __builtin_fmaf(wl[x][pair], f, l);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) v[y] = __builtin_fmaf(sums[x][lane][y], f, v[y]);
+        }
+    }
+    if (h >= hq) return;
+    const bool none = l == 0.0f;
+    if (4 * c4 < a.dim)
+        *reinterpret_cast<u32x2*>(a.out + (int64_t)row * a.out_stride + (int64_t)h * a.dim + 4 * c4) =
+            none ? u32x2{0u, 0u} : u32x2{pack2<TYPE>(v[0] / l, v[1] / l), pack2<TYPE>(v[2] / l, v[3] / l)};
+    if (c4 == 0 && a.lse) a.lse[(size_t)row * hq + h] = lse_of(top, l);
 }
 
 // ---------------------------------------------------------------------------
@@ -1087,7 +1285,7 @@ struct Choice {
     int m, dp;          // query rows a workgroup, channels (padded)
     int target, slots;  // parts wanted, room for partial results
     int64_t grid;
-    uint64_t bytes;
+    uint64_t bytes, plan;  // of the scratch; where the plan lies in it
 };
 
 constexpr int kMinChunk = 8;  // key tiles
@@ -1095,12 +1293,14 @@ constexpr int kMinChunk = 8;  // key tiles
 template <int TYPE, int DP>
 void choose_form(int rows, Choice& c) {
     c.dp = DP;
+    // (TM = 2 with 16-bit pages of 128 channels would need more than 256 registers)
+    constexpr bool kTwo = DP == 64 || (DP == 128 && TYPE == RAC_CACHE_FP8);
     if (rows <= 16 && DP < 256) {
         c.m = 16;
         c.kernel = reinterpret_cast<const void*>(tree_few_kernel<TYPE, DP < 256 ? DP : 128, 1>);
-    } else if (rows <= 32 && DP < 256) {
+    } else if (rows <= 32 && kTwo) {
         c.m = 32;
-        c.kernel = reinterpret_cast<const void*>(tree_few_kernel<TYPE, DP < 256 ? DP : 128, 2>);
+        c.kernel = reinterpret_cast<const void*>(tree_few_kernel<TYPE, kTwo ? DP : 64, 2>);
     } else if (rows <= 64 || DP == 256) {
         c.m = 64;
         c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP, 1>);
@@ -1111,6 +1311,20 @@ void choose_form(int rows, Choice& c) {
         c.m = 256;
         c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, 64, 4>);
     }
+}
+
+constexpr int kSplitJoin = 1024;
+
+template <int TYPE>
+const void* join_of(int dp, bool split) {
+    if (dp == 64)
+        return split ? reinterpret_cast<const void*>(tree_join_kernel<TYPE, 64, true>)
+                     : reinterpret_cast<const void*>(tree_join_kernel<TYPE, 64, false>);
+    if (dp == 128)
+        return split ? reinterpret_cast<const void*>(tree_join_kernel<TYPE, 128, true>)
+                     : reinterpret_cast<const void*>(tree_join_kernel<TYPE, 128, false>);
+    return split ? reinterpret_cast<const void*>(tree_join_kernel<TYPE, 256, true>)
+                 : reinterpret_cast<const void*>(tree_join_kernel<TYPE, 256, false>);
 }
 
 template <int TYPE>
@@ -1138,12 +1352,14 @@ Choice choose(const rac_cache_config* cfg, const rac_tree_config* tree) {
     int64_t keys = (int64_t)cfg->max_pages * cfg->page_tokens;
     if (tree->window > 0 && tree->window < keys) keys = tree->window + kTile;
     const int64_t most = (keys + kTile - 1) / kTile + ((int64_t)tree->max_draft + kTile - 1) / kTile;
-    c.target = most > kMinChunk ? (c.m <= 64 ? 512 : 256) : 0;
+    const int64_t row_tiles = ((int64_t)tree->rows * group + c.m - 1) / c.m;
+    c.target = most > kMinChunk && row_tiles * cfg->kv_heads < 512 ? 512 : 0;
     // (a sequence that is split has fewer than twice its keys over the part's size parts)
     c.slots = 2 * c.target;
-    c.bytes = 256 + (uint64_t)c.slots * (uint64_t)c.m * (uint64_t)(c.dp + 2) * 4u;
+    c.plan = ((uint64_t)c.slots * (uint64_t)c.m * (uint64_t)(c.dp + 2) * 4u + 255u) & ~uint64_t(255);
+    c.bytes = c.plan + (uint64_t)(cfg->seqs + 1) * sizeof(SeqPlan);
     const int64_t seqs = cfg->seqs < tree->rows ? cfg->seqs : tree->rows;
-    c.grid = c.target + (((int64_t)tree->rows * group + c.m - 1) / c.m + seqs) * cfg->kv_heads;
+    c.grid = c.target + (row_tiles + seqs) * cfg->kv_heads;
     return c;
 }
 
@@ -1165,7 +1381,7 @@ rac_status rac_tree_attention(const rac_cache_config* cfg, const rac_tree_config
     if (!pool || !table || !lengths || !t->q || !t->q_start || !t->out || !workspace) return RAC_ERR_INVALID;
     if (t->q_stride < q_row || t->out_stride < q_row || t->q_stride % 8 || t->out_stride % 8) return RAC_ERR_INVALID;
     if ((t->k != nullptr) != (t->v != nullptr) || t->draft_rows < 0 || t->mask_words < 0) return RAC_ERR_INVALID;
-    if (t->k && (t->kv_stride < kv_row || t->kv_stride % 8)) return RAC_ERR_INVALID;
+    if (t->k && (t->kv_stride < kv_row || t->kv_stride % 8 || t->kv_stride > (1 << 25))) return RAC_ERR_INVALID;
     if ((t->mask != nullptr) != (t->mask_words > 0)) return RAC_ERR_INVALID;
     if (!aligned(pool, 16) || !aligned(t->q, 16) || !aligned(t->k, 16) || !aligned(t->v, 16) || !aligned(t->out, 16) ||
         !aligned(table, 4) || !aligned(lengths, 4) || !aligned(t->q_start, 4) || !aligned(t->draft_start, 4) ||
@@ -1212,19 +1428,23 @@ rac_status rac_tree_attention(const rac_cache_config* cfg, const rac_tree_config
     a.parts = static_cast<float*>(workspace);
     a.slots = c.slots;
     if ((int64_t)tree->rows * tree->q_heads >= (int64_t(1) << 26)) return RAC_ERR_UNSUPPORTED;
+    a.plan = cfg->seqs > 64 ? reinterpret_cast<SeqPlan*>(static_cast<uint8_t*>(workspace) + c.plan) : nullptr;
+    a.m = c.m;
     void* p[] = {&a};
-    if (hipLaunchKernel(c.kernel, dim3((unsigned)c.grid), dim3(64 * kWaves), p, 0, stream) != hipSuccess)
-        return RAC_ERR_HIP;
-    if (c.target == 0) return RAC_OK;
-    int m = c.m, dp = c.dp;
-    void* j[] = {&a, &m, &dp};
-    const int64_t units = (int64_t)tree->rows * tree->q_heads;
-    const void* join = cfg->type == RAC_CACHE_FP16 ? reinterpret_cast<const void*>(tree_join_kernel<RAC_CACHE_FP16>)
-                                                   : reinterpret_cast<const void*>(tree_join_kernel<RAC_CACHE_BF16>);
-    return hipLaunchKernel(join, dim3((unsigned)((units + kWaves - 1) / kWaves)), dim3(64 * kWaves), j, 0, stream) ==
-                   hipSuccess
-               ? RAC_OK
-               : RAC_ERR_HIP;
+    const auto launch = [&](const void* kernel, int64_t grid, int threads) {
+        return hipLaunchKernel(kernel, dim3((unsigned)grid), dim3((unsigned)threads), p, 0, stream) == hipSuccess
+                   ? RAC_OK
+                   : RAC_ERR_HIP;
+    };
+    rac_status st = RAC_OK;
+    if (a.plan) st = launch(reinterpret_cast<const void*>(tree_plan_kernel), 1, kPlanThreads);
+    if (st == RAC_OK) st = launch(c.kernel, c.grid, 64 * kWaves);
+    if (st != RAC_OK || c.target == 0) return st;
+    const int pairs = 256 / c.dp;  // (row, head) pairs a wavefront
+    const int64_t units = (int64_t)tree->rows * ((tree->q_heads + pairs - 1) / pairs);
+    const bool split = units < kSplitJoin;
+    const void* join = cfg->type == RAC_CACHE_FP16 ? join_of<RAC_CACHE_FP16>(c.dp, split) : join_of<RAC_CACHE_BF16>(c.dp, split);
+    return launch(join, split ? units : (units + kWaves - 1) / kWaves, 64 * kWaves);
 }
 
 }  // extern "C"
