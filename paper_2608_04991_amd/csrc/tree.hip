@@ -139,6 +139,14 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
 }
 
+// The largest of three; a NaN among them is passed over.  (__builtin_fmaxf adds
+// an instruction to each operand that might be a signalling NaN.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 // The four lanes l, l ^ 16, l ^ 32, l ^ 48 of a query row.
 __device__ __forceinline__ float max_row(float v) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -414,16 +422,22 @@ struct Rows {
         return __any(mixed);
     }
 
-    // Scores to weights, in the type and order that the values' product takes.
-    // c: factor of the scores, with log2(e) in it; vs: factor of the values.
-    __device__ __forceinline__ void weights(const f32x4 (&s)[TM][2], float c, float vs, u32x4 (&p)[TM]) {
+    // Scores of NT tiles to weights, in the type and order that the values'
+    // product takes.  c: factors of the scores, with log2(e) in them; vs: factors
+    // of the values (8-bit pages).
+    template <int NT>
+    __device__ __forceinline__ void weights(const f32x4 (&s)[NT][TM][2], const float (&c)[NT], const float (&vs)[NT],
+                                            u32x4 (&p)[NT][TM]) {
         float top[TM];
         bool grow = false;
 #pragma unroll
         for (int r = 0; r < TM; ++r) {
-            const float x = __builtin_fmaxf(__builtin_fmaxf(s[r][0][0], s[r][0][1]), __builtin_fmaxf(s[r][0][2], s[r][0][3]));
-            const float y = __builtin_fmaxf(__builtin_fmaxf(s[r][1][0], s[r][1][1]), __builtin_fmaxf(s[r][1][2], s[r][1][3]));
-            top[r] = __builtin_fmaxf(x, y) * c;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const f32x4 u = s[n][r][0], v = s[n][r][1];
+                const float x = max3(max3(max3(u[0], u[1], u[2]), u[3], v[0]), v[1], v[2]);
+                top[r] = n ? max3(top[r], x * c[n], v[3] * c[n]) : max3(x, v[3], v[3]) * c[n];
+            }
             grow |= top[r] > m[r] + 8.0f;
         }
         if (__any(grow)) {  // (seldom: the reference need not be the maximum, only near it)
@@ -440,20 +454,22 @@ struct Rows {
             }
         }
 #pragma unroll
-        for (int r = 0; r < TM; ++r) {
-            const float ref = m[r] == -INFINITY ? 0.0f : m[r];
-            float e[8];
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][i / 4][i % 4], c, -ref));
-            l[r] = l[r] + (((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+            for (int r = 0; r < TM; ++r) {
+                const float ref = m[r] == -INFINITY ? 0.0f : m[r];
+                float e[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (TYPE == RAC_CACHE_FP8)
-                    p[r][i] = pack2<TYPE>(e[2 * i] * vs, e[2 * i + 1] * vs);
-                else
-                    p[r][i] = pack2<TYPE>(e[2 * i], e[2 * i + 1]);
+                for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r][i / 4][i % 4], c[n], -ref));
+                l[r] = l[r] + (((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (TYPE == RAC_CACHE_FP8)
+                        p[n][r][i] = pack2<TYPE>(e[2 * i] * vs[n], e[2 * i + 1] * vs[n]);
+                    else
+                        p[n][r][i] = pack2<TYPE>(e[2 * i], e[2 * i + 1]);
+                }
             }
-        }
     }
 
     // Adds the values of the tile in LDS by their weights.
@@ -522,12 +538,14 @@ __device__ __forceinline__ TreeArgs args_again() {
 // The key axis of a workgroup, as its loop needs it.
 struct Axis {
     const uint8_t* pool;   // keys of this layer and head in page 0
-    uint64_t page_stride;  // bytes
+    uint32_t page_stride;  // in 16 bytes (a page is less than 64 GiB)
     uint32_t side;         // bytes from a page's keys to its values
     const int32_t* row;    // the sequence's table entries
     const uint16_t* k;     // drafted keys and values of this sequence and head
     const uint16_t* v;
     int64_t kv_stride;
+    const uint64_t* mask;
+    int mask_words;
     int max_pages, log_page, pages, dim, length, n;
     // the tiles that the rows see at all: committed ones [ca, ca + committed), then drafted ones from da on
     int ca, committed, da, count;
@@ -539,13 +557,15 @@ __device__ __forceinline__ Axis axis_of(const TreeArgs& a, const Work& w, int fr
     const uint64_t plane = ((uint64_t)a.dim << a.log_page) * kB;
     Axis x;
     x.pool = a.pool + ((uint64_t)a.layer * 2 * a.heads + w.head) * plane;
-    x.page_stride = plane * a.heads * 2 * a.layers;
+    x.page_stride = (uint32_t)(plane / 16 * a.heads * 2 * a.layers);
     x.side = (uint32_t)(plane * a.heads);
     x.row = a.table + (size_t)w.seq * a.max_pages;
     const int64_t o = w.q.d0 * a.kv_stride + (int64_t)w.head * a.dim;
     x.k = a.k + o;
     x.v = a.v + o;
     x.kv_stride = a.kv_stride;
+    x.mask = a.mask;
+    x.mask_words = a.mask_words;
     x.max_pages = a.max_pages;
     x.log_page = a.log_page;
     x.pages = a.pages;
@@ -567,17 +587,19 @@ __device__ __forceinline__ Axis axis_of(const TreeArgs& a, const Work& w, int fr
     return x;
 }
 
-// The table entries of eight keys each.
+// The table entries of ROWS keys from key row0 of a tile on, eight keys each.
+template <int ROWS>
 struct Pages {
-    int p[4];
+    int p[ROWS / 8];
 };
 
-__device__ __forceinline__ Pages pages_of(const Axis& x, int tile) {
+template <int ROWS>
+__device__ __forceinline__ Pages<ROWS> pages_of(const Axis& x, int tile, int row0) {
     using cptr = const __attribute__((address_space(4))) int32_t*;  // read-only in this launch: scalar loads
-    Pages r;
+    Pages<ROWS> r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int at = (tile * kTile + 8 * i) >> x.log_page;
+    for (int i = 0; i < ROWS / 8; ++i) {
+        const int at = (tile * kTile + row0 + 8 * i) >> x.log_page;
         r.p[i] = ((cptr)x.row)[at < x.max_pages ? at : x.max_pages - 1];
     }
     return r;
@@ -597,7 +619,7 @@ struct Load {
     // drafted rows whatever the tile lacks: what does not exist becomes zeros when
     // it is put.  (One sequence of loads: with one each for committed and drafted
     // tiles the registers of both are live, 37 more.)
-    __device__ __forceinline__ void tile(const Axis& ax, int i, const Pages& pg, int row0, bool values) {
+    __device__ __forceinline__ void tile(const Axis& ax, int i, const Pages<ROWS>& pg, int row0, bool values) {
         const uint32_t lane = threadIdx.x & 63u;
         constexpr int kB = TYPE == RAC_CACHE_FP8 ? 1 : 2, kR = TYPE == RAC_CACHE_FP8 ? kRowsAtOnce8 : kRowsAtOnce;
         constexpr uint32_t kP = TYPE == RAC_CACHE_FP8 ? kPieces8 : kPieces;
@@ -607,29 +629,31 @@ struct Load {
         const int tile = past ? ax.ca + i : ax.da + i - ax.committed;
         // (eight aligned rows lie in one page: its address is the same in all
         // lanes, but for the second eight of sixteen)
-        const uint32_t inner = (kR > 8 ? in & 7u : in) * row_bytes;
+        const uint32_t inner = (kR > 8 ? in & 7u : in) * row_bytes + c;
         const uint8_t* const pool = ax.pool + (values ? ax.side : 0u);
         const uint8_t* eight[ROWS / 8];
 #pragma unroll
         for (int g = 0; g < ROWS / 8; ++g) {
-            int p = ROWS == 16 && row0 ? pg.p[(g + 2) & 3] : pg.p[g & 3];
-            p = (uint32_t)p < (uint32_t)ax.pages ? p : 0;
-            eight[g] = pool + (uint64_t)(uint32_t)p * ax.page_stride +
-                       ((uint32_t)(tile * kTile + row0 + 8 * g) & ((1u << ax.log_page) - 1u)) * row_bytes;
+            const uint32_t p = (uint32_t)pg.p[g] < (uint32_t)ax.pages ? (uint32_t)pg.p[g] : 0u;
+            eight[g] = pool + (((uint64_t)p * ax.page_stride << 4) +
+                               ((uint32_t)(tile * kTile + row0 + 8 * g) & ((1u << ax.log_page) - 1u)) * row_bytes);
         }
-        const uint8_t* const draft = reinterpret_cast<const uint8_t*>((values ? ax.v : ax.k) + (int64_t)tile * kTile * ax.kv_stride);
-        const int last = ax.n - 1 - tile * kTile;
+        // (a drafted row past the last reads the last)
+        const uint32_t stride = (uint32_t)(2 * ax.kv_stride);
+        const int first = tile * kTile + row0;
+        const uint8_t* const draft = reinterpret_cast<const uint8_t*>((values ? ax.v : ax.k) + (int64_t)(first < ax.n ? first : ax.n - 1) * ax.kv_stride);
+        const uint32_t own = past ? inner : in * stride + c, last = past ? ~0u : (first < ax.n ? ax.n - 1 - first : 0) * stride + c;
 #pragma unroll
         for (int y = 0; y < kN; ++y) {
-            const uint8_t* at = eight[y * kR / 8] + (uint32_t)(y * kR % 8) * row_bytes;
+            const uint8_t* at = eight[y * kR / 8];
             if constexpr (kR > 8) at = in >= 8u ? eight[(y * kR / 8 + 1) % (ROWS / 8)] : at;
-            uint32_t off = inner;
-            if constexpr (TYPE != RAC_CACHE_FP8) {
-                const int row = row0 + y * kR + (int)in;
-                at = past ? at : draft;
-                off = past ? off : (uint32_t)(row < last ? row : last) * (uint32_t)(2 * ax.kv_stride);
+            if constexpr (TYPE == RAC_CACHE_FP8) {
+                at += (uint32_t)(y * kR % 8) * row_bytes + inner;
+            } else {
+                const uint32_t off = own + (past ? (uint32_t)(y * kR % 8) * row_bytes : (uint32_t)(y * kR) * stride);
+                at = (past ? at : draft) + (off < last ? off : last);
             }
-            x[y] = *reinterpret_cast<const u32x4*>(at + (off + c));
+            x[y] = *reinterpret_cast<const u32x4*>(at);
         }
     }
     // Half a tile of drafted keys or values: with 8-bit pages the registers hold
@@ -677,6 +701,11 @@ struct Load {
                 }
         }
     }
+    __device__ __forceinline__ void put_zeros(u32x4* lds, int row0) {
+        if constexpr (TYPE == RAC_CACHE_FP8) {
+            for (uint32_t y = threadIdx.x & 63u; y < ROWS * DP / 8; y += 64u) lds[row0 * (DP / 8) + y] = u32x4{0u, 0u, 0u, 0u};
+        }
+    }
     __device__ __forceinline__ void put_wide(u32x4* lds, const Axis& ax, uint32_t valid, int row0, bool clean) {
         const uint32_t lane = threadIdx.x & 63u, c = lane % kPieces, in = lane / kPieces;
         if (valid != ~0u || ax.dim != DP)
@@ -713,12 +742,14 @@ struct Load {
 
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// The keys of committed tile `tile` that exist.
-__device__ __forceinline__ uint32_t committed_there(const Axis& x, int tile, const Pages& pg) {
-    uint32_t r = low_bits(x.length - tile * kTile);
+// The keys of a tile that exist, of those from row0 on (bits as in the tile).
+template <int ROWS>
+__device__ __forceinline__ uint32_t exist_of(const Axis& x, int i, const Pages<ROWS>& pg, int row0) {
+    if (i >= x.committed) return i < x.count ? low_bits(x.n - (x.da + i - x.committed) * kTile) : 0u;
+    uint32_t r = low_bits(x.length - (x.ca + i) * kTile);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if ((uint32_t)pg.p[i] >= (uint32_t)x.pages) r &= ~(0xFFu << (8 * i));
+    for (int g = 0; g < ROWS / 8; ++g)
+        if ((uint32_t)pg.p[g] >= (uint32_t)x.pages) r &= ~(0xFFu << (row0 + 8 * g));
     return r;
 }
 
@@ -727,12 +758,11 @@ struct Seen {
     int from, first, end, mask_row;
 };
 
-__device__ __forceinline__ uint32_t bits_of(const Seen& r, bool past, int tile) {
+__device__ __forceinline__ uint32_t bits_of(const Axis& x, const Seen& r, bool past, int tile) {
     if (past) return ~low_bits(r.from - tile * kTile);
     uint32_t b = low_bits(r.end - tile * kTile) & ~low_bits(r.first - tile * kTile);
-    const TreeArgs a = args_again();
-    if (a.mask && b)  // (a mask reaches r.end)
-        b &= reinterpret_cast<const uint32_t*>(a.mask + (size_t)r.mask_row * a.mask_words)[tile];
+    if (x.mask && b)  // (a mask reaches r.end)
+        b &= reinterpret_cast<const uint32_t*>(x.mask + (size_t)r.mask_row * x.mask_words)[tile];
     return b;
 }
 
@@ -857,16 +887,26 @@ __device__ __forceinline__ Work uniform(const Work& w) {
 }
 
 // The queries of a wavefront's rows, and what they see: into registers and LDS.
-// Returns the extremes: first committed position any (every) row sees from, the
-// first drafted token, and the end of the drafted ones.
+// Returns the extremes.
 struct Reach {
-    int from_lo, from_hi, first, end;
+    int from_lo, from_hi;    // least and greatest first committed position
+    int first, first_hi;     // of the first drafted token
+    int end, end_lo;         // greatest and least end of the drafted ones
+
+    // Whether every row sees all of a tile.
+    __device__ __forceinline__ bool all_see(const Axis& ax, bool past, int tile) const {
+        return past ? tile * kTile >= from_hi : !ax.mask && tile * kTile >= first_hi && (tile + 1) * kTile <= end_lo;
+    }
+    // Whether no row sees any of it.
+    __device__ __forceinline__ bool none_sees(bool past, int tile) const {
+        return past ? (tile + 1) * kTile <= from_lo : tile * kTile >= end || (tile + 1) * kTile <= first;
+    }
 };
 
 template <int TYPE, int DP, int TM>
 __device__ __forceinline__ Reach take_rows(const TreeArgs& a, const Work& w, int row0, Rows<TYPE, DP, TM>& rows, Seen* seen) {
     const uint32_t lane = threadIdx.x & 63u;
-    Reach x{1 << 30, 0, 1 << 30, 0};
+    Reach x{1 << 30, 0, 1 << 30, 0, 0, 1 << 30};
 #pragma unroll
     for (int r = 0; r < TM; ++r) {
         const RowAt at = row_at(a, w, row0 + 16 * r + (int)(lane & 15u));
@@ -874,7 +914,9 @@ __device__ __forceinline__ Reach take_rows(const TreeArgs& a, const Work& w, int
         x.from_lo = at.see.from < x.from_lo ? at.see.from : x.from_lo;
         x.from_hi = at.see.from > x.from_hi ? at.see.from : x.from_hi;
         x.first = at.see.first < x.first ? at.see.first : x.first;
+        x.first_hi = at.see.first > x.first_hi ? at.see.first : x.first_hi;
         x.end = at.see.end > x.end ? at.see.end : x.end;
+        x.end_lo = at.see.end < x.end_lo ? at.see.end : x.end_lo;
         const uint16_t* q = a.q + (int64_t)(w.q.q0 + at.node) * a.q_stride + (int64_t)at.head * a.dim;
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t) {
@@ -883,7 +925,8 @@ __device__ __forceinline__ Reach take_rows(const TreeArgs& a, const Work& w, int
             if (c < a.dim) rows.q[r][t] = *reinterpret_cast<const u32x4*>(q + c);
         }
     }
-    return Reach{min_wave(x.from_lo), max_wave(x.from_hi), min_wave(x.first), max_wave(x.end)};
+    return Reach{min_wave(x.from_lo), max_wave(x.from_hi), min_wave(x.first), max_wave(x.first_hi), max_wave(x.end),
+                 min_wave(x.end_lo)};
 }
 
 // Few rows: all wavefronts hold the same 16 TM rows and take key tiles in
@@ -901,13 +944,12 @@ __global__ __launch_bounds__(64 * kWaves, TM == 1 && (DP == 64 || TYPE == RAC_CA
     const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
     Rows<TYPE, DP, TM> rows;
     Axis ax;
-    int from_hi;
+    Reach x;
     {
         Work w;
         if (!find_work(a, (int)blockIdx.x, w)) return;
         if (threadIdx.x == 0u) work = w;
-        const Reach x = take_rows(a, w, w.row_tile * M, rows, seen[wv]);
-        from_hi = x.from_hi;
+        x = take_rows(a, w, w.row_tile * M, rows, seen[wv]);
         ax = axis_of<TYPE>(a, w, x.from_lo, x.first, x.end);
     }
     u32x4* const tile_lds = reinterpret_cast<u32x4*>(mem) + wv * kTileP;
@@ -916,15 +958,11 @@ __global__ __launch_bounds__(64 * kWaves, TM == 1 && (DP == 64 || TYPE == RAC_CA
     auto pass = [&](bool clean) {
         rows.start();
         uint32_t there = 0;
-        Pages pg{};
-        // the keys of tile i that exist
-        auto exist = [&](int i) {
-            return i < ax.committed ? committed_there(ax, ax.ca + i, pg) : low_bits(ax.n - (ax.da + i - ax.committed) * kTile);
-        };
-        auto fetch = [&](int i) { if (i < ax.committed) pg = pages_of(ax, ax.ca + i); };
+        Pages<kTile> pg{};
+        auto fetch = [&](int i) { if (i < ax.committed) pg = pages_of<kTile>(ax, ax.ca + i, 0); };
         fetch(wv);
         if (wv < ax.count) {
-            there = exist(wv);
+            there = exist_of(ax, wv, pg, 0);
             if (TYPE != RAC_CACHE_FP8 || wv < ax.committed) {
                 lk.tile(ax, wv, pg, 0, false);
                 lv.tile(ax, wv, pg, 0, true);
@@ -940,12 +978,12 @@ __global__ __launch_bounds__(64 * kWaves, TM == 1 && (DP == 64 || TYPE == RAC_CA
             else
                 lk.put_drafted(tile_lds, ax, ax.k, tile, now, 0, false);
             if (i + kWaves < ax.count) {
-                there = exist(i + kWaves);
+                there = exist_of(ax, i + kWaves, pg, 0);
                 if (TYPE != RAC_CACHE_FP8 || i + kWaves < ax.committed) lk.tile(ax, i + kWaves, pg, 0, false);
             }
             wave_sync();
-            f32x4 s[TM][2];
-            rows.scores(tile_lds, s);
+            f32x4 s[1][TM][2];
+            rows.scores(tile_lds, s[0]);
             wave_sync();
             if (past)
                 lv.put_committed(tile_lds, ax, now, 0, clean);
@@ -954,17 +992,18 @@ __global__ __launch_bounds__(64 * kWaves, TM == 1 && (DP == 64 || TYPE == RAC_CA
             if (i + kWaves < (TYPE == RAC_CACHE_FP8 ? ax.committed : ax.count)) lv.tile(ax, i + kWaves, pg, 0, true);
             fetch(i + 2 * kWaves);
             bool mixed = false;
-            if (!(past && now == ~0u && tile * kTile >= from_hi)) {
+            if (!(now == ~0u && x.all_see(ax, past, tile))) {
                 uint32_t bits[TM];
 #pragma unroll
-                for (int r = 0; r < TM; ++r) bits[r] = now & bits_of(seen[wv][16 * r + (lane & 15u)], past, tile);
-                mixed = rows.hide(s, bits, now);
+                for (int r = 0; r < TM; ++r) bits[r] = now & bits_of(ax, seen[wv][16 * r + (lane & 15u)], past, tile);
+                mixed = rows.hide(s[0], bits, now);
             }
-            u32x4 p[TM];
-            rows.weights(s, narrow ? c8 : c16, narrow ? v8 : 1.0f, p);
+            u32x4 p[1][TM];
+            const float c[1] = {narrow ? c8 : c16}, vs[1] = {narrow ? v8 : 1.0f};
+            rows.weights(s, c, vs, p);
             wave_sync();
             if (mixed) rows.look(tile_lds);
-            rows.values(tile_lds, p);
+            rows.values(tile_lds, p[0]);
             wave_sync();
         }
     };
@@ -1041,7 +1080,7 @@ template <int TYPE, int DP, int TM>
 __global__ __launch_bounds__(64 * kWaves, TM * DP <= 256 && DP < 256 ? 2 : 1) void tree_many_kernel(TreeArgs a) {
     constexpr int M = 16 * TM * kWaves, kTileP = kTile * DP / 8;
     __shared__ u32x4 mem[2][2][2][kTileP];  // pair, tile, keys or values
-    __shared__ uint32_t exist[2][2];         // the keys of a tile that exist
+    __shared__ alignas(4) uint16_t exist[2][2][2];  // the keys of a tile that exist, by halves
     __shared__ Seen seen[kWaves][16 * TM];
     __shared__ Reach reach[kWaves];
     __shared__ Work work;
@@ -1071,6 +1110,10 @@ __global__ __launch_bounds__(64 * kWaves, TM * DP <= 256 && DP < 256 ? 2 : 1) vo
         const auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
         ax = axis_of<TYPE>(a, w, u(all.from_lo), u(all.first), u(all.end));
     }
+    // the tiles that this wavefront's rows see all of, if all their keys exist, as runs of indices
+    const int plain0 = (x.from_hi + kTile - 1) / kTile - ax.ca, draft0 = ax.committed - ax.da;
+    const int plain2 = ax.mask ? 1 << 30 : draft0 + (x.first_hi + kTile - 1) / kTile, plain3 = draft0 + x.end_lo / kTile;
+    const auto plain = [&](int i) { return i < ax.committed ? i >= plain0 : i >= plain2 && i < plain3; };
     // (this wavefront brings half a tile of every pair)
     const int half = 16 * (wv & 1), which = wv >> 1;
     Load<TYPE, DP, 16> lk, lv;
@@ -1078,55 +1121,71 @@ __global__ __launch_bounds__(64 * kWaves, TM * DP <= 256 && DP < 256 ? 2 : 1) vo
     bool clean = false;
 again:
     rows.start();
-    Pages pg{};
+    Pages<16> pg{};
     uint32_t there = 0;
-    auto load = [&](int i) {  // (a pair's second tile may be missing: what is put there is not used)
-        if (i >= ax.count) return;
-        there = i < ax.committed ? committed_there(ax, ax.ca + i, pg) : low_bits(ax.n - (ax.da + i - ax.committed) * kTile);
-        if (TYPE == RAC_CACHE_FP8 && i >= ax.committed) return;
+    auto load = [&](int i) {
+        there = exist_of(ax, i, pg, half);
+        if (i >= (TYPE == RAC_CACHE_FP8 ? ax.committed : ax.count)) return;
         lk.tile(ax, i, pg, half, false);
         lv.tile(ax, i, pg, half, true);
     };
-    auto fetch = [&](int i) { if (i < ax.committed) pg = pages_of(ax, ax.ca + i); };
+    auto fetch = [&](int i) { if (i < ax.committed) pg = pages_of<16>(ax, ax.ca + i, half); };
+    auto pair = [&](int i, u32x4 (&buf)[2][2][kTileP], uint16_t (&ex)[2][2]) {
+        const int mine = i + which;
+        if (TYPE != RAC_CACHE_FP8 || mine < ax.committed) {
+            lk.put_committed(buf[which][0], ax, there, half, false);
+            lv.put_committed(buf[which][1], ax, there, half, clean);
+        } else if (mine < ax.count) {
+            const int tile = ax.da + mine - ax.committed;
+            lk.put_drafted(buf[which][0], ax, ax.k, tile, there, half, false);
+            lv.put_drafted(buf[which][1], ax, ax.v, tile, there, half, clean);
+        } else {
+            lk.put_zeros(buf[which][0], half);
+            lv.put_zeros(buf[which][1], half);
+        }
+        if (lane == 0u) ex[which][wv & 1] = (uint16_t)(there >> half);
+        load(mine + 2);
+        fetch(mine + 4);
+        __syncthreads();
+        if (!busy) return;
+        // two tiles at a time: their products and weights overlap
+        f32x4 s[2][TM][2];
+        const uint32_t now0 = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t*>(ex[0]));
+        const uint32_t now1 = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t*>(ex[1]));
+        if ((now0 & now1) == ~0u && plain(i) && plain(i + 1)) {
+            rows.scores(buf[0][0], s[0]);
+            rows.scores(buf[1][0], s[1]);
+        } else {
+            const auto tile_of = [&](int j) { return j < ax.committed ? ax.ca + j : ax.da + j - ax.committed; };
+            // what no row of this wavefront sees is passed over
+            if (x.none_sees(i < ax.committed, tile_of(i)) &&
+                (i + 1 >= ax.count || x.none_sees(i + 1 < ax.committed, tile_of(i + 1))))
+                return;
+            rows.scores(buf[0][0], s[0]);
+            rows.scores(buf[1][0], s[1]);
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const uint32_t now = y ? now1 : now0;
+                uint32_t bits[TM];
+#pragma unroll
+                for (int r = 0; r < TM; ++r)
+                    bits[r] = now ? now & bits_of(ax, seen[wv][16 * r + (lane & 15u)], i + y < ax.committed, tile_of(i + y)) : 0u;
+                if (rows.hide(s[y], bits, now)) rows.look(buf[y][1]);
+            }
+        }
+        u32x4 p[2][TM];
+        const bool n0 = TYPE == RAC_CACHE_FP8 && i < ax.committed, n1 = TYPE == RAC_CACHE_FP8 && i + 1 < ax.committed;
+        const float c[2] = {n0 ? c8 : c16, n1 ? c8 : c16}, vs[2] = {n0 ? v8 : 1.0f, n1 ? v8 : 1.0f};
+        rows.weights(s, c, vs, p);
+        rows.values(buf[0][1], p[0]);
+        rows.values(buf[1][1], p[1]);
+    };
     fetch(which);
     load(which);
     fetch(which + 2);
-    for (int i = 0; i < ax.count; i += 2) {
-        u32x4(&buf)[2][2][kTileP] = mem[(i >> 1) & 1];
-        if (i + which < ax.committed) {
-            lk.put_committed(buf[which][0], ax, there, half, false);
-            lv.put_committed(buf[which][1], ax, there, half, clean);
-        } else if (i + which < ax.count) {
-            const int tile = ax.da + i + which - ax.committed;
-            lk.put_drafted(buf[which][0], ax, ax.k, tile, there, half, false);
-            lv.put_drafted(buf[which][1], ax, ax.v, tile, there, half, clean);
-        }
-        if (half == 0 && lane == 0u) exist[(i >> 1) & 1][which] = there;
-        if (i + 2 < ax.count) load(i + 2 + which);
-        fetch(i + 4 + which);
-        __syncthreads();
-#pragma unroll 1
-        for (int y = 0; y < 2; ++y) {
-            const int j = i + y;
-            if (j >= ax.count || !busy) break;
-            const bool past = j < ax.committed;
-            const int tile = past ? ax.ca + j : ax.da + j - ax.committed;
-            // what no row of this wavefront sees is passed over
-            if (past ? (tile + 1) * kTile <= x.from_lo : tile * kTile >= x.end || (tile + 1) * kTile <= x.first) continue;
-            const uint32_t now = __builtin_amdgcn_readfirstlane(exist[(i >> 1) & 1][y]);
-            f32x4 s[TM][2];
-            rows.scores(buf[y][0], s);
-            if (!(past && now == ~0u && tile * kTile >= x.from_hi)) {
-                uint32_t bits[TM];
-#pragma unroll
-                for (int r = 0; r < TM; ++r) bits[r] = now & bits_of(seen[wv][16 * r + (lane & 15u)], past, tile);
-                if (rows.hide(s, bits, now)) rows.look(buf[y][1]);
-            }
-            const bool narrow = TYPE == RAC_CACHE_FP8 && past;
-            u32x4 p[TM];
-            rows.weights(s, narrow ? c8 : c16, narrow ? v8 : 1.0f, p);
-            rows.values(buf[y][1], p);
-        }
+    for (int i = 0; i < ax.count; i += 4) {
+        pair(i, mem[0], exist[0]);
+        if (i + 2 < ax.count) pair(i + 2, mem[1], exist[1]);
     }
     if (!clean && __syncthreads_or(rows.alone)) {
         clean = true;
