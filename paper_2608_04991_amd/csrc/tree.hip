@@ -205,15 +205,6 @@ __device__ __forceinline__ int chunk_tiles(const TreeArgs& a, int64_t total) {
     return c < a.min_chunk ? a.min_chunk : (int)(c < (1 << 30) ? c : (1 << 30));
 }
 
-__device__ __forceinline__ int scan_wave(int v) {  // sum over the lanes up to this one
-    const int lane = (int)threadIdx.x & 63;
-    for (int o = 1; o < 64; o <<= 1) {
-        const int x = __shfl_up(v, o);
-        v += lane >= o ? x : 0;
-    }
-    return v;
-}
-
 // Up to 64 sequences need no launch ahead: a lane a sequence, each wavefront
 // finds the cuts by itself.  (A launch ahead of 8 sequences takes longer than
 // that; beyond 64 each wavefront would read all sequences again and again: 200
@@ -238,9 +229,15 @@ __device__ __forceinline__ LaneSeq lane_seq(const TreeArgs& a) {
         most = chunk_tiles(a, total);
     }
     if (lane < a.seqs) r.c = cut_of(a, r.q, most);
-    const int units = r.c.tiles * r.c.chunks * a.heads, split = r.c.chunks > 1 ? units : 0;
-    r.base = scan_wave(units) - units;
-    r.slot = a.target ? scan_wave(split) - split : 0;
+    const int units = r.c.tiles * r.c.chunks * a.heads;
+    // the sequences with the longest parts first: what starts last ends last
+    const int keys = lane < a.seqs ? (key_tiles(a, r.q) + r.c.chunks - 1) / r.c.chunks : -1;
+    for (int j = 0; j < a.seqs; ++j) {
+        const int k = __builtin_amdgcn_readlane(keys, j), u = __builtin_amdgcn_readlane(units, j);
+        const bool ahead = k > keys || (k == keys && j < lane);
+        r.base += ahead ? u : 0;
+        r.slot += ahead && __builtin_amdgcn_readlane(r.c.chunks, j) > 1 ? u : 0;
+    }
     return r;
 }
 
@@ -273,9 +270,9 @@ __device__ __forceinline__ bool find_work(const TreeArgs& a, int block, Work& w)
         w.slot = p.slot + i;
     } else {
         const LaneSeq l = lane_seq(a);
-        const uint64_t past = __ballot(block < l.base + l.c.tiles * l.c.chunks * a.heads);
-        if (!past) return false;
-        const int at = __builtin_ctzll(past);
+        const uint64_t mine = __ballot(block >= l.base && block < l.base + l.c.tiles * l.c.chunks * a.heads);
+        if (!mine) return false;
+        const int at = __builtin_ctzll(mine);
         const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
         w.seq = at;
         w.q = Seq{of(l.q.q0), of(l.q.m), of(l.q.d0), of(l.q.n), of(l.q.length)};
