@@ -62,7 +62,26 @@ class CacheConfig:
     v_scale: float = 1.0
 
     def _c(self) -> _CacheConfig:
-        return _cache_struct(self)
+        return self._struct
+
+    # (made once a configuration: the small calls are bound by the host, and the
+    # library reads the struct during the call only)
+    @functools.cached_property
+    def _struct(self) -> _CacheConfig:
+        return _CacheConfig(self.layers, self.kv_heads, self.head_dim, self.page_tokens, self.pages, self.seqs,
+                            self.max_pages, self.type, self.k_scale, self.v_scale)
+
+    @functools.cached_property
+    def _ref(self):
+        return ctypes.byref(self._struct)
+
+    @functools.cached_property
+    def _pool_bytes(self) -> int:
+        return int(_rac.library().rac_cache_pool_bytes(self._ref))
+
+    @functools.cached_property
+    def _commit_bytes(self) -> int:
+        return int(_rac.library().rac_cache_commit_workspace(self._ref))
 
 
 @dataclass(frozen=True)
@@ -75,20 +94,15 @@ class TreeConfig:
     scale: float = 0.0
 
     def _c(self) -> _TreeConfig:
-        return _tree_struct(self)
+        return self._struct
 
+    @functools.cached_property
+    def _struct(self) -> _TreeConfig:
+        return _TreeConfig(self.q_heads, self.rows, self.max_rows, self.max_draft, self.window, self.scale)
 
-# (the library reads the structs during the call only, so one instance per
-# configuration can be passed to every call)
-@functools.lru_cache(maxsize=512)
-def _cache_struct(c: CacheConfig) -> _CacheConfig:
-    return _CacheConfig(c.layers, c.kv_heads, c.head_dim, c.page_tokens, c.pages, c.seqs, c.max_pages, c.type,
-                        c.k_scale, c.v_scale)
-
-
-@functools.lru_cache(maxsize=512)
-def _tree_struct(t: TreeConfig) -> _TreeConfig:
-    return _TreeConfig(t.q_heads, t.rows, t.max_rows, t.max_draft, t.window, t.scale)
+    @functools.cached_property
+    def _ref(self):
+        return ctypes.byref(self._struct)
 
 
 def declare(L) -> None:
@@ -115,35 +129,29 @@ def _pool(cfg: CacheConfig, pool, what: str = "pool"):
     if pool is None or isinstance(pool, int):
         return pool
     size = pool.element_size()
-    return _rac._dev(pool, what, size, -(-_pool_bytes(cfg, _rac.library()) // size))
+    return _rac._dev(pool, what, size, -(-cfg._pool_bytes // size))
 
 
 def _rows(t, what: str, rows: int, heads: int, dim: int):
-    """(address, elements between rows) of a 16-bit [rows][heads][dim] tensor
-    whose heads lie together; its rows may be apart."""
-    if t is None or isinstance(t, int):
-        return t, heads * dim
+    """(address, elements between rows, rows) of a 16-bit [rows][heads][dim]
+    tensor whose heads lie together; its rows may be apart."""
     try:
-        if t.is_cuda and t.element_size() == 2 and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dim \
-                and t.shape[0] >= rows:
-            st = t.stride()
-            if t.shape[0] <= 1:
-                st = (heads * dim, st[1], st[2])
-            if st[2] == 1 and (st[1] == dim or heads == 1) and st[0] >= heads * dim:
-                return t.data_ptr(), st[0]
-    except AttributeError:
-        pass
+        n, h, d = t.shape
+        row, head, one = t.stride()
+        if n <= 1:
+            row = heads * dim
+        if h == heads and d == dim and n >= rows and one == 1 and (head == dim or h == 1) and row >= heads * dim \
+                and t.is_cuda and t.element_size() == 2:
+            return t.data_ptr(), row, n
+    except (AttributeError, ValueError, TypeError):
+        if t is None or isinstance(t, int):
+            return t, heads * dim, rows
     raise ValueError(f"{what}: expected a GPU tensor of 2-byte elements, [{rows}][{heads}][{dim}], heads and channels "
                      "contiguous")
 
 
 def rac_cache_pool_bytes(cfg: CacheConfig) -> int:
-    return _pool_bytes(cfg, _rac.library())
-
-
-@functools.lru_cache(maxsize=512)
-def _pool_bytes(cfg: CacheConfig, lib) -> int:
-    return int(lib.rac_cache_pool_bytes(ctypes.byref(cfg._c())))
+    return cfg._pool_bytes
 
 
 def rac_cache_new(cfg: CacheConfig, device: str = "cuda"):
@@ -155,12 +163,12 @@ def rac_cache_new(cfg: CacheConfig, device: str = "cuda"):
 
 
 def rac_tree_attention_workspace(cfg: CacheConfig, tree: TreeConfig) -> int:
-    return _attention_workspace(cfg, tree, _rac.library())
-
-
-@functools.lru_cache(maxsize=512)
-def _attention_workspace(cfg: CacheConfig, tree: TreeConfig, lib) -> int:
-    return int(lib.rac_tree_attention_workspace(ctypes.byref(cfg._c()), ctypes.byref(tree._c())))
+    # (both are immutable: the size of the last pair stays with the tree)
+    last = tree.__dict__.get("_workspace")
+    if last is None or last[0] is not cfg:
+        last = cfg, int(_rac.library().rac_tree_attention_workspace(cfg._ref, tree._ref))
+        tree.__dict__["_workspace"] = last
+    return last[1]
 
 
 def rac_tree_attention(cfg: CacheConfig, tree: TreeConfig, layer: int, pool, table, lengths, q, q_start, k, v, out,
@@ -172,26 +180,24 @@ def rac_tree_attention(cfg: CacheConfig, tree: TreeConfig, layer: int, pool, tab
     [rows][q_heads].  Rows of q, k, v and out may be apart (views of a larger
     tensor); k and v by the same distance."""
     dev = _rac._dev
-    R, H, D = tree.rows, cfg.kv_heads, cfg.head_dim
-    drafted = 0 if k is None or isinstance(k, int) else int(k.shape[0])
-    qp, qs = _rows(q, "q", R, tree.q_heads, D)
-    op, os_ = _rows(out, "out", R, tree.q_heads, D)
-    kp, ks = _rows(k, "k", 0, H, D)
-    vp, vs = _rows(v, "v", drafted, H, D)
-    if k is not None and v is not None and drafted > 1 and ks != vs:
+    R, Q, H, D, S = tree.rows, tree.q_heads, cfg.kv_heads, cfg.head_dim, cfg.seqs
+    qp, qs, _ = _rows(q, "q", R, Q, D)
+    op, os_, _ = _rows(out, "out", R, Q, D)
+    kp, ks, drafted = _rows(k, "k", 0, H, D)
+    vp, vs, _ = _rows(v, "v", drafted, H, D)
+    if ks != vs and drafted > 1 and v is not None:
         raise ValueError("k and v: expected the same distance between rows")
     words = 0
     if mask is not None:
         words = mask if isinstance(mask, int) else int(mask.shape[-1])
-    t = _TreeTensors(qp, kp, vp, dev(q_start, "q_start", 4, cfg.seqs + 1),
-                     dev(draft_start, "draft_start", 4, cfg.seqs + 1), dev(mask, "mask", 8, R * words), op,
-                     dev(lse, "lse", 4, R * tree.q_heads), qs, ks, os_, drafted, words)
-    need = _attention_workspace(cfg, tree, _rac.library())
-    _rac._check(_rac.library().rac_tree_attention(
-        ctypes.byref(cfg._c()), ctypes.byref(tree._c()), int(layer), _pool(cfg, pool),
-        dev(table, "table", 4, cfg.seqs * cfg.max_pages), dev(lengths, "lengths", 4, cfg.seqs), ctypes.byref(t),
-        dev(workspace, "workspace", 1, need), need if isinstance(workspace, int) else _rac._nbytes(workspace),
-        _rac._stream(stream)), "rac_tree_attention")
+    t = _TreeTensors(qp, kp, vp, dev(q_start, "q_start", 4, S + 1), dev(draft_start, "draft_start", 4, S + 1),
+                     dev(mask, "mask", 8, R * words), op, dev(lse, "lse", 4, R * Q), qs, ks, os_, drafted, words)
+    need = rac_tree_attention_workspace(cfg, tree)
+    status = _rac.library().rac_tree_attention(
+        cfg._ref, tree._ref, layer, _pool(cfg, pool), dev(table, "table", 4, S * cfg.max_pages),
+        dev(lengths, "lengths", 4, S), ctypes.byref(t), dev(workspace, "workspace", 1, need), need, _rac._stream(stream))
+    if status:
+        _rac._check(status, "rac_tree_attention")
 
 
 def rac_cache_fork(cfg: CacheConfig, parents, table, lengths, refs, keep_from=None, keep_to=None, stream=None) -> None:
@@ -200,18 +206,13 @@ def rac_cache_fork(cfg: CacheConfig, parents, table, lengths, refs, keep_from=No
     and free sequences, in place."""
     dev, S = _rac._dev, cfg.seqs
     _rac._check(_rac.library().rac_cache_fork(
-        ctypes.byref(cfg._c()), dev(parents, "parents", 4, S), dev(keep_from, "keep_from", 4, S),
+        cfg._ref, dev(parents, "parents", 4, S), dev(keep_from, "keep_from", 4, S),
         dev(keep_to, "keep_to", 4, S), dev(table, "table", 4, S * cfg.max_pages), dev(lengths, "lengths", 4, S),
         dev(refs, "refs", 4, cfg.pages), _rac._stream(stream)), "rac_cache_fork")
 
 
 def rac_cache_commit_workspace(cfg: CacheConfig) -> int:
-    return _commit_workspace(cfg, _rac.library())
-
-
-@functools.lru_cache(maxsize=512)
-def _commit_workspace(cfg: CacheConfig, lib) -> int:
-    return int(lib.rac_cache_commit_workspace(ctypes.byref(cfg._c())))
+    return cfg._commit_bytes
 
 
 def _layers(t, what: str, cfg: CacheConfig):
@@ -219,15 +220,16 @@ def _layers(t, what: str, cfg: CacheConfig):
     [layers][rows][kv_heads][head_dim] tensor."""
     H, D = cfg.kv_heads, cfg.head_dim
     try:
-        if t.is_cuda and t.element_size() == 2 and t.dim() == 4 and t.shape[0] == cfg.layers and t.shape[2] == H \
-                and t.shape[3] == D:
-            st, rows = t.stride(), int(t.shape[1])
-            row = st[1] if rows > 1 else H * D
-            if (st[3] == 1 and (st[2] == D or H == 1)) and row >= H * D:
-                return t.data_ptr(), row, st[0] if cfg.layers > 1 else 0, rows
+        layers, rows, heads, dim = t.shape
+        layer, row, head, one = t.stride()
+        if layers == cfg.layers and heads == H and dim == D and t.is_cuda and t.element_size() == 2:
             if t.numel() == 0:
                 return t.data_ptr(), H * D, 0, rows
-    except AttributeError:
+            if rows == 1:
+                row = H * D
+            if one == 1 and (head == D or H == 1) and row >= H * D:
+                return t.data_ptr(), row, layer if layers > 1 else 0, rows
+    except (AttributeError, ValueError, TypeError):
         pass
     raise ValueError(f"{what}: expected a GPU tensor of 2-byte elements, [{cfg.layers}][rows][{H}][{D}], heads and "
                      "channels contiguous")
@@ -246,19 +248,18 @@ def rac_cache_commit(cfg: CacheConfig, pool, table, lengths, refs, k, v, draft_s
         raise ValueError("k and v: expected the same rows, apart by the same distances")
     if max_path is None:
         max_path = rows if path is None else int(path.shape[-1])
-    need = _commit_workspace(cfg, _rac.library())
     _rac._check(_rac.library().rac_cache_commit(
-        ctypes.byref(cfg._c()), _pool(cfg, pool), dev(table, "table", 4, S * cfg.max_pages),
+        cfg._ref, _pool(cfg, pool), dev(table, "table", 4, S * cfg.max_pages),
         dev(lengths, "lengths", 4, S), dev(refs, "refs", 4, cfg.pages), kp, vp, row, layer, rows,
         dev(draft_start, "draft_start", 4, S + 1), dev(path, "path", 4, S * int(max_path)), int(max_path),
-        dev(committed, "committed", 4, S), dev(workspace, "workspace", 1, need),
-        need if isinstance(workspace, int) else _rac._nbytes(workspace), _rac._stream(stream)), "rac_cache_commit")
+        dev(committed, "committed", 4, S), dev(workspace, "workspace", 1, cfg._commit_bytes), cfg._commit_bytes,
+        _rac._stream(stream)), "rac_cache_commit")
 
 
 def rac_cache_copy(cfg: CacheConfig, src_pool, src, dst_pool, dst, n: int | None = None, stream=None) -> None:
     """Copies page src[i] of src_pool to page dst[i] of dst_pool (int32 arrays)."""
     count = int(n) if n is not None else int(src.numel())
     _rac._check(_rac.library().rac_cache_copy(
-        ctypes.byref(cfg._c()), _pool(cfg, src_pool, "src_pool"), _rac._dev(src, "src", 4, count),
+        cfg._ref, _pool(cfg, src_pool, "src_pool"), _rac._dev(src, "src", 4, count),
         _pool(cfg, dst_pool, "dst_pool"), _rac._dev(dst, "dst", 4, count), count, _rac._stream(stream)),
         "rac_cache_copy")

@@ -11,7 +11,7 @@ namespace {
 // ---------------------------------------------------------------------------
 // Fork.  A table entry only moves within its column, so a workgroup that owns
 // whole columns can read all of them before it writes any, in place and in one
-// launch: kCols columns of all sequences through LDS.  Lengths move within the
+// launch: COLS columns of all sequences through LDS.  Lengths move within the
 // first workgroup alone.
 struct ForkArgs {
     const int32_t* parents;
@@ -23,30 +23,57 @@ struct ForkArgs {
     int32_t seqs, max_pages, pages, log_page;
 };
 
-constexpr int kForkCols = 4;
 constexpr int kForkThreads = 256;
 
+// Adds to the count of a page; neighbouring sequences often hold the same one,
+// so a thread adds up what it has for a page before it touches the count.
+struct RefSum {
+    int32_t* refs;
+    int32_t pages, page, sum;
+    __device__ __forceinline__ void add(int p, int by) {
+        if (p != page) {
+            flush();
+            page = p;
+        }
+        sum += by;
+    }
+    __device__ __forceinline__ void flush() {
+        if (sum != 0 && page >= 0 && page < pages) atomicAdd(refs + page, sum);
+        sum = 0;
+    }
+};
+
+template <int COLS>
 __global__ __launch_bounds__(kForkThreads) void cache_fork_kernel(ForkArgs a) {
-    extern __shared__ int32_t old[];  // [seqs][kForkCols]
-    const int c = (int)threadIdx.x % kForkCols, j = (int)blockIdx.x * kForkCols + c;
+    extern __shared__ int32_t old[];  // [seqs][COLS]
+    constexpr int kRows = kForkThreads / COLS;
+    const int c = (int)threadIdx.x % COLS, j = (int)blockIdx.x * COLS + c;
+    const int each = (a.seqs + kRows - 1) / kRows;  // sequences a thread, one after the other
+    const int d0 = (int)threadIdx.x / COLS * each, d1 = d0 + each < a.seqs ? d0 + each : a.seqs;
     const bool in = j < a.max_pages;
-    if (in)
-        for (int d = (int)threadIdx.x / kForkCols; d < a.seqs; d += kForkThreads / kForkCols)
-            old[d * kForkCols + c] = a.table[(size_t)d * a.max_pages + j];
+    int32_t* const column = a.table + j;
+    if (in) {
+#pragma unroll 8
+        for (int d = d0; d < d1; ++d) old[d * COLS + c] = column[(size_t)d * a.max_pages];
+    }
     __syncthreads();
     if (in) {
         const int first = j << a.log_page, past = (j + 1) << a.log_page;
-        for (int d = (int)threadIdx.x / kForkCols; d < a.seqs; d += kForkThreads / kForkCols) {
-            const int parent = a.parents[d], was = old[d * kForkCols + c];
-            int now = parent >= 0 && parent < a.seqs ? old[parent * kForkCols + c] : -1;
+        RefSum less{a.refs, a.pages, -1, 0}, more{a.refs, a.pages, -1, 0};
+#pragma unroll 4
+        for (int d = d0; d < d1; ++d) {
+            const int parent = a.parents[d], was = old[d * COLS + c];
+            int now = parent >= 0 && parent < a.seqs ? old[parent * COLS + c] : -1;
             if (a.to && first >= a.to[d]) now = -1;
             if (a.from && past <= a.from[d]) now = -1;
             if (now < 0 || now >= a.pages) now = -1;
             if (now == was) continue;
-            a.table[(size_t)d * a.max_pages + j] = now;
-            if (was >= 0 && was < a.pages) atomicAdd(a.refs + was, -1);
-            if (now >= 0) atomicAdd(a.refs + now, 1);
+            column[(size_t)d * a.max_pages] = now;
+            less.add(was, -1);
+            more.add(now, 1);
         }
+        less.flush();
+        more.flush();
     }
     if (blockIdx.x != 0) return;
     __syncthreads();
@@ -86,6 +113,7 @@ struct PlanArgs {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / 64;
+constexpr int kNear = 4096;
 
 // Rows of a sequence's drafts, whatever start[] holds.
 __device__ __forceinline__ int2 row_range(const int32_t* start, int s, int rows) {
@@ -93,9 +121,31 @@ __device__ __forceinline__ int2 row_range(const int32_t* start, int s, int rows)
     return make_int2(lo, hi - lo);
 }
 
+// How many of the first entries of a path name one of `drafted` rows.
+__device__ __forceinline__ int path_length(const int32_t* p, int most, int drafted) {
+    for (int n = 0;; n += 8) {
+        int e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = n + i < most ? p[n + i] : -1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (e[i] < 0 || e[i] >= drafted) return n + i;
+    }
+}
+
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
     __shared__ int sums[kPlanWaves];
-    const int t = (int)threadIdx.x, page = 1 << a.log_page;
+    __shared__ int32_t near[kNear];  // the first free pages (the others through memory)
+    const int t = (int)threadIdx.x, lane = t & 63, page = 1 << a.log_page;
+    // A wavefront looks at 1024 pages a step, 64 at a time, in ascending order.
+    constexpr int kEach = 16, kStep = kPlanThreads * kEach;
+    const int own = t / 64 * (64 * kEach) + lane;
+    int ref[kEach];
+    auto look = [&](int p0) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) ref[i] = p0 + own + 64 * i < a.pages ? a.refs[p0 + own + 64 * i] : 1;
+    };
+    look(0);  // (on its way while the demand is counted)
     constexpr int kPer = 4;  // sequences a thread (4096 / 1024)
     int tokens[kPer], need[kPer], base[kPer], length[kPer], tail[kPer];
     bool copies[kPer], fresh[kPer];
@@ -103,28 +153,26 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int s = t + i * kPlanThreads;
-        tokens[i] = need[i] = length[i] = 0;
+        tokens[i] = need[i] = length[i] = base[i] = 0;
         tail[i] = -1;
         copies[i] = fresh[i] = false;
+        if (i * kPlanThreads >= a.seqs) continue;
         if (s < a.seqs) {
-            const int drafted = row_range(a.start, s, a.draft_rows).y;
-            int n = 0;
-            if (a.path) {
-                const int32_t* p = a.path + (size_t)s * a.max_path;
-                while (n < a.max_path && p[n] >= 0 && p[n] < drafted) ++n;
-            } else {
-                n = drafted < a.max_path ? drafted : a.max_path;
-            }
             const int most = a.max_pages << a.log_page, len = clamp_int(a.lengths[s], 0, most);
+            const int32_t* const row = a.table + (size_t)s * a.max_pages;
+            const int drafted = row_range(a.start, s, a.draft_rows).y;
+            if (len & (page - 1)) tail[i] = row[len >> a.log_page];
+            if ((uint32_t)tail[i] >= (uint32_t)a.pages) tail[i] = -1;
+            const bool shared = tail[i] >= 0 && a.refs[tail[i] < 0 ? 0 : tail[i]] > 1;
+            const int n = a.path ? path_length(a.path + (size_t)s * a.max_path, a.max_path, drafted)
+                                 : drafted < a.max_path ? drafted : a.max_path;
             length[i] = len;
             if (n > 0 && n <= most - len) {
                 tokens[i] = n;
                 need[i] = ((len + n + page - 1) >> a.log_page) - ((len + page - 1) >> a.log_page);
                 if (len & (page - 1)) {
-                    tail[i] = a.table[(size_t)s * a.max_pages + (len >> a.log_page)];
-                    if (tail[i] < 0 || tail[i] >= a.pages) tail[i] = -1;
-                    copies[i] = tail[i] >= 0 && a.refs[tail[i]] > 1;
-                    fresh[i] = copies[i] || tail[i] < 0;
+                    copies[i] = shared;
+                    fresh[i] = shared || tail[i] < 0;
                     need[i] += fresh[i];
                 }
             }
@@ -135,15 +183,37 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
     }
     // the free pages, lowest first, until the demand is met
     int found = 0;
-    for (int p0 = 0; p0 < a.pages && found < demand; p0 += kPlanThreads) {
-        const int p = p0 + t;
-        const bool is = p < a.pages && a.refs[p] == 0;
-        int all;
-        const int at = found + scan_workgroup<kPlanWaves>(is, sums, &all);
-        if (is && at < demand) a.free_list[at] = p;
-        found += all;
+    for (int p0 = 0; p0 < a.pages && found < demand; p0 += kStep) {
+        if (p0) look(p0);
+        uint64_t free[kEach];
+        int mine = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            free[i] = __ballot(ref[i] == 0);
+            mine += __popcll(free[i]);
+        }
+        __syncthreads();
+        if (lane == 0) sums[t / 64] = mine;
+        __syncthreads();
+        int at = found;
+        for (int w = 0; w < kPlanWaves; ++w) {
+            at += w < t / 64 ? sums[w] : 0;
+            found += sums[w];
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int k = at + __popcll(free[i] & ((uint64_t(1) << lane) - 1));
+            if (ref[i] == 0 && k < demand) {
+                if (k < kNear)
+                    near[k] = p0 + own + 64 * i;
+                else
+                    a.free_list[k] = p0 + own + 64 * i;
+            }
+            at += __popcll(free[i]);
+        }
     }
     __syncthreads();  // (the list is read by other threads of this workgroup)
+    const auto free_page = [&](int k) { return k < kNear ? near[k] : a.free_list[k]; };
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int s = t + i * kPlanThreads;
@@ -154,13 +224,13 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
             int32_t* row = a.table + (size_t)s * a.max_pages;
             int at = ((length[i] + page - 1) >> a.log_page) - (fresh[i] ? 1 : 0);
             for (int k = 0; k < need[i]; ++k, ++at) {
-                const int p = a.free_list[base[i] + k];
+                const int p = free_page(base[i] + k);
                 row[at] = p;
                 a.refs[p] = 1;
             }
             if (copies[i]) {
                 r.copy_from = tail[i];
-                r.copy_to = a.free_list[base[i]];
+                r.copy_to = free_page(base[i]);
                 atomicAdd(a.refs + tail[i], -1);
             }
             a.lengths[s] = length[i] + r.tokens;
@@ -170,7 +240,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
     }
 }
 
-// Second launch: a workgroup per (sequence, layer).
+// Second launch: `parts` workgroups per (sequence, layer), which take its tokens
+// in turn; the first also copies the shared page.
 struct MoveArgs {
     uint8_t* pool;
     const int32_t* table;
@@ -181,7 +252,7 @@ struct MoveArgs {
     const CommitRecord* record;
     int64_t kv_stride, layer_stride;
     float k_scale, v_scale;
-    int32_t layers, heads, dim, log_page, max_pages, pages, draft_rows, max_path;
+    int32_t layers, heads, dim, log_page, max_pages, pages, draft_rows, max_path, parts;
 };
 
 constexpr int kMoveThreads = 256;
@@ -205,39 +276,65 @@ __device__ __forceinline__ u32x2 to_fp8(u32x4 x, float scale) {
 
 template <bool FP8>
 __global__ __launch_bounds__(kMoveThreads) void cache_move_kernel(MoveArgs a) {
-    const int s = (int)blockIdx.x / a.layers, layer = (int)blockIdx.x % a.layers, t = (int)threadIdx.x;
+    const int part = (int)blockIdx.x % a.parts, sl = (int)blockIdx.x / a.parts;
+    const int s = sl / a.layers, layer = sl % a.layers, t = (int)threadIdx.x;
     const CommitRecord r = a.record[s];
-    if (r.tokens == 0) return;
+    if (r.tokens <= part) return;
     constexpr int kB = FP8 ? 1 : 2;
     const int page = 1 << a.log_page;
     const size_t plane = (size_t)page * a.dim * kB;         // keys or values of one head in a page
     const size_t side = plane * a.heads, whole = 2 * side;  // of all heads; of both
     auto at = [&](int p) { return a.pool + ((size_t)p * a.layers + layer) * whole; };
-    if (r.copy_from >= 0) {
-        const int bytes = (r.length & (page - 1)) * a.dim * kB;  // a multiple of 16
+    if (part == 0 && r.copy_from >= 0) {
+        const int per = (r.length & (page - 1)) * a.dim * kB / 16, all = per * 2 * a.heads;  // 16-byte pieces
         const uint8_t* from = at(r.copy_from);
         uint8_t* to = at(r.copy_to);
-        const int per = bytes / 16;
-        for (int i = t; i < per * 2 * a.heads; i += kMoveThreads) {
-            const size_t o = (size_t)(i / per) * plane + (size_t)(i % per) * 16;
-            *reinterpret_cast<u32x4*>(to + o) = *reinterpret_cast<const u32x4*>(from + o);
+        constexpr int kAtOnce = 4;
+        for (int i0 = t; i0 < all; i0 += kMoveThreads * kAtOnce) {
+            u32x4 x[kAtOnce];
+            size_t o[kAtOnce];
+#pragma unroll
+            for (int y = 0; y < kAtOnce; ++y) {
+                const int i = i0 + y * kMoveThreads;
+                o[y] = (size_t)(i / per) * plane + (size_t)(i % per) * 16;
+                if (i < all) x[y] = *reinterpret_cast<const u32x4*>(from + o[y]);
+            }
+#pragma unroll
+            for (int y = 0; y < kAtOnce; ++y)
+                if (i0 + y * kMoveThreads < all) *reinterpret_cast<u32x4*>(to + o[y]) = x[y];
         }
     }
-    const int2 rows = row_range(a.start, s, a.draft_rows);
-    const int per = a.dim / 8, all = r.tokens * 2 * a.heads * per;
-    for (int i = t; i < all; i += kMoveThreads) {
-        const int c = i % per, h = i / per % a.heads, side_of = i / per / a.heads % 2, n = i / per / a.heads / 2;
-        const int node = a.path ? a.path[(size_t)s * a.max_path + n] : n;
-        const uint16_t* from = (side_of ? a.v : a.k) + (size_t)layer * a.layer_stride +
-                               (size_t)(rows.x + node) * a.kv_stride + (size_t)h * a.dim + 8 * c;
-        const int pos = r.length + n, p = a.table[(size_t)s * a.max_pages + (pos >> a.log_page)];
-        if (p < 0 || p >= a.pages) continue;
-        uint8_t* to = at(p) + side_of * side + h * plane + ((size_t)(pos & (page - 1)) * a.dim + 8 * c) * kB;
-        const u32x4 x = *reinterpret_cast<const u32x4*>(from);
-        if constexpr (FP8)
-            *reinterpret_cast<u32x2*>(to) = to_fp8(x, side_of ? a.v_scale : a.k_scale);
-        else
-            *reinterpret_cast<u32x4*>(to) = x;
+    const int row0 = row_range(a.start, s, a.draft_rows).x;
+    const int per = a.dim / 8, pieces = 2 * a.heads * per;  // of a token: (keys or values, head, eight channels)
+    const int32_t* const path = a.path ? a.path + (size_t)s * a.max_path : nullptr;
+    const int32_t* const row = a.table + (size_t)s * a.max_pages;
+    for (int i = t; i < pieces; i += kMoveThreads) {
+        const int c = i % per, h = i / per % a.heads, values = i / per / a.heads;
+        const uint16_t* const from = (values ? a.v : a.k) + (size_t)layer * a.layer_stride + (size_t)h * a.dim + 8 * c;
+        const size_t to = values * side + h * plane + 8 * c * kB;
+        constexpr int kAtOnce = 4;  // tokens
+        for (int n0 = part; n0 < r.tokens; n0 += kAtOnce * a.parts) {
+            u32x4 x[kAtOnce];
+            int p[kAtOnce];
+#pragma unroll
+            for (int y = 0; y < kAtOnce; ++y) {
+                const int n = n0 + y * a.parts;
+                if (n >= r.tokens) continue;
+                const int node = path ? path[n] : n;
+                p[y] = row[(r.length + n) >> a.log_page];
+                x[y] = *reinterpret_cast<const u32x4*>(from + (size_t)(row0 + node) * a.kv_stride);
+            }
+#pragma unroll
+            for (int y = 0; y < kAtOnce; ++y) {
+                const int n = n0 + y * a.parts;
+                if (n >= r.tokens || (uint32_t)p[y] >= (uint32_t)a.pages) continue;
+                uint8_t* out = at(p[y]) + to + (size_t)((r.length + n) & (page - 1)) * a.dim * kB;
+                if constexpr (FP8)
+                    *reinterpret_cast<u32x2*>(out) = to_fp8(x[y], values ? a.v_scale : a.k_scale);
+                else
+                    *reinterpret_cast<u32x4*>(out) = x[y];
+            }
+        }
     }
 }
 
@@ -304,9 +401,12 @@ rac_status rac_cache_fork(const rac_cache_config* cfg, const int32_t* parents, c
         return RAC_ERR_ALIGN;
     const ForkArgs a{parents, keep_from, keep_to, table, lengths, refs, cfg->seqs, cfg->max_pages, cfg->pages,
                      log2_of(cfg->page_tokens)};
-    const unsigned grid = (unsigned)((cfg->max_pages + kForkCols - 1) / kForkCols);
-    return launch(reinterpret_cast<const void*>(cache_fork_kernel), grid, kForkThreads, a,
-                  (size_t)cfg->seqs * kForkCols * sizeof(int32_t), stream);
+    // (64-byte pieces of the table's rows where 64 KiB of LDS hold that many columns)
+    const int cols = cfg->seqs <= 1024 ? 16 : 4;
+    const void* kernel = cols == 16 ? reinterpret_cast<const void*>(cache_fork_kernel<16>)
+                                    : reinterpret_cast<const void*>(cache_fork_kernel<4>);
+    return launch(kernel, (unsigned)((cfg->max_pages + cols - 1) / cols), kForkThreads, a,
+                  (size_t)cfg->seqs * cols * sizeof(int32_t), stream);
 }
 
 size_t rac_cache_commit_workspace(const rac_cache_config* cfg) {
@@ -336,13 +436,18 @@ rac_status rac_cache_commit(const rac_cache_config* cfg, void* pool, int32_t* ta
                         cfg->pages, lp, draft_rows, max_path};
     rac_status st = launch(reinterpret_cast<const void*>(cache_plan_kernel), 1, kPlanThreads, plan, 0, stream);
     if (st != RAC_OK) return st;
-    const MoveArgs move{static_cast<uint8_t*>(pool), table, static_cast<const uint16_t*>(k),
+    MoveArgs move{static_cast<uint8_t*>(pool), table, static_cast<const uint16_t*>(k),
                         static_cast<const uint16_t*>(v), draft_start, path, record, kv_stride, layer_stride,
                         cfg->k_scale, cfg->v_scale, cfg->layers, cfg->kv_heads, cfg->head_dim, lp, cfg->max_pages,
-                        cfg->pages, draft_rows, max_path};
+                        cfg->pages, draft_rows, max_path, 0};
+    // (a workgroup per 8 of the longest path's tokens; the grid stays a million at most)
+    const int64_t most = max_path < draft_rows ? max_path : draft_rows, units = (int64_t)cfg->seqs * cfg->layers;
+    int64_t parts = (most + 7) / 8;
+    if (parts * units > (1 << 20)) parts = (1 << 20) / units;
+    move.parts = (int32_t)(parts < 1 ? 1 : parts);
     const void* kernel = cfg->type == RAC_CACHE_FP8 ? reinterpret_cast<const void*>(cache_move_kernel<true>)
                                                     : reinterpret_cast<const void*>(cache_move_kernel<false>);
-    return launch(kernel, (unsigned)(cfg->seqs * cfg->layers), kMoveThreads, move, 0, stream);
+    return launch(kernel, (unsigned)(units * move.parts), kMoveThreads, move, 0, stream);
 }
 
 rac_status rac_cache_copy(const rac_cache_config* cfg, const void* src_pool, const int32_t* src, void* dst_pool,

@@ -1073,13 +1073,13 @@ __global__ __launch_bounds__(64 * kWaves, TM == 1 && (DP == 64 || TYPE == RAC_CA
 
 // Many rows: each wavefront holds 16 TM rows of its own, and all share the
 // keys and values of two tiles at a time in LDS, two such pairs in turn.
-template <int TYPE, int DP, int TM>
-__global__ __launch_bounds__(64 * kWaves, TM * DP <= 256 && DP < 256 ? 2 : 1) void tree_many_kernel(TreeArgs a) {
-    constexpr int M = 16 * TM * kWaves, kTileP = kTile * DP / 8;
+template <int TYPE, int DP, int TM, int W>
+__global__ __launch_bounds__(64 * W, TM * DP <= 256 && DP < 256 ? 2 : 1) void tree_many_kernel(TreeArgs a) {
+    constexpr int M = 16 * TM * W, kBring = 2 * kTile / W, kParts = kTile / kBring, kTileP = kTile * DP / 8;
     __shared__ u32x4 mem[2][2][2][kTileP];  // pair, tile, keys or values
-    __shared__ alignas(4) uint16_t exist[2][2][2];  // the keys of a tile that exist, by halves
-    __shared__ Seen seen[kWaves][16 * TM];
-    __shared__ Reach reach[kWaves];
+    __shared__ uint32_t exist[2][2][kParts];  // the keys of a tile that exist, by parts
+    __shared__ Seen seen[W][16 * TM];
+    __shared__ Reach reach[W];
     __shared__ Work work;
     const uint32_t lane = threadIdx.x & 63u;
     const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
@@ -1098,7 +1098,7 @@ __global__ __launch_bounds__(64 * kWaves, TM * DP <= 256 && DP < 256 ? 2 : 1) vo
         __syncthreads();
         Reach all = reach[0];
 #pragma unroll
-        for (int y = 1; y < kWaves; ++y) {
+        for (int y = 1; y < W; ++y) {
             const Reach z = reach[y];
             all.from_lo = z.from_lo < all.from_lo ? z.from_lo : all.from_lo;
             all.first = z.first < all.first ? z.first : all.first;
@@ -1111,14 +1111,14 @@ __global__ __launch_bounds__(64 * kWaves, TM * DP <= 256 && DP < 256 ? 2 : 1) vo
     const int plain0 = (x.from_hi + kTile - 1) / kTile - ax.ca, draft0 = ax.committed - ax.da;
     const int plain2 = ax.mask ? 1 << 30 : draft0 + (x.first_hi + kTile - 1) / kTile, plain3 = draft0 + x.end_lo / kTile;
     const auto plain = [&](int i) { return i < ax.committed ? i >= plain0 : i >= plain2 && i < plain3; };
-    // (this wavefront brings half a tile of every pair)
-    const int half = 16 * (wv & 1), which = wv >> 1;
-    Load<TYPE, DP, 16> lk, lv;
+    // (this wavefront brings kBring rows of every pair)
+    const int half = kBring * (wv % kParts), which = wv / kParts;
+    Load<TYPE, DP, kBring> lk, lv;
     const float c16 = a.scale2, c8 = a.scale2 * a.k_scale, v8 = a.v_scale;
     bool clean = false;
 again:
     rows.start();
-    Pages<16> pg{};
+    Pages<kBring> pg{};
     uint32_t there = 0;
     auto load = [&](int i) {
         there = exist_of(ax, i, pg, half);
@@ -1126,8 +1126,8 @@ again:
         lk.tile(ax, i, pg, half, false);
         lv.tile(ax, i, pg, half, true);
     };
-    auto fetch = [&](int i) { if (i < ax.committed) pg = pages_of<16>(ax, ax.ca + i, half); };
-    auto pair = [&](int i, u32x4 (&buf)[2][2][kTileP], uint16_t (&ex)[2][2]) {
+    auto fetch = [&](int i) { if (i < ax.committed) pg = pages_of<kBring>(ax, ax.ca + i, half); };
+    auto pair = [&](int i, u32x4 (&buf)[2][2][kTileP], uint32_t (&ex)[2][kParts]) {
         const int mine = i + which;
         if (TYPE != RAC_CACHE_FP8 || mine < ax.committed) {
             lk.put_committed(buf[which][0], ax, there, half, false);
@@ -1140,15 +1140,21 @@ again:
             lk.put_zeros(buf[which][0], half);
             lv.put_zeros(buf[which][1], half);
         }
-        if (lane == 0u) ex[which][wv & 1] = (uint16_t)(there >> half);
+        if (lane == 0u) ex[which][wv % kParts] = there & (low_bits(kBring) << half);
         load(mine + 2);
         fetch(mine + 4);
         __syncthreads();
         if (!busy) return;
         // two tiles at a time: their products and weights overlap
         f32x4 s[2][TM][2];
-        const uint32_t now0 = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t*>(ex[0]));
-        const uint32_t now1 = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t*>(ex[1]));
+        uint32_t now0 = ex[0][0], now1 = ex[1][0];
+#pragma unroll
+        for (int y = 1; y < kParts; ++y) {
+            now0 |= ex[0][y];
+            now1 |= ex[1][y];
+        }
+        now0 = __builtin_amdgcn_readfirstlane(now0);
+        now1 = __builtin_amdgcn_readfirstlane(now1);
         if ((now0 & now1) == ~0u && plain(i) && plain(i + 1)) {
             rows.scores(buf[0][0], s[0]);
             rows.scores(buf[1][0], s[1]);
@@ -1359,13 +1365,13 @@ void choose_form(int rows, Choice& c) {
         c.kernel = reinterpret_cast<const void*>(tree_few_kernel<TYPE, kTwo ? DP : 64, 2>);
     } else if (rows <= 64 || DP == 256) {
         c.m = 64;
-        c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP, 1>);
+        c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP, 1, 4>);
     } else if (rows <= 128 || DP == 128) {
         c.m = 128;
-        c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP < 256 ? DP : 128, 2>);
+        c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP < 256 ? DP : 128, 2, 4>);
     } else {
         c.m = 256;
-        c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, 64, 4>);
+        c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, 64, 4, 4>);
     }
 }
 
