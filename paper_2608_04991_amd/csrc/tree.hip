@@ -1344,6 +1344,7 @@ bool tree_valid(const rac_cache_config* c, const rac_tree_config* t) {
 // Which kernel a call takes, how its work is split, and what that needs.
 struct Choice {
     const void* kernel;
+    int threads;        // a workgroup
     int m, dp;          // query rows a workgroup, channels (padded)
     int target, slots;  // parts wanted, room for partial results
     int64_t grid;
@@ -1355,6 +1356,7 @@ constexpr int kMinChunk = 8;  // key tiles
 template <int TYPE, int DP>
 void choose_form(int rows, Choice& c) {
     c.dp = DP;
+    c.threads = 64 * kWaves;
     // (TM = 2 with 16-bit pages of 128 channels would need more than 256 registers)
     constexpr bool kTwo = DP == 64 || (DP == 128 && TYPE == RAC_CACHE_FP8);
     if (rows <= 16 && DP < 256) {
@@ -1366,12 +1368,13 @@ void choose_form(int rows, Choice& c) {
     } else if (rows <= 64 || DP == 256) {
         c.m = 64;
         c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP, 1, 4>);
-    } else if (rows <= 128 || DP == 128) {
+    } else if (rows < 512 || DP == 64) {
         c.m = 128;
         c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP < 256 ? DP : 128, 2, 4>);
     } else {
         c.m = 256;
-        c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, 64, 4, 4>);
+        c.threads = 512;
+        c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, 128, 2, 8>);
     }
 }
 
@@ -1500,7 +1503,7 @@ rac_status rac_tree_attention(const rac_cache_config* cfg, const rac_tree_config
     };
     rac_status st = RAC_OK;
     if (a.plan) st = launch(reinterpret_cast<const void*>(tree_plan_kernel), 1, kPlanThreads);
-    if (st == RAC_OK) st = launch(c.kernel, c.grid, 64 * kWaves);
+    if (st == RAC_OK) st = launch(c.kernel, c.grid, c.threads);
     if (st != RAC_OK || c.target == 0) return st;
     const int pairs = 256 / c.dp;  // (row, head) pairs a wavefront
     const int64_t units = (int64_t)tree->rows * ((tree->q_heads + pairs - 1) / pairs);
