@@ -78,10 +78,12 @@ size_t rac_cache_pool_bytes(const rac_cache_config* cfg);
  * NaNs included.  One drafted token a sequence and no mask is the ordinary
  * decode step, a chunk of a prompt and no mask its causal attention.
  *
- * Scores, maxima, sums and the accumulated output are fp32; the weights p are
- * rounded to the 16-bit type of the queries before they meet the values (at
- * most 2^-8 (bf16) or 2^-11 (fp16) of each), the sum of the weights takes them
- * unrounded; the output is rounded once. */
+ * Scores, maxima, sums and the accumulated output are fp32; the sum of the
+ * weights takes them unrounded.  Before they meet the values the weights are
+ * rounded to the 16-bit type of the queries (at most 2^-8 (bf16) or 2^-11 (fp16)
+ * of each); where a sequence has few rows a key-value head (max_rows * q_heads /
+ * kv_heads <= 16, and up to 32 in some types) what the rounding left goes in as
+ * well.  The output is rounded once. */
 typedef struct {
     int32_t q_heads;   /* a multiple of kv_heads, at most 64 times as many        */
     int32_t rows;      /* rows of q and out, 0..2^20                              */
@@ -165,6 +167,39 @@ rac_status rac_cache_commit(const rac_cache_config* cfg, void* pool, int32_t* ta
  * is skipped.  One kernel launch. */
 rac_status rac_cache_copy(const rac_cache_config* cfg, const void* src_pool, const int32_t* src, void* dst_pool,
                           const int32_t* dst, int32_t n, rac_stream_t stream);
+
+/* ---- The reference predictor over drafted trees ---------------------------
+ * rac_predictor_step (rac.h) for sequences whose history lies in a paged cache
+ * and whose inputs are nodes of drafted trees.  Sender and receiver run it
+ * level by level: the states of a level are coded against the references that
+ * their parents' reconstructions predict, and become the inputs of the next.
+ * Row r is one input (the reconstruction of a node, or the last committed one):
+ * its key and value go to row slot[r] of draft_k and draft_v, and it sees what
+ * rac_tree_attention says for these drafted rows, mask, window (that of cfg) and
+ * cache; every row should see its own.  The layers and their roundings are
+ * those of rac_predictor_step, except that the turned queries are bf16.  The
+ * accepted path's keys and values are committed with rac_cache_commit.
+ *   cfg       : batch sizes aside, the predictor; tree->rows <= cfg->max_batch
+ *   cache     : one layer, kv_heads = cfg->heads, head_dim 64, not FP16
+ *   tree      : q_heads = cfg->heads, window = cfg->window, scale 0
+ *   h_prev    : bf16 [rows][hidden]           pos  : int32 [rows], the inputs' positions
+ *   q_start   : int32 [seqs + 1], the rows of each sequence
+ *   slot      : int32 [rows]; a row whose slot is none of the draft_rows stores nothing
+ *   draft_k/v : bf16 [draft_rows][model]      draft_start : int32 [seqs + 1]
+ *   ref_out   : bf16 [rows][hidden]           mask : as in rac_tree_tensors, or NULL
+ * Alignments as in rac_predictor_step and rac_tree_attention; the workspace of
+ * rac_predictor_tree_workspace() bytes, 256-byte aligned.  The launches of
+ * rac_predictor_step and rac_tree_attention, the former's attention turning only. */
+size_t rac_predictor_tree_workspace(const rac_predictor_config* cfg, const rac_cache_config* cache,
+                                    const rac_tree_config* tree);
+
+rac_status rac_predictor_tree_step(const rac_predictor_config* cfg, const rac_cache_config* cache,
+                                   const rac_tree_config* tree, const void* weights, const void* pool,
+                                   const int32_t* table, const int32_t* lengths, const int32_t* q_start,
+                                   const int32_t* draft_start, const int32_t* slot, const int32_t* pos,
+                                   const uint64_t* mask, int32_t mask_words, const void* h_prev, void* draft_k,
+                                   void* draft_v, int32_t draft_rows, void* ref_out, void* workspace,
+                                   size_t workspace_bytes, rac_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -23,7 +23,8 @@ import paper_2608_04991_amd as _rac
 __all__ = [
     "RAC_CACHE_BF16", "RAC_CACHE_FP16", "RAC_CACHE_FP8", "CacheConfig", "TreeConfig", "rac_cache_pool_bytes",
     "rac_cache_new", "rac_tree_attention_workspace", "rac_tree_attention", "rac_cache_fork",
-    "rac_cache_commit_workspace", "rac_cache_commit", "rac_cache_copy",
+    "rac_cache_commit_workspace", "rac_cache_commit", "rac_cache_copy", "rac_predictor_tree_workspace",
+    "rac_predictor_tree_step",
 ]
 
 RAC_CACHE_BF16 = 0
@@ -118,7 +119,10 @@ def declare(L) -> None:
             ("rac_cache_commit_workspace", [cp], sz),
             ("rac_cache_commit", [cp, vp, vp, vp, vp, vp, vp, i64, i64, i32, vp, vp, i32, vp, vp, sz, vp],
              ctypes.c_int),
-            ("rac_cache_copy", [cp, vp, vp, vp, vp, i32, vp], ctypes.c_int)):
+            ("rac_cache_copy", [cp, vp, vp, vp, vp, i32, vp], ctypes.c_int),
+            ("rac_predictor_tree_workspace", [ctypes.POINTER(_rac._PredConfig), cp, tp], sz),
+            ("rac_predictor_tree_step", [ctypes.POINTER(_rac._PredConfig), cp, tp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32,
+                                         vp, vp, vp, i32, vp, vp, sz, vp], ctypes.c_int)):
         f = getattr(L, name)
         f.argtypes = args
         f.restype = res
@@ -263,3 +267,29 @@ def rac_cache_copy(cfg: CacheConfig, src_pool, src, dst_pool, dst, n: int | None
         cfg._ref, _pool(cfg, src_pool, "src_pool"), _rac._dev(src, "src", 4, count),
         _pool(cfg, dst_pool, "dst_pool"), _rac._dev(dst, "dst", 4, count), count, _rac._stream(stream)),
         "rac_cache_copy")
+
+
+def rac_predictor_tree_workspace(cfg, cache: CacheConfig, tree: TreeConfig) -> int:
+    return int(_rac.library().rac_predictor_tree_workspace(ctypes.byref(cfg._c()), cache._ref, tree._ref))
+
+
+def rac_predictor_tree_step(cfg, cache: CacheConfig, tree: TreeConfig, weights, pool, table, lengths, q_start,
+                            draft_start, slot, pos, h_prev, draft_k, draft_v, ref_out, workspace, *, mask=None,
+                            stream=None) -> None:
+    """One predictor step over drafted trees (cfg: PredictorConfig): row r's
+    input h_prev[r] (bf16 [rows][hidden]) at position pos[r] stores its key and
+    value in row slot[r] of draft_k and draft_v (bf16 [draft_rows][heads][64]) and
+    predicts ref_out[r]."""
+    dev, R, S, need = _rac._dev, tree.rows, cache.seqs, rac_predictor_tree_workspace(cfg, cache, tree)
+    kp, ks, drafted = _rows(draft_k, "draft_k", 0, cfg.heads, 64)
+    vp, vs, _ = _rows(draft_v, "draft_v", drafted, cfg.heads, 64)
+    if drafted > 1 and (ks != cfg.model or vs != cfg.model):
+        raise ValueError("draft_k and draft_v: expected contiguous rows")
+    words = 0 if mask is None else int(mask.shape[-1])
+    _rac._check(_rac.library().rac_predictor_tree_step(
+        ctypes.byref(cfg._c()), cache._ref, tree._ref, dev(weights, "weights", 1, 0), _pool(cache, pool),
+        dev(table, "table", 4, S * cache.max_pages), dev(lengths, "lengths", 4, S), dev(q_start, "q_start", 4, S + 1),
+        dev(draft_start, "draft_start", 4, S + 1), dev(slot, "slot", 4, R), dev(pos, "pos", 4, R),
+        dev(mask, "mask", 8, R * words), words, dev(h_prev, "h_prev", 2, R * cfg.hidden), kp, vp, drafted,
+        dev(ref_out, "ref_out", 2, R * cfg.hidden), dev(workspace, "workspace", 1, need), need, _rac._stream(stream)),
+        "rac_predictor_tree_step")

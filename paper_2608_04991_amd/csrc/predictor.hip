@@ -34,6 +34,7 @@
 #include <type_traits>
 
 #include "rac.h"
+#include "rac_cache.h"
 
 namespace {
 
@@ -613,6 +614,39 @@ __global__ __launch_bounds__(kW * NW) void pred_attn(AttnArgs a) {
 }
 
 // ---------------------------------------------------------------------------
+// The part of a step's attention that is not tree_attention's: the rotary
+// positions of a row's queries and keys (as pred_attn forms them), the queries as
+// bf16 and the keys and values to the row's place among the drafted ones.  A
+// wavefront per (row, head).
+struct TurnArgs {
+    const float* qkv;    // [B][3m]: q | k | v
+    const int32_t* pos;  // [B]
+    const int32_t* slot; // [B]
+    int32_t m, heads, draft_rows;
+    uint16_t* q;         // [B][m]
+    uint16_t* k;         // [draft_rows][m]
+    uint16_t* v;
+};
+
+__global__ __launch_bounds__(kW) void tree_turn_kernel(TurnArgs a) {
+    const int b = (int)blockIdx.x / a.heads, at = (int)blockIdx.x % a.heads * kHd + (int)threadIdx.x, d = threadIdx.x;
+    const float* row = a.qkv + (size_t)b * 3 * a.m + at;
+    float q = row[0], k = row[a.m];
+    const float v = row[2 * a.m];
+    const int pv = a.pos[b], slot = a.slot[b];
+    const double th = (double)(pv < 0 ? 0 : pv) * kTheta[d >> 1], kTwoPi = 6.283185307179586476925;
+    float sn, cs;
+    sincosf((float)(th - kTwoPi * rint(th / kTwoPi)), &sn, &cs);
+    const float qo = __shfl_xor(q, 1), ko = __shfl_xor(k, 1);
+    q = (d & 1) ? qo * sn + q * cs : q * cs - qo * sn;
+    k = (d & 1) ? ko * sn + k * cs : k * cs - ko * sn;
+    a.q[(size_t)b * a.m + at] = to_bf(q);
+    if (slot < 0 || slot >= a.draft_rows) return;
+    a.k[(size_t)slot * a.m + at] = to_bf(k);
+    a.v[(size_t)slot * a.m + at] = to_bf(v);
+}
+
+// ---------------------------------------------------------------------------
 // Host side
 
 struct PLayout {
@@ -766,6 +800,70 @@ rac_status attention(const rac_predictor_config* cfg, const float* qkv, void* ca
 
 bool al(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// The layers of a step around its attention (q, k, v -> o).
+template <class Attend>
+rac_status step_layers(const rac_predictor_config* cfg, const void* weights, int B, const void* h_prev, void* ref_out,
+                       void* workspace, hipStream_t st, Attend attend) {
+    const PWork Wb = pwork(cfg, B);  // (layout for this batch; fits in the max-batch one)
+    const PLayout L = playout(cfg);
+    const int d = cfg->hidden, m = cfg->model, f = cfg->ffn;
+    const uint8_t* wb = static_cast<const uint8_t*>(weights);
+    auto wt = [&](uint64_t off) { return reinterpret_cast<const uint16_t*>(wb + off); };
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    float* ss = reinterpret_cast<float*>(ws + Wb.ss);  // sums of squares of the residual stream, [B][m / 16 or m / 8]
+    float* h0 = reinterpret_cast<float*>(ws + Wb.h0);
+    float* h1 = reinterpret_cast<float*>(ws + Wb.h1);
+    float* h2 = reinterpret_cast<float*>(ws + Wb.h2);
+    float* qkv = reinterpret_cast<float*>(ws + Wb.qkv);
+    uint16_t* n = reinterpret_cast<uint16_t*>(ws + Wb.n);
+    uint16_t* o = reinterpret_cast<uint16_t*>(ws + Wb.o);
+    uint16_t* gg = reinterpret_cast<uint16_t*>(ws + Wb.gg);
+    const uint16_t* x = static_cast<const uint16_t*>(h_prev);
+    rac_status s;
+    Prod p{};
+    p.M = B;
+    // h0 = x W_in^T
+    p.a = x; p.w = wt(L.w_in); p.N = m; p.K = d; p.out = h0; p.ssout = ss;
+    if ((s = prod_hidden(p, st)) != RAC_OK) return s;
+    // q, k, v; attention
+    p.h = h0; p.ssin = ss; p.gain = wt(L.g1); p.w = wt(L.w_qkv); p.N = 3 * m; p.K = m; p.out = qkv;
+    if ((s = prod_wide<kQkv>(p, n, st)) != RAC_OK) return s;
+    if ((s = attend(qkv, o)) != RAC_OK) return s;
+    // h1 = h0 + o W_o^T
+    p.a = o; p.w = wt(L.w_o); p.N = m; p.K = m; p.resid = h0; p.out = h1;
+    if ((s = prod_hidden(p, st)) != RAC_OK) return s;
+    // SwiGLU; h2 = h1 + g W_down^T
+    p.h = h1; p.gain = wt(L.g2); p.w = wt(L.w_gu); p.N = 2 * f; p.K = m; p.out16 = gg;
+    if ((s = prod_wide<kGate>(p, n, st)) != RAC_OK) return s;
+    p.a = gg; p.w = wt(L.w_down); p.N = m; p.K = f; p.resid = h1; p.out = h2;
+    if ((s = prod_hidden(p, st)) != RAC_OK) return s;
+    // R = x + n3 W_out^T (bf16)
+    p.h = h2; p.gain = wt(L.g3); p.w = wt(L.w_out); p.N = d; p.K = m; p.resid16 = x;
+    p.out16 = static_cast<uint16_t*>(ref_out);
+    return prod_wide<kOut>(p, n, st);
+}
+
+// A step over drafted trees needs the step's scratch, the turned queries and
+// the attention's scratch.
+bool tree_step_valid(const rac_predictor_config* cfg, const rac_cache_config* cache, const rac_tree_config* tree) {
+    return pcfg_valid(cfg) && cache && tree && rac_tree_attention_workspace(cache, tree) > 0 && cache->layers == 1 &&
+           cache->kv_heads == cfg->heads && cache->head_dim == kHd && cache->type != RAC_CACHE_FP16 &&
+           tree->q_heads == cfg->heads && tree->window == cfg->window && tree->scale == 0.0f &&
+           tree->rows <= cfg->max_batch;
+}
+
+struct TWork {
+    uint64_t q, attention, total;
+};
+
+TWork twork(const rac_predictor_config* cfg, const rac_cache_config* cache, const rac_tree_config* tree) {
+    TWork W;
+    W.q = pwork(cfg, cfg->max_batch).total;
+    W.attention = up256(W.q + (uint64_t)tree->rows * (uint64_t)cfg->model * 2u);
+    W.total = W.attention + rac_tree_attention_workspace(cache, tree);
+    return W;
+}
+
 }  // namespace
 
 extern "C" {
@@ -807,44 +905,56 @@ rac_status rac_predictor_step(const rac_predictor_config* cfg, const void* weigh
         return RAC_ERR_ALIGN;
     const PWork W = pwork(cfg, cfg->max_batch);
     if (workspace_bytes < W.total) return RAC_ERR_CAPACITY;
-    const PWork Wb = pwork(cfg, batch);  // (layout for this batch; fits in the max-batch one)
-    const PLayout L = playout(cfg);
-    const int B = batch, d = cfg->hidden, m = cfg->model, f = cfg->ffn;
-    const uint8_t* wb = static_cast<const uint8_t*>(weights);
-    auto wt = [&](uint64_t off) { return reinterpret_cast<const uint16_t*>(wb + off); };
-    uint8_t* ws = static_cast<uint8_t*>(workspace);
-    float* ss = reinterpret_cast<float*>(ws + Wb.ss);  // sums of squares of the residual stream, [B][m / 16 or m / 8]
-    float* h0 = reinterpret_cast<float*>(ws + Wb.h0);
-    float* h1 = reinterpret_cast<float*>(ws + Wb.h1);
-    float* h2 = reinterpret_cast<float*>(ws + Wb.h2);
-    float* qkv = reinterpret_cast<float*>(ws + Wb.qkv);
-    uint16_t* n = reinterpret_cast<uint16_t*>(ws + Wb.n);
-    uint16_t* o = reinterpret_cast<uint16_t*>(ws + Wb.o);
-    uint16_t* gg = reinterpret_cast<uint16_t*>(ws + Wb.gg);
-    const uint16_t* x = static_cast<const uint16_t*>(h_prev);
-    hipStream_t st = stream;
-    rac_status s;
-    Prod p{};
-    p.M = B;
-    // h0 = x W_in^T
-    p.a = x; p.w = wt(L.w_in); p.N = m; p.K = d; p.out = h0; p.ssout = ss;
-    if ((s = prod_hidden(p, st)) != RAC_OK) return s;
-    // q, k, v; attention over the window
-    p.h = h0; p.ssin = ss; p.gain = wt(L.g1); p.w = wt(L.w_qkv); p.N = 3 * m; p.K = m; p.out = qkv;
-    if ((s = prod_wide<kQkv>(p, n, st)) != RAC_OK) return s;
-    if ((s = attention(cfg, qkv, cache, pos, B, o, st)) != RAC_OK) return s;
-    // h1 = h0 + o W_o^T
-    p.a = o; p.w = wt(L.w_o); p.N = m; p.K = m; p.resid = h0; p.out = h1;
-    if ((s = prod_hidden(p, st)) != RAC_OK) return s;
-    // SwiGLU; h2 = h1 + g W_down^T
-    p.h = h1; p.gain = wt(L.g2); p.w = wt(L.w_gu); p.N = 2 * f; p.K = m; p.out16 = gg;
-    if ((s = prod_wide<kGate>(p, n, st)) != RAC_OK) return s;
-    p.a = gg; p.w = wt(L.w_down); p.N = m; p.K = f; p.resid = h1; p.out = h2;
-    if ((s = prod_hidden(p, st)) != RAC_OK) return s;
-    // R = x + n3 W_out^T (bf16)
-    p.h = h2; p.gain = wt(L.g3); p.w = wt(L.w_out); p.N = d; p.K = m; p.resid16 = x;
-    p.out16 = static_cast<uint16_t*>(ref_out);
-    return prod_wide<kOut>(p, n, st);
+    return step_layers(cfg, weights, batch, h_prev, ref_out, workspace, stream, [&](const float* qkv, uint16_t* o) {
+        return attention(cfg, qkv, cache, pos, batch, o, stream);
+    });
+}
+
+size_t rac_predictor_tree_workspace(const rac_predictor_config* cfg, const rac_cache_config* cache,
+                                    const rac_tree_config* tree) {
+    return tree_step_valid(cfg, cache, tree) ? (size_t)twork(cfg, cache, tree).total : 0;
+}
+
+rac_status rac_predictor_tree_step(const rac_predictor_config* cfg, const rac_cache_config* cache,
+                                   const rac_tree_config* tree, const void* weights, const void* pool,
+                                   const int32_t* table, const int32_t* lengths, const int32_t* q_start,
+                                   const int32_t* draft_start, const int32_t* slot, const int32_t* pos,
+                                   const uint64_t* mask, int32_t mask_words, const void* h_prev, void* draft_k,
+                                   void* draft_v, int32_t draft_rows, void* ref_out, void* workspace,
+                                   size_t workspace_bytes, rac_stream_t stream) {
+    if (!tree_step_valid(cfg, cache, tree) || draft_rows < 0 || mask_words < 0) return RAC_ERR_INVALID;
+    const int B = tree->rows, m = cfg->model;
+    if (B == 0) return RAC_OK;
+    if (!weights || !pool || !table || !lengths || !q_start || !draft_start || !slot || !pos || !h_prev || !ref_out ||
+        !workspace || (draft_rows > 0 && (!draft_k || !draft_v)) || (mask != nullptr) != (mask_words > 0))
+        return RAC_ERR_INVALID;
+    if (!al(weights, 256) || !al(pool, 16) || !al(table, 4) || !al(lengths, 4) || !al(q_start, 4) ||
+        !al(draft_start, 4) || !al(slot, 4) || !al(pos, 4) || !al(mask, 8) || !al(h_prev, 16) || !al(draft_k, 16) ||
+        !al(draft_v, 16) || !al(ref_out, 16) || !al(workspace, 256))
+        return RAC_ERR_ALIGN;
+    const TWork W = twork(cfg, cache, tree);
+    if (workspace_bytes < W.total) return RAC_ERR_CAPACITY;
+    uint8_t* const ws = static_cast<uint8_t*>(workspace);
+    return step_layers(cfg, weights, B, h_prev, ref_out, workspace, stream, [&](const float* qkv, uint16_t* o) {
+        TurnArgs turn{qkv, pos, slot, m, cfg->heads, draft_rows, reinterpret_cast<uint16_t*>(ws + W.q),
+                      static_cast<uint16_t*>(draft_k), static_cast<uint16_t*>(draft_v)};
+        void* args[] = {&turn};
+        if (hipLaunchKernel(reinterpret_cast<const void*>(tree_turn_kernel), dim3((unsigned)(B * cfg->heads)), dim3(kW),
+                            args, 0, stream) != hipSuccess)
+            return RAC_ERR_HIP;
+        rac_tree_tensors t{};
+        t.q = turn.q;
+        t.k = draft_rows > 0 ? draft_k : nullptr;
+        t.v = draft_rows > 0 ? draft_v : nullptr;
+        t.q_start = q_start;
+        t.draft_start = draft_start;
+        t.mask = mask;
+        t.mask_words = mask_words;
+        t.out = o;
+        t.q_stride = t.kv_stride = t.out_stride = m;
+        t.draft_rows = draft_rows;
+        return rac_tree_attention(cache, tree, 0, pool, table, lengths, &t, ws + W.attention, W.total - W.attention, stream);
+    });
 }
 
 }  // extern "C"

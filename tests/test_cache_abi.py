@@ -121,6 +121,32 @@ def test_commit_refusals(lib):
     assert call(workspace_bytes=need - 1) == 3
 
 
+def test_predictor_tree_refusals(lib):
+    pred = rac.PredictorConfig(512, 128, 2, 256, 16, 8)
+    cfg, tree = rac.CacheConfig(1, 2, 64, 16, 20, 4, 5), rac.TreeConfig(2, 6, 3, 3, 16)
+    need = rac.rac_predictor_tree_workspace(pred, cfg, tree)
+    assert need > rac.rac_predictor_workspace_bytes(pred)
+    for c, t in ((dataclasses.replace(cfg, layers=2), tree), (dataclasses.replace(cfg, kv_heads=1), tree),
+                 (dataclasses.replace(cfg, head_dim=128), tree), (dataclasses.replace(cfg, type=rac.RAC_CACHE_FP16), tree),
+                 (cfg, dataclasses.replace(tree, q_heads=4)), (cfg, dataclasses.replace(tree, window=0)),
+                 (cfg, dataclasses.replace(tree, rows=9)), (cfg, dataclasses.replace(tree, scale=0.5))):
+        assert rac.rac_predictor_tree_workspace(pred, c, t) == 0
+    names = ("weights", "pool", "table", "lengths", "q_start", "draft_start", "slot", "pos", "mask", "mask_words", "h_prev",
+             "draft_k", "draft_v", "draft_rows", "ref_out", "workspace", "workspace_bytes")
+    ok = dict(zip(names, (P, P, P, P, P, P, P, P, P, 1, P, P, P, 9, P, P, need)))
+
+    def call(tree=tree, **bad):
+        return lib.rac_predictor_tree_step(ctypes.byref(pred._c()), cfg._ref, tree._ref, *{**ok, **bad}.values(), 0)
+
+    for name in names:
+        if name not in ("mask_words", "draft_rows", "workspace_bytes"):
+            assert call(**{name: None}) == 1, name
+            assert call(**{name: P + 2 if name in ("table", "lengths", "q_start", "draft_start", "slot", "pos", "mask")
+                           else P + 8}) == 2, name
+    assert call(draft_rows=-1) == 1 and call(mask_words=0) == 1 and call(workspace_bytes=need - 1) == 3
+    assert call(tree=dataclasses.replace(tree, rows=0), weights=None) == 0
+
+
 class _Fake:
     """A tensor's shape without memory."""
 

@@ -43,6 +43,11 @@ for kind, cfg, tree in json.load(sys.stdin):
         row = c.kv_heads * c.head_dim
         n = rac.rac_cache_commit_workspace(c)
         assert rac.library().rac_cache_commit(c._ref, P, P, P, P, P, P, row, row * tree, tree, P, P, tree, P, P, n, 0) == 0
+    elif kind == "predictor":
+        p, t = rac.PredictorConfig(64 * c.kv_heads * 4, 64 * c.kv_heads, c.kv_heads, 256, 8, 16), rac.TreeConfig(*tree)
+        n = rac.rac_predictor_tree_workspace(p, c, t)
+        assert rac.library().rac_predictor_tree_step(ctypes.byref(p._c()), c._ref, t._ref, P, P, P, P, P, P, P, P, None, 0, P,
+                                                     P, P, 9, P, P, n, 0) == 0
     out.append(rec.recorded().decode())
 print(json.dumps(out))
 """
@@ -83,6 +88,7 @@ def test_every_kernel_is_run_by_a_gpu_test(record):
     # (tests/test_gpu_cache.py has these)
     calls += [("fork", [1, 1, 16, 8, 100, s, 3], None) for s in (4, 4096)]
     calls += [("copy", [1, 1, 16, 8, 100, 1, 1], 5)] + [("commit", [1, 1, 16, 8, 100, 4, 3, k], 9) for k in (0, 2)]
+    calls.append(("predictor", [1, 2, 64, 8, 36, 3, 12], [2, 5, 3, 3, 8]))  # (tests/test_gpu_predictor_tree.py)
     every, *got = record(calls)
     kernels = {k for k, _, _ in every if k.startswith(("tree_", "cache_"))}
     assert len(kernels) > 40
