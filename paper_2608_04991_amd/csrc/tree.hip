@@ -2,6 +2,8 @@
 // the paged cache.  The contract is in include/rac_cache.h.
 #include <math.h>
 
+#include <type_traits>
+
 #include "cache_common.h"
 
 namespace {
@@ -28,7 +30,7 @@ struct TreeArgs {
     int32_t rows, max_rows, draft_rows, max_draft, window, mask_words;
     float scale2;   // of the scores, times log2(e)
     float k_scale, v_scale;
-    int32_t target;     // parts wanted, a power of two (0: sequences are not split)
+    int32_t target;     // parts wanted (0: sequences are not split)
     int32_t min_chunk;  // fewest key tiles of a part
     float* parts;       // [slots] partial results
     int32_t slots;
@@ -205,13 +207,48 @@ __device__ __forceinline__ Cut cut_of(const TreeArgs& a, const Seq& q, int most)
     return Cut{(q.m * a.group + a.m - 1) / a.m, keys > most ? (keys + most - 1) / most : 1};
 }
 
-// Parts of at most this many key tiles, so that all parts together are about
-// a.target and of like size whatever the lengths.  total: (tiles of rows) x
-// (tiles of keys) of all sequences, for one head.
-__device__ __forceinline__ int chunk_tiles(const TreeArgs& a, int64_t total) {
+// Sums over the lanes up to this one, by moves between neighbouring lanes.
+template <class T>
+__device__ __forceinline__ T scan_wave(T v) {
+    const auto from = [](T x, auto ctrl, auto rows) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value,
+                                                                 decltype(rows)::value, 0xF, false));
+    };
+    using std::integral_constant;
+    using all = integral_constant<int, 0xF>;
+    v = v + from(v, integral_constant<int, 0x111>{}, all{});                          // row_shr:1
+    v = v + from(v, integral_constant<int, 0x112>{}, all{});
+    v = v + from(v, integral_constant<int, 0x114>{}, all{});
+    v = v + from(v, integral_constant<int, 0x118>{}, all{});
+    v = v + from(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});  // row_bcast:15
+    return v + from(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});  // row_bcast:31
+}
+
+// Parts of at most this many key tiles: all parts of all sequences together just
+// fill the workgroups that the device holds at once (a.target), or twice that
+// where the sequences alone take nearly half of them and rounding their parts up
+// would leave many idle, and are of like size whatever the lengths.  sum(f): the
+// sum over all sequences of f(tiles of rows, tiles of keys).  The first size would
+// give as many parts if none were rounded up; a second round of a few workgroups
+// costs more than parts a little longer (us, with the first size alone and now:
+// 32 x 16k tokens 236, 216; 32 rows each 174, 143; trees of 64 nodes 110, 94;
+// 64 x 4k tokens 69, 66).
+template <class Sum>
+__device__ __forceinline__ int chunk_tiles(const TreeArgs& a, Sum sum) {
     if (a.target == 0) return 1 << 30;
-    const int64_t c = (total * a.heads + a.target - 1) >> (31 - __builtin_clz(a.target));
-    return c < a.min_chunk ? a.min_chunk : (int)(c < (1 << 30) ? c : (1 << 30));
+    const float heads = (float)a.heads;
+    const float units = heads * sum([](float t, float) { return t; });
+    const float work = heads * sum([](float t, float k) { return t * k; });
+    const float full = (float)a.target, want = a.m <= 32 && units > 0.4f * full && units < full ? 2.0f * full : full;
+    // (the margin keeps sums in fp32 from asking for more than a.slots)
+    float most = __builtin_fminf(work / want * 1.0001f + 1.0f, 1e9f);
+    for (int i = 0; i < 3 && units < want; ++i) {
+        const float whole = __builtin_floorf(most);
+        const float parts = heads * sum([whole](float t, float k) { return t * __builtin_ceilf(k / whole); });
+        if (parts <= want) break;
+        most = __builtin_fminf(most * (parts / want) + 0.5f, 1e9f);
+    }
+    return (int)most < a.min_chunk ? a.min_chunk : (int)most;
 }
 
 // Up to 64 sequences need no launch ahead: a lane a sequence, each wavefront
@@ -227,19 +264,25 @@ struct LaneSeq {
 __device__ __forceinline__ LaneSeq lane_seq(const TreeArgs& a) {
     const int lane = (int)threadIdx.x & 63;
     LaneSeq r{Seq{0, 0, 0, 0, 0}, Cut{0, 1}, 0, 0};
-    int64_t total = 0;
+    float t = 0.0f, k = 0.0f;
     if (lane < a.seqs) {
         r.q = seq_of(a, lane);
-        total = (int64_t)cut_of(a, r.q, 1 << 30).tiles * key_tiles(a, r.q);
+        t = (float)cut_of(a, r.q, 1 << 30).tiles;
+        k = (float)key_tiles(a, r.q);
     }
-    int most = 1 << 30;
-    if (a.target) {
-        for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
-        most = chunk_tiles(a, total);
-    }
+    const int most = chunk_tiles(a, [&](auto f) {
+        const float all = scan_wave(f(t, k));
+        return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, all), 63));
+    });
     if (lane < a.seqs) r.c = cut_of(a, r.q, most);
     const int units = r.c.tiles * r.c.chunks * a.heads;
-    // the sequences with the longest parts first: what starts last ends last
+    if (a.m <= 32) {
+        const int split = r.c.chunks > 1 ? units : 0;
+        r.base = scan_wave(units) - units;
+        r.slot = scan_wave(split) - split;
+        return r;
+    }
+    // (many rows) the sequences with the longest parts first: what starts last ends last
     const int keys = lane < a.seqs ? (key_tiles(a, r.q) + r.c.chunks - 1) / r.c.chunks : -1;
     for (int j = 0; j < a.seqs; ++j) {
         const int k = __builtin_amdgcn_readlane(keys, j), u = __builtin_amdgcn_readlane(units, j);
@@ -305,25 +348,30 @@ constexpr int kPlanThreads = 1024;
 __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreeArgs a) {
     constexpr int kPer = 4;  // sequences a thread (4096 / 1024)
     __shared__ int sums[kPlanThreads / 64];
-    __shared__ int64_t totals[kPlanThreads / 64];
+    __shared__ float totals[kPlanThreads / 64];
     const int t = (int)threadIdx.x;
     Seq q[kPer];
-    int64_t total = 0;
+    float tiles[kPer], keys[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int s = t + i * kPlanThreads;
         q[i] = Seq{0, 0, 0, 0, 0};
+        tiles[i] = keys[i] = 0.0f;
         if (s < a.seqs) {
             q[i] = seq_of(a, s);
-            total += (int64_t)cut_of(a, q[i], 1 << 30).tiles * key_tiles(a, q[i]);
+            tiles[i] = (float)cut_of(a, q[i], 1 << 30).tiles;
+            keys[i] = (float)key_tiles(a, q[i]);
         }
     }
-    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
-    if ((t & 63) == 0) totals[t / 64] = total;
-    __syncthreads();
-    total = 0;
-    for (int i = 0; i < kPlanThreads / 64; ++i) total += totals[i];
-    const int most = chunk_tiles(a, total);
+    const int most = chunk_tiles(a, [&](auto f) {
+        const float all = scan_wave((f(tiles[0], keys[0]) + f(tiles[1], keys[1])) + (f(tiles[2], keys[2]) + f(tiles[3], keys[3])));
+        __syncthreads();
+        if ((t & 63) == 63) totals[t / 64] = all;
+        __syncthreads();
+        float total = 0.0f;
+        for (int i = 0; i < kPlanThreads / 64; ++i) total = total + totals[i];
+        return total;
+    });
     int base = 0, slot = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -952,7 +1000,7 @@ __device__ __forceinline__ Reach take_rows(const TreeArgs& a, const Work& w, int
 // turn, each through LDS of its own (first the keys, then, in the same place,
 // the values), without a barrier until they join.
 template <int TYPE, int DP, int TM>
-__global__ __launch_bounds__(64 * kWaves, TM == 1 && (DP == 64 || TYPE == RAC_CACHE_FP8) ? 3 : 2) void tree_few_kernel(TreeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, TM == 1 && DP == 64 ? 4 : TM == 1 && TYPE == RAC_CACHE_FP8 ? 3 : 2) void tree_few_kernel(TreeArgs a) {
     constexpr int M = 16 * TM, kTileP = kTile * DP / 8, kPad = DP + 4;
     constexpr int kStage = kTileP * 16 * kWaves, kJoin = kWaves * 16 * kPad * 4;
     __shared__ alignas(16) uint8_t mem[kStage > kJoin ? kStage : kJoin];
@@ -1375,14 +1423,21 @@ struct Choice {
 
 constexpr int kMinChunk = 8;  // key tiles
 
+// rows: the most of a sequence and a key-value head; mean: of all sequences.
 template <int TYPE, int DP>
-void choose_form(int rows, Choice& c) {
+void choose_form(int rows, int mean, Choice& c) {
     c.dp = DP;
     c.threads = 64 * kWaves;
+    // (workgroups of the form that the 256 compute units hold at once)
+    c.target = DP == 256 ? 256 : 512;
     // (TM = 2 with 16-bit pages of 128 channels would need more than 256 registers)
     constexpr bool kTwo = DP == 64 || (DP == 128 && TYPE == RAC_CACHE_FP8);
-    if (rows <= 16 && DP < 256) {
+    // (most sequences with 16 rows or fewer: two tiles of 16 for the others are
+    // faster, 64 sequences of 12 to 20 rows 69 us, 89 with one of 32; where all have
+    // 32 it is the other way round, 177 and 268)
+    if ((rows <= 16 || (rows <= 32 && mean <= 17)) && DP < 256) {
         c.m = 16;
+        c.target = DP == 64 ? 1024 : TYPE == RAC_CACHE_FP8 ? 768 : 512;
         c.kernel = reinterpret_cast<const void*>(tree_few_kernel<TYPE, DP < 256 ? DP : 128, 1>);
     } else if (rows <= 32 && kTwo) {
         c.m = 32;
@@ -1415,13 +1470,13 @@ const void* join_of(int dp, bool split) {
 }
 
 template <int TYPE>
-void choose_type(int dim, int rows, Choice& c) {
+void choose_type(int dim, int rows, int mean, Choice& c) {
     if (dim <= 64)
-        choose_form<TYPE, 64>(rows, c);
+        choose_form<TYPE, 64>(rows, mean, c);
     else if (dim <= 128)
-        choose_form<TYPE, 128>(rows, c);
+        choose_form<TYPE, 128>(rows, mean, c);
     else
-        choose_form<TYPE, 256>(rows, c);
+        choose_form<TYPE, 256>(rows, mean, c);
 }
 
 Choice choose(const rac_cache_config* cfg, const rac_tree_config* tree) {
@@ -1429,24 +1484,25 @@ Choice choose(const rac_cache_config* cfg, const rac_tree_config* tree) {
     const int group = tree->q_heads / cfg->kv_heads;
     const int64_t of_seq = tree->max_rows < tree->rows ? tree->max_rows : tree->rows;
     const int rows = (int)(of_seq * group);
+    const int64_t seqs = cfg->seqs < tree->rows ? cfg->seqs : tree->rows > 0 ? tree->rows : 1;
+    const int mean = (int)((int64_t)tree->rows * group / seqs);
     if (cfg->type == RAC_CACHE_BF16)
-        choose_type<RAC_CACHE_BF16>(cfg->head_dim, rows, c);
+        choose_type<RAC_CACHE_BF16>(cfg->head_dim, rows, mean, c);
     else if (cfg->type == RAC_CACHE_FP16)
-        choose_type<RAC_CACHE_FP16>(cfg->head_dim, rows, c);
+        choose_type<RAC_CACHE_FP16>(cfg->head_dim, rows, mean, c);
     else
-        choose_type<RAC_CACHE_FP8>(cfg->head_dim, rows, c);
+        choose_type<RAC_CACHE_FP8>(cfg->head_dim, rows, mean, c);
     // the longest key axis there can be
     int64_t keys = (int64_t)cfg->max_pages * cfg->page_tokens;
     if (tree->window > 0 && tree->window < keys) keys = tree->window + kTile;
     const int64_t most = (keys + kTile - 1) / kTile + ((int64_t)tree->max_draft + kTile - 1) / kTile;
     const int64_t row_tiles = ((int64_t)tree->rows * group + c.m - 1) / c.m;
-    c.target = most > kMinChunk && row_tiles * cfg->kv_heads < 512 ? 512 : 0;
+    if (most <= kMinChunk || row_tiles * cfg->kv_heads >= c.target) c.target = 0;
     // (a sequence that is split has fewer than twice its keys over the part's size parts)
-    c.slots = 2 * c.target;
+    c.slots = 2 * c.target * (c.m <= 32 ? 2 : 1);
     c.plan = ((uint64_t)c.slots * (uint64_t)c.m * (uint64_t)(c.dp + 2) * 4u + 255u) & ~uint64_t(255);
     c.bytes = c.plan + (uint64_t)(cfg->seqs + 1) * sizeof(SeqPlan);
-    const int64_t seqs = cfg->seqs < tree->rows ? cfg->seqs : tree->rows;
-    c.grid = c.target + (row_tiles + seqs) * cfg->kv_heads;
+    c.grid = c.slots / 2 + (row_tiles + seqs) * cfg->kv_heads;
     return c;
 }
 
