@@ -8,9 +8,9 @@
 
 namespace {
 
-// Where the workgroups of a sequence, and its partial results, begin.
-struct SeqPlan {
-    int32_t base, slot, chunks;
+// Where the workgroups of a sequence, and its partial results, begin, and what it brings.
+struct alignas(16) SeqPlan {
+    int32_t base, slot, chunks, q0, m, d0, n, length;
 };
 
 struct TreeArgs {
@@ -312,14 +312,26 @@ __device__ __forceinline__ int last_at_most(int n, int x, At at) {
 __device__ __forceinline__ bool find_work(const TreeArgs& a, int block, Work& w) {
     int i, tiles;
     if (a.plan) {
-        if (block >= a.plan[a.seqs].base) return false;
-        w.seq = __builtin_amdgcn_readfirstlane(last_at_most(a.seqs, block, [&](int s) { return a.plan[s].base; }));
-        const SeqPlan p = a.plan[w.seq];
-        w.q = seq_of(a, w.seq);
+        // 64 records at a time, the last step with all that a record holds
+        const int lane = (int)threadIdx.x & 63, all = a.plan[a.seqs].base;
+        int lo = 0, n = a.seqs;
+        while (n > 64) {
+            const int step = (n + 63) / 64;
+            const int k = __popcll(__ballot(lane * step < n && a.plan[lo + lane * step].base <= block)) - 1;
+            lo += k * step;
+            n = n - k * step < step ? n - k * step : step;
+        }
+        SeqPlan p{};
+        if (lane < n) p = a.plan[lo + lane];
+        const int at = __popcll(__ballot(lane < n && p.base <= block)) - 1;
+        if (block >= all || at < 0) return false;
+        const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+        w.seq = __builtin_amdgcn_readfirstlane(lo + at);
+        w.q = Seq{of(p.q0), of(p.m), of(p.d0), of(p.n), of(p.length)};
         tiles = cut_of(a, w.q, 1 << 30).tiles;
-        w.chunks = p.chunks;
-        i = block - p.base;
-        w.slot = p.slot + i;
+        w.chunks = of(p.chunks);
+        i = block - of(p.base);
+        w.slot = of(p.slot) + i;
     } else {
         const LaneSeq l = lane_seq(a);
         const uint64_t mine = __ballot(block >= l.base && block < l.base + l.c.tiles * l.c.chunks * a.heads);
@@ -382,11 +394,11 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreeArgs a) {
         int all_units, all_split;
         const int b = base + scan_workgroup<kPlanThreads / 64>(units, sums, &all_units);
         const int l = slot + scan_workgroup<kPlanThreads / 64>(split, sums, &all_split);
-        if (s <= a.seqs) a.plan[s] = SeqPlan{b, l, c.chunks};
+        if (s <= a.seqs) a.plan[s] = SeqPlan{b, l, c.chunks, q[i].q0, q[i].m, q[i].d0, q[i].n, q[i].length};
         base += all_units;
         slot += all_split;
     }
-    if (t == 0 && a.seqs == kPer * kPlanThreads) a.plan[a.seqs] = SeqPlan{base, slot, 1};
+    if (t == 0 && a.seqs == kPer * kPlanThreads) a.plan[a.seqs] = SeqPlan{base, slot, 1, 0, 0, 0, 0, 0};
 }
 
 // ---------------------------------------------------------------------------
@@ -1303,8 +1315,8 @@ again:
 }
 
 // Joins the parts of the sequences that were split.  DP / 4 lanes take a (row,
-// query head) pair, four channels each; with SPLIT (few pairs, so many parts)
-// a workgroup's wavefronts share the parts of the same pairs.
+// query head) pair, four channels each.  A workgroup takes a row; with SPLIT (few
+// pairs, so many parts) a few pairs, and its wavefronts share their parts.
 template <int TYPE, int DP, bool SPLIT>
 __global__ __launch_bounds__(64 * kWaves) void tree_join_kernel(TreeArgs a) {
     constexpr int kLanes = DP / 4, kPairs = 64 / kLanes, kAtOnce = 8;
@@ -1312,17 +1324,17 @@ __global__ __launch_bounds__(64 * kWaves) void tree_join_kernel(TreeArgs a) {
     __shared__ float wm[SPLIT ? kWaves : 1][kPairs], wl[SPLIT ? kWaves : 1][kPairs];
     const int lane = (int)threadIdx.x & 63, wv = (int)threadIdx.x / 64, hq = a.heads * a.group;
     const int groups = (hq + kPairs - 1) / kPairs;  // of the heads of a row
-    const int unit = SPLIT ? (int)blockIdx.x : (int)blockIdx.x * kWaves + wv;
-    const int row = __builtin_amdgcn_readfirstlane(unit / groups);
+    const int row = SPLIT ? (int)blockIdx.x / groups : (int)blockIdx.x;
     if (row >= a.rows) return;
     Seq q;
     int chunks, slot;
     if (a.plan) {
         const int s = __builtin_amdgcn_readfirstlane(last_at_most(a.seqs, row, [&](int i) { return i ? a.q_start[i] : -1; }));
-        chunks = a.plan[s].chunks;
+        const SeqPlan p = a.plan[s];
+        chunks = p.chunks;
         if (chunks == 1) return;
-        q = seq_of(a, s);
-        slot = a.plan[s].slot;
+        q = Seq{p.q0, p.m, p.d0, p.n, p.length};
+        slot = p.slot;
     } else {
         const LaneSeq l = lane_seq(a);
         const uint64_t has = __ballot(row >= l.q.q0 && row < l.q.q0 + l.q.m);
@@ -1336,70 +1348,72 @@ __global__ __launch_bounds__(64 * kWaves) void tree_join_kernel(TreeArgs a) {
     }
     const int tiles = cut_of(a, q, 1 << 30).tiles;
     if (row < q.q0 || row >= q.q0 + q.m || (uint32_t)(slot + tiles * chunks * a.heads) > (uint32_t)a.slots) return;
-    const int pair = lane / kLanes, h = unit % groups * kPairs + pair, c4 = lane % kLanes;
-    const int hc = h < hq ? h : hq - 1, r = (row - q.q0) * a.group + hc % a.group;
-    const int in = r % a.m;
+    const int pair = lane / kLanes, c4 = lane % kLanes;
     // parts of a row tile are a.heads slots apart
-    const size_t stride = (size_t)a.m * (DP + 2);
-    const float* const base = a.parts + ((size_t)slot + (size_t)((tiles - 1 - r / a.m) * chunks) * a.heads + hc / a.group) * stride;
-    const size_t step = stride * a.heads;
-    float top = -INFINITY, l = 0.0f;
-    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int first = SPLIT ? wv : 0, by = SPLIT ? kWaves : 1;
-    for (int c = first; c < chunks; c += by * kAtOnce) {
-        f32x4 x[kAtOnce];
-        float m[kAtOnce], s[kAtOnce], now = top;
+    const size_t stride = (size_t)a.m * (DP + 2), step = stride * a.heads;
+    for (int g = SPLIT ? (int)blockIdx.x % groups : wv; g < groups; g += SPLIT ? groups : kWaves) {
+        const int h = g * kPairs + pair;
+        const int hc = h < hq ? h : hq - 1, r = (row - q.q0) * a.group + hc % a.group;
+        const int in = r % a.m;
+        const float* const base = a.parts + ((size_t)slot + (size_t)((tiles - 1 - r / a.m) * chunks) * a.heads + hc / a.group) * stride;
+        float top = -INFINITY, l = 0.0f;
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        const int first = SPLIT ? wv : 0, by = SPLIT ? kWaves : 1;
+        for (int c = first; c < chunks; c += by * kAtOnce) {
+            f32x4 x[kAtOnce];
+            float m[kAtOnce], s[kAtOnce], now = top;
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const bool is = c + i * by < chunks;
-            const float* p = base + (size_t)(is ? c + i * by : c) * step;
-            x[i] = *reinterpret_cast<const f32x4*>(p + (size_t)in * DP + 4 * c4);
-            m[i] = is ? p[a.m * DP + in] : -INFINITY;
-            s[i] = p[a.m * DP + a.m + in];
+            for (int i = 0; i < kAtOnce; ++i) {
+                const bool is = c + i * by < chunks;
+                const float* p = base + (size_t)(is ? c + i * by : c) * step;
+                x[i] = *reinterpret_cast<const f32x4*>(p + (size_t)in * DP + 4 * c4);
+                m[i] = is ? p[a.m * DP + in] : -INFINITY;
+                s[i] = p[a.m * DP + a.m + in];
+            }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) now = __builtin_fmaxf(now, m[i]);
+            const float ref = now == -INFINITY ? 0.0f : now, keep = __builtin_amdgcn_exp2f(top - ref);
+            l = l * keep;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = v[i] * keep;
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                if (c + i * by >= chunks) break;
+                const float f = __builtin_amdgcn_exp2f(m[i] - ref);
+                l = __builtin_fmaf(s[i], f, l);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) v[y] = __builtin_fmaf(x[i][y], f, v[y]);
+            }
+            top = now;
         }
+        if constexpr (SPLIT) {
+            sums[wv][lane] = v;
+            if (c4 == 0) {
+                wm[wv][pair] = top;
+                wl[wv][pair] = l;
+            }
+            __syncthreads();
+            if (wv != 0) return;
+            top = wm[0][pair];
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) now = __builtin_fmaxf(now, m[i]);
-        const float ref = now == -INFINITY ? 0.0f : now, keep = __builtin_amdgcn_exp2f(top - ref);
-        l = l * keep;
+            for (int x = 1; x < kWaves; ++x) top = __builtin_fmaxf(top, wm[x][pair]);
+            v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            l = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = v[i] * keep;
+            for (int x = 0; x < kWaves; ++x) {
+                const float f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(wm[x][pair] - top);
+                l = __builtin_fmaf(wl[x][pair], f, l);
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            if (c + i * by >= chunks) break;
-            const float f = __builtin_amdgcn_exp2f(m[i] - ref);
-            l = __builtin_fmaf(s[i], f, l);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) v[y] = __builtin_fmaf(x[i][y], f, v[y]);
+                for (int y = 0; y < 4; ++y) v[y] = __builtin_fmaf(sums[x][lane][y], f, v[y]);
+            }
         }
-        top = now;
+        if (h >= hq) continue;
+        const bool none = l == 0.0f;
+        if (4 * c4 < a.dim)
+            *reinterpret_cast<u32x2*>(a.out + (int64_t)row * a.out_stride + (int64_t)h * a.dim + 4 * c4) =
+                none ? u32x2{0u, 0u} : u32x2{pack2<TYPE>(v[0] / l, v[1] / l), pack2<TYPE>(v[2] / l, v[3] / l)};
+        if (c4 == 0 && a.lse) a.lse[(size_t)row * hq + h] = lse_of(top, l);
     }
-    if constexpr (SPLIT) {
-        sums[wv][lane] = v;
-        if (c4 == 0) {
-            wm[wv][pair] = top;
-            wl[wv][pair] = l;
-        }
-        __syncthreads();
-        if (wv != 0) return;
-        top = wm[0][pair];
-#pragma unroll
-        for (int x = 1; x < kWaves; ++x) top = __builtin_fmaxf(top, wm[x][pair]);
-        v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        l = 0.0f;
-#pragma unroll
-        for (int x = 0; x < kWaves; ++x) {
-            const float f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(wm[x][pair] - top);
-            l = __builtin_fmaf(wl[x][pair], f, l);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) v[y] = __builtin_fmaf(sums[x][lane][y], f, v[y]);
-        }
-    }
-    if (h >= hq) return;
-    const bool none = l == 0.0f;
-    if (4 * c4 < a.dim)
-        *reinterpret_cast<u32x2*>(a.out + (int64_t)row * a.out_stride + (int64_t)h * a.dim + 4 * c4) =
-            none ? u32x2{0u, 0u} : u32x2{pack2<TYPE>(v[0] / l, v[1] / l), pack2<TYPE>(v[2] / l, v[3] / l)};
-    if (c4 == 0 && a.lse) a.lse[(size_t)row * hq + h] = lse_of(top, l);
 }
 
 // ---------------------------------------------------------------------------
@@ -1497,12 +1511,21 @@ Choice choose(const rac_cache_config* cfg, const rac_tree_config* tree) {
     if (tree->window > 0 && tree->window < keys) keys = tree->window + kTile;
     const int64_t most = (keys + kTile - 1) / kTile + ((int64_t)tree->max_draft + kTile - 1) / kTile;
     const int64_t row_tiles = ((int64_t)tree->rows * group + c.m - 1) / c.m;
-    if (most <= kMinChunk || row_tiles * cfg->kv_heads >= c.target) c.target = 0;
+    // (no parts, and no join, where there is nothing to cut, where the sequences
+    // fill the device by themselves, or nearly do and none is long)
+    const int64_t units = row_tiles * cfg->kv_heads;
+    if (most <= kMinChunk || units >= c.target || (2 * units >= c.target && most <= 8 * kMinChunk)) c.target = 0;
     // (a sequence that is split has fewer than twice its keys over the part's size parts)
     c.slots = 2 * c.target * (c.m <= 32 ? 2 : 1);
     c.plan = ((uint64_t)c.slots * (uint64_t)c.m * (uint64_t)(c.dp + 2) * 4u + 255u) & ~uint64_t(255);
     c.bytes = c.plan + (uint64_t)(cfg->seqs + 1) * sizeof(SeqPlan);
-    c.grid = c.slots / 2 + (row_tiles + seqs) * cfg->kv_heads;
+    // (see chunk_tiles: at most the workgroups it wants, and one more a sequence, head and tile of rows)
+    const int64_t most_units = (row_tiles + seqs) * cfg->kv_heads, t = c.target;
+    c.grid = t + most_units;
+    if (c.m <= 32) {
+        const int64_t twice = 2 * t + (most_units < t ? most_units : t);
+        c.grid = twice > c.grid ? twice : c.grid;
+    }
     return c;
 }
 
@@ -1587,7 +1610,7 @@ rac_status rac_tree_attention(const rac_cache_config* cfg, const rac_tree_config
     const int64_t units = (int64_t)tree->rows * ((tree->q_heads + pairs - 1) / pairs);
     const bool split = units < kSplitJoin;
     const void* join = cfg->type == RAC_CACHE_FP16 ? join_of<RAC_CACHE_FP16>(c.dp, split) : join_of<RAC_CACHE_BF16>(c.dp, split);
-    return launch(join, split ? units : (units + kWaves - 1) / kWaves, 64 * kWaves);
+    return launch(join, split ? units : tree->rows, 64 * kWaves);
 }
 
 }  // extern "C"
