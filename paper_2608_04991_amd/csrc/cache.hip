@@ -13,6 +13,9 @@ namespace {
 // whole columns can read all of them before it writes any, in place and in one
 // launch: COLS columns of all sequences through LDS.  Lengths move within the
 // first workgroup alone.
+//
+// Bound by latency: entries, parents and bounds are dependent reads.  8 sequences of
+// up to 250 tokens 2.6 us; 256 of up to 32000 (6 MB of table and counts) 10.6.
 struct ForkArgs {
     const int32_t* parents;
     const int32_t* from;
@@ -92,6 +95,11 @@ __global__ __launch_bounds__(kForkThreads) void cache_fork_kernel(ForkArgs a) {
 // sequence takes, which pages are free (a scan of the counts that ends when
 // the demand is met), and the new table entries, counts and lengths.  The
 // second launch moves the data by the records this one leaves.
+//
+// Bound by the latency of dependent reads (lengths, table, count, path) and of the
+// sums over the workgroup: 7 us for 8 sequences, 12 for 128 with paths of 40 nodes.  Pages and
+// the order of the sequences are those of a serial loop, so one workgroup has to
+// see all of it.
 struct CommitRecord {
     int32_t length;      // before the call
     int32_t tokens;      // appended
@@ -241,7 +249,9 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
 }
 
 // Second launch: `parts` workgroups per (sequence, layer), which take its tokens
-// in turn; the first also copies the shared page.
+// in turn; the first also copies the shared page.  Bound by bytes where there are
+// many: 128 sequences, 8 layers of 8 heads of 128 channels to 8 bits, 64 MB with
+// the copied pages, 15.6 us (4.1 TB/s); 8 sequences of one layer 4.3 us.
 struct MoveArgs {
     uint8_t* pool;
     const int32_t* table;
@@ -339,7 +349,9 @@ __global__ __launch_bounds__(kMoveThreads) void cache_move_kernel(MoveArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Copy: a workgroup per kCopyBytes of a page.
+// Copy: a workgroup per kCopyBytes of a page, four loads of 16 bytes a thread on
+// their way before the first store.  Bound by bytes: 900 pages of 1 MiB, read and
+// written, in 368 us (5.1 TB/s; a plain copy of 4 GB reaches 4.9); five of 32 KiB 3.0 us.
 constexpr int kCopyThreads = 256;
 constexpr int kCopyBytes = kCopyThreads * 16 * 4;
 

@@ -252,9 +252,10 @@ __device__ __forceinline__ int chunk_tiles(const TreeArgs& a, Sum sum) {
 }
 
 // Up to 64 sequences need no launch ahead: a lane a sequence, each wavefront
-// finds the cuts by itself.  (A launch ahead of 8 sequences takes longer than
-// that; beyond 64 each wavefront would read all sequences again and again: 200
-// sequences in a window of 1000 took 117 us instead of the 53 with a plan.)
+// finds the cuts by itself.  That is the faster side up to the last size that a
+// wavefront's lanes can hold (us, so and with tree_plan_kernel ahead: 8 drafted
+// trees of up to 12 tokens 10.9, 13.3; one token of 8k 16.2, 19.3; 32 x 16k tokens
+// 217, 221; 64 x 4k tokens 72, 75).
 struct LaneSeq {
     Seq q;
     Cut c;
@@ -354,7 +355,8 @@ __device__ __forceinline__ bool find_work(const TreeArgs& a, int block, Work& w)
     return w.row_tile >= 0 && (w.chunks == 1 || (uint32_t)w.slot < (uint32_t)a.slots);
 }
 
-// The plan of more sequences: one workgroup.
+// The plan of more sequences: one workgroup, four sequences a thread.  Bound by
+// the latency of its few dependent reads and sums: 5.0 us for 200 sequences.
 constexpr int kPlanThreads = 1024;
 
 __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreeArgs a) {
@@ -433,8 +435,8 @@ __device__ __forceinline__ u32x2 read_column(const u32x4* tile, uint32_t lane, u
 // FINE: a weight goes to the matrix cores as two 16-bit numbers, its rounding
 // and the rest, so that only the output's rounding is left: with one, the two
 // roundings together are 1.4 times the output's.  Where few rows wait for memory
-// the second product costs next to nothing (32 x 16k tokens 241 us, 239 without;
-// 131k in 8 bits 59.7 and 59.3).
+// the second product costs nothing (32 x 16k tokens 217 us with it and without,
+// one sequence of 8k 16).
 template <int TYPE, int DP, int TM, bool FINE>
 struct Rows {
     static constexpr int kP = FINE ? 2 : 1;
@@ -573,7 +575,7 @@ struct Rows {
     // Two tiles, for many rows: the fragments of a step are read while the step
     // before is multiplied, and the first of the values while the weights are
     // formed (a read takes longer than its products). Chunks of a prompt of 2048
-    // take 369 us with this and 377 without, 256 values a head 61 and 64.
+    // take 369 us with this and 377 without, 256 channels a head 61 and 64.
     struct KeyStep {
         u32x4 k[2][2];
     };
@@ -1083,6 +1085,15 @@ __device__ __forceinline__ Reach take_rows(const TreeArgs& a, const Work& w, int
 // Few rows: all wavefronts hold the same 16 TM rows and take key tiles in
 // turn, each through LDS of its own (first the keys, then, in the same place,
 // the values), without a barrier until they join.
+//
+// Bound by the bytes of the committed keys and values, which each (sequence,
+// key-value head) reads once: a query row brings 2 flop a byte (4 in 8 bits) and the
+// matrix cores would take 250.  So every wavefront keeps the keys and
+// values of its next tile on their way while it works on one, and one tile of LDS a
+// wavefront, not two, lets more of them run on a compute unit.  32 sequences of up to 16k tokens, 8 heads of 128 channels
+// (1.18 GB): 211 us, 5.6 TB/s; one of 131k in 8 bits (268 MB): 48 us, 5.6 TB/s; a
+// copy that reads and writes reaches 4.9.  Short sequences are latency: 200 of up
+// to 1000 tokens in a window (44 MB) 42 us, 8 trees over up to 64 tokens 7.7.
 template <int TYPE, int DP, int TM>
 __global__ __launch_bounds__(64 * kWaves, TM == 1 && DP == 64 ? 4 : TM == 1 && TYPE == RAC_CACHE_FP8 ? 3 : 2) void tree_few_kernel(TreeArgs a) {
     constexpr int M = 16 * TM, kTileP = kTile * DP / 8, kPad = DP + 4;
@@ -1226,7 +1237,18 @@ __global__ __launch_bounds__(64 * kWaves, TM == 1 && DP == 64 ? 4 : TM == 1 && T
 }
 
 // Many rows: each wavefront holds 16 TM rows of its own, and all share the
-// keys and values of two tiles at a time in LDS, two such pairs in turn.
+// keys and values of two tiles at a time in LDS, two such pairs in turn: the next
+// pair's loads are under way during the products of this one, and one barrier a
+// pair is enough.
+//
+// Bound by the matrix cores together with what feeds them: a fragment of keys or
+// values read from LDS (16 bytes a lane) serves TM products of 16 x 16 x 32.
+// Without its exponentials the prompt's case would take 335 us instead of 369; four
+// tiles of rows a wavefront would halve the reads, but do not fit in the registers
+// (755 us).  Chunks of prompts of up to 2048 tokens, 28 query heads of 128 channels
+// (310 GF): 369 us, 840 TF/s, where a product of two 8192 x 8192 matrices reaches
+// 1210.  16 trees of up to 64 nodes over up to 8k tokens, four query heads a key-value
+// head (34 GF, 211 MB): 81 us and a join of 13.
 template <int TYPE, int DP, int TM, int W>
 __global__ __launch_bounds__(64 * W, TM * DP <= 256 && DP < 256 ? 2 : 1) void tree_many_kernel(TreeArgs a) {
     // Fragments read ahead need registers: four wavefronts of 32 rows have none left.
@@ -1393,9 +1415,13 @@ again:
     }
 }
 
-// Joins the parts of the sequences that were split.  DP / 4 lanes take a (row,
-// query head) pair, four channels each.  A workgroup takes a row; with SPLIT (few
-// pairs, so many parts) a few pairs, and its wavefronts share their parts.
+// Joins the parts of the sequences that were split:
+//   max = max_c m_c,  l = sum_c l_c 2^(m_c - max),  out = sum_c o_c 2^(m_c - max) / l.
+// DP / 4 lanes take a (row, query head) pair, four channels each.  A workgroup takes
+// a row; with SPLIT (few pairs, so many parts) a few pairs, and its wavefronts share
+// their parts.  Bound by latency where parts are many and pairs few (one sequence of
+// 131k tokens, 64 pairs: 7.1 us; 32 of 16k: 5.9) and by the parts' bytes where pairs
+// are many (694 rows of 32 heads, 13 us).
 template <int TYPE, int DP, bool SPLIT>
 __global__ __launch_bounds__(64 * kWaves) void tree_join_kernel(TreeArgs a) {
     constexpr int kLanes = DP / 4, kPairs = 64 / kLanes, kAtOnce = 8;
@@ -1514,7 +1540,10 @@ struct Choice {
     uint64_t bytes, plan;  // of the scratch; where the plan lies in it
 };
 
-constexpr int kMinChunk = 8;  // key tiles
+// Key tiles that a part has at least, two a wavefront: shorter ones cost more in
+// the join than they save, longer ones leave compute units without work (one
+// sequence of 8k tokens 16.2 us; 18.6 with 4, 18.2 with 16).
+constexpr int kMinChunk = 8;
 
 // rows: the most of a sequence and a key-value head; mean: of all sequences.
 template <int TYPE, int DP>
@@ -1526,8 +1555,8 @@ void choose_form(int rows, int mean, Choice& c) {
     // (TM = 2 with 16-bit pages of 128 channels would need more than 256 registers)
     constexpr bool kTwo = DP == 64 || (DP == 128 && TYPE == RAC_CACHE_FP8);
     // (most sequences with 16 rows or fewer: two tiles of 16 for the others are
-    // faster, 64 sequences of 12 to 20 rows 69 us, 89 with one of 32; where all have
-    // 32 it is the other way round, 177 and 268)
+    // faster, 64 sequences of 12 to 20 rows, 64 channels, 58 us, 64 with one of 32; where
+    // all have 32 it is the other way round, 135 and 126, in 8 bits 174 and 145)
     if ((rows <= 16 || (rows <= 32 && mean <= 17)) && DP < 256) {
         c.m = 16;
         c.target = DP == 64 ? 1024 : TYPE == RAC_CACHE_FP8 ? 768 : 512;
@@ -1536,9 +1565,13 @@ void choose_form(int rows, int mean, Choice& c) {
         c.m = 32;
         c.kernel = reinterpret_cast<const void*>(tree_few_kernel<TYPE, kTwo ? DP : 64, 2>);
     } else if (rows <= 64 || DP == 256) {
+        // (64 rows on up to 8k tokens 142 us, 151 with 128 rows a workgroup; 24 rows 240 and 252;
+        // 256 channels leave registers for 16 rows a wavefront)
         c.m = 64;
         c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP, 1, 4>);
     } else if (rows < 512 || DP == 64) {
+        // (trees of 64 nodes, 256 rows: 93 us, 108 with 256 rows a workgroup, which leaves too few;
+        // prompts, 4900 to 14000 rows: 386 and 369)
         c.m = 128;
         c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP < 256 ? DP : 128, 2, 4>);
     } else {
@@ -1548,6 +1581,9 @@ void choose_form(int rows, int mean, Choice& c) {
     }
 }
 
+// Workgroups from which the join takes a row each instead of sharing the parts of
+// a few pairs (us, rows and shared: one of 32 heads, 8k tokens, 29.8, 16.2; 694 of 32
+// heads 92, 129).
 constexpr int kSplitJoin = 1024;
 
 template <int TYPE>
