@@ -12,7 +12,7 @@ namespace {
 // Fork.  A table entry only moves within its column, so a workgroup that owns
 // whole columns can read all of them before it writes any, in place and in one
 // launch: COLS columns of all sequences through LDS.  Lengths move within the
-// first workgroup alone.
+// last workgroup, which does nothing else.
 //
 // Bound by latency: entries, parents and bounds are dependent reads.  8 sequences of
 // up to 250 tokens 2.6 us; 256 of up to 32000 (6 MB of table and counts) 10.6.
@@ -50,44 +50,60 @@ template <int COLS>
 __global__ __launch_bounds__(kForkThreads) void cache_fork_kernel(ForkArgs a) {
     extern __shared__ int32_t old[];  // [seqs][COLS]
     constexpr int kRows = kForkThreads / COLS;
+    if (blockIdx.x == gridDim.x - 1) {
+        for (int d = (int)threadIdx.x; d < a.seqs; d += kForkThreads) old[d] = a.lengths[d];
+        __syncthreads();
+        for (int d = (int)threadIdx.x; d < a.seqs; d += kForkThreads) {
+            const int parent = a.parents[d];
+            int n = parent >= 0 && parent < a.seqs ? old[parent] : 0;
+            if (a.to && a.to[d] < n) n = a.to[d];
+            a.lengths[d] = n < 0 ? 0 : n;
+        }
+        return;
+    }
     const int c = (int)threadIdx.x % COLS, j = (int)blockIdx.x * COLS + c;
     const int each = (a.seqs + kRows - 1) / kRows;  // sequences a thread, one after the other
     const int d0 = (int)threadIdx.x / COLS * each, d1 = d0 + each < a.seqs ? d0 + each : a.seqs;
     const bool in = j < a.max_pages;
     int32_t* const column = a.table + j;
+    // (what the call asks of a few sequences, read ahead of the stores between them)
+    constexpr int kAtOnce = 8;
+    int parent[kAtOnce], from[kAtOnce], to[kAtOnce];
+    const auto ask = [&](int d) {
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) {
+            if (d + y >= d1) break;
+            parent[y] = a.parents[d + y];
+            from[y] = a.from ? a.from[d + y] : 0;
+            to[y] = a.to ? a.to[d + y] : 0x7FFFFFFF;
+        }
+    };
     if (in) {
+        ask(d0);
 #pragma unroll 8
         for (int d = d0; d < d1; ++d) old[d * COLS + c] = column[(size_t)d * a.max_pages];
     }
     __syncthreads();
-    if (in) {
-        const int first = j << a.log_page, past = (j + 1) << a.log_page;
-        RefSum less{a.refs, a.pages, -1, 0}, more{a.refs, a.pages, -1, 0};
-#pragma unroll 4
-        for (int d = d0; d < d1; ++d) {
-            const int parent = a.parents[d], was = old[d * COLS + c];
-            int now = parent >= 0 && parent < a.seqs ? old[parent * COLS + c] : -1;
-            if (a.to && first >= a.to[d]) now = -1;
-            if (a.from && past <= a.from[d]) now = -1;
+    if (!in) return;
+    const int first = j << a.log_page, past = (j + 1) << a.log_page;
+    RefSum less{a.refs, a.pages, -1, 0}, more{a.refs, a.pages, -1, 0};
+    for (int d = d0; d < d1; d += kAtOnce) {
+        if (d != d0) ask(d);
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) {
+            if (d + y >= d1) break;
+            const int was = old[(d + y) * COLS + c];
+            int now = parent[y] >= 0 && parent[y] < a.seqs ? old[parent[y] * COLS + c] : -1;
+            if (first >= to[y] || past <= from[y]) now = -1;
             if (now < 0 || now >= a.pages) now = -1;
             if (now == was) continue;
-            column[(size_t)d * a.max_pages] = now;
+            column[(size_t)(d + y) * a.max_pages] = now;
             less.add(was, -1);
             more.add(now, 1);
         }
-        less.flush();
-        more.flush();
     }
-    if (blockIdx.x != 0) return;
-    __syncthreads();
-    for (int d = (int)threadIdx.x; d < a.seqs; d += kForkThreads) old[d] = a.lengths[d];
-    __syncthreads();
-    for (int d = (int)threadIdx.x; d < a.seqs; d += kForkThreads) {
-        const int parent = a.parents[d];
-        int n = parent >= 0 && parent < a.seqs ? old[parent] : 0;
-        if (a.to && a.to[d] < n) n = a.to[d];
-        a.lengths[d] = n < 0 ? 0 : n;
-    }
+    less.flush();
+    more.flush();
 }
 
 // ---------------------------------------------------------------------------
@@ -417,7 +433,7 @@ rac_status rac_cache_fork(const rac_cache_config* cfg, const int32_t* parents, c
     const int cols = cfg->seqs <= 1024 ? 16 : 4;
     const void* kernel = cols == 16 ? reinterpret_cast<const void*>(cache_fork_kernel<16>)
                                     : reinterpret_cast<const void*>(cache_fork_kernel<4>);
-    return launch(kernel, (unsigned)((cfg->max_pages + cols - 1) / cols), kForkThreads, a,
+    return launch(kernel, (unsigned)((cfg->max_pages + cols - 1) / cols + 1), kForkThreads, a,
                   (size_t)cfg->seqs * cols * sizeof(int32_t), stream);
 }
 
