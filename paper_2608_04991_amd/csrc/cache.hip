@@ -15,7 +15,7 @@ namespace {
 // last workgroup, which does nothing else.
 //
 // Bound by latency: entries, parents and bounds are dependent reads.  8 sequences of
-// up to 250 tokens 2.6 us; 256 of up to 32000 (6 MB of table and counts) 10.6.
+// up to 250 tokens 2.0 us; 256 of up to 32000 (6 MB of table and counts) 7.9.
 struct ForkArgs {
     const int32_t* parents;
     const int32_t* from;
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
 // Second launch: `parts` workgroups per (sequence, layer), which take its tokens
 // in turn; the first also copies the shared page.  Bound by bytes where there are
 // many: 128 sequences, 8 layers of 8 heads of 128 channels to 8 bits, 64 MB with
-// the copied pages, 15.6 us (4.1 TB/s); 8 sequences of one layer 4.3 us.
+// the copied pages, 14 us (4.5 TB/s); 8 sequences of one layer 4.6 us.
 struct MoveArgs {
     uint8_t* pool;
     const int32_t* table;
