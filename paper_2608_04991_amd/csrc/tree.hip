@@ -791,11 +791,13 @@ struct Load {
             eight[g] = pool + (((uint64_t)p * ax.page_stride << 4) +
                                ((uint32_t)(tile * kTile + row0 + 8 * g) & ((1u << ax.log_page) - 1u)) * row_bytes);
         }
-        // (a drafted row past the last reads the last)
+        // (a drafted row past the last reads the last; offsets from the first row of
+        // the tile, so that ROWS - 1 rows of up to 2^26 bytes are the most)
         const uint32_t stride = (uint32_t)(2 * ax.kv_stride);
-        const int first = tile * kTile + row0;
+        const int first = tile * kTile + row0, left = ax.n - 1 - first;
+        const uint32_t rows = left <= 0 ? 0u : left < ROWS ? (uint32_t)left : (uint32_t)(ROWS - 1);
         const uint8_t* const draft = reinterpret_cast<const uint8_t*>((values ? ax.v : ax.k) + (int64_t)(first < ax.n ? first : ax.n - 1) * ax.kv_stride);
-        const uint32_t own = past ? inner : in * stride + c, last = past ? ~0u : (first < ax.n ? ax.n - 1 - first : 0) * stride + c;
+        const uint32_t own = past ? inner : in * stride + c, last = past ? ~0u : rows * stride + c;
 #pragma unroll
         for (int y = 0; y < kN; ++y) {
             const uint8_t* at = eight[y * kR / 8];
