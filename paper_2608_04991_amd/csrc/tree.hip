@@ -691,7 +691,7 @@ __device__ __forceinline__ TreeArgs args_again() {
 // The key axis of a workgroup, as its loop needs it.
 struct Axis {
     const uint8_t* pool;   // keys of this layer and head in page 0
-    uint32_t page_stride;  // in 16 bytes (a page is less than 64 GiB)
+    uint32_t page_stride;  // in 256 bytes, which divide every page (2^38 bytes are the largest)
     uint32_t side;         // bytes from a page's keys to its values
     const int32_t* row;    // the sequence's table entries
     const uint16_t* k;     // drafted keys and values of this sequence and head
@@ -710,7 +710,7 @@ __device__ __forceinline__ Axis axis_of(const TreeArgs& a, const Work& w, int fr
     const uint64_t plane = ((uint64_t)a.dim << a.log_page) * kB;
     Axis x;
     x.pool = a.pool + ((uint64_t)a.layer * 2 * a.heads + w.head) * plane;
-    x.page_stride = (uint32_t)(plane / 16 * a.heads * 2 * a.layers);
+    x.page_stride = (uint32_t)(plane / 128 * a.heads * a.layers);
     x.side = (uint32_t)(plane * a.heads);
     x.row = a.table + (size_t)w.seq * a.max_pages;
     const int64_t o = w.q.d0 * a.kv_stride + (int64_t)w.head * a.dim;
@@ -788,7 +788,7 @@ struct Load {
 #pragma unroll
         for (int g = 0; g < ROWS / 8; ++g) {
             const uint32_t p = (uint32_t)pg.p[g] < (uint32_t)ax.pages ? (uint32_t)pg.p[g] : 0u;
-            eight[g] = pool + (((uint64_t)p * ax.page_stride << 4) +
+            eight[g] = pool + (((uint64_t)p * ax.page_stride << 8) +
                                ((uint32_t)(tile * kTile + row0 + 8 * g) & ((1u << ax.log_page) - 1u)) * row_bytes);
         }
         // (a drafted row past the last reads the last; offsets from the first row of
