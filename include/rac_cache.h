@@ -81,7 +81,8 @@ size_t rac_cache_pool_bytes(const rac_cache_config* cfg);
  * Scores, maxima, sums and the accumulated output are fp32; the sum of the
  * weights takes them unrounded.  Before they meet the values the weights are
  * rounded to the 16-bit type of the queries (at most 2^-8 (bf16) or 2^-11 (fp16)
- * of each); where a sequence has few rows a key-value head (max_rows * q_heads /
+ * of each; fp16 weights below 2^-25 of the row's largest by at most 2^-36 of that
+ * one); where a sequence has few rows a key-value head (max_rows * q_heads /
  * kv_heads <= 16, and up to 32 in some types) what the rounding left goes in as
  * well.  The output is rounded once. */
 typedef struct {

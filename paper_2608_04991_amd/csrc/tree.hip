@@ -437,12 +437,18 @@ __device__ __forceinline__ u32x2 read_column(const u32x4* tile, uint32_t lane, u
 // roundings together are 1.4 times the output's.  Where few rows wait for memory
 // the second product costs nothing (32 x 16k tokens 217 us with it and without,
 // one sequence of 8k 16).
+//
+// The largest weight of a row so far lies between 2^kUp and 2^(kUp + kSlack).  bf16
+// has the exponents of the sums, so kUp = 0 does.  fp16 weights end below 2^16 and
+// lose bits below 2^-14: as far up as they go, a weight keeps its 11 bits down to 2^-25
+// of the largest (17 nats below it), and what is smaller is off by 2^-36 of it at most.
 template <int TYPE, int DP, int TM, bool FINE>
 struct Rows {
     static constexpr int kP = FINE ? 2 : 1;
+    static constexpr float kUp = TYPE == RAC_CACHE_FP16 ? 11.0f : 0.0f, kSlack = TYPE == RAC_CACHE_FP16 ? 4.0f : 8.0f;
     u32x4 q[TM][DP / 32];
     f32x4 o[TM][DP / 16];
-    float m[TM];  // reference of the exponentials, log2: at most 8 below the largest score so far
+    float m[TM];  // reference of the exponentials, log2: kUp to kUp + kSlack below the largest score so far
     float l[TM];  // sum of the weights over this lane's keys
     bool alone;   // a value that some row must not see is an infinity or NaN: the rows are redone one by one
 
@@ -513,12 +519,12 @@ struct Rows {
                 const float x = max3(max3(max3(u[0], u[1], u[2]), u[3], v[0]), v[1], v[2]);
                 top[r] = n ? max3(top[r], x * c[n], v[3] * c[n]) : max3(x, v[3], v[3]) * c[n];
             }
-            grow |= top[r] > m[r] + 8.0f;
+            grow |= top[r] > m[r] + (kUp + kSlack);
         }
         if (__any(grow)) {  // (seldom: the reference need not be the maximum, only near it)
 #pragma unroll
             for (int r = 0; r < TM; ++r) {
-                const float now = __builtin_fmaxf(m[r], max_row(top[r]));
+                const float now = __builtin_fmaxf(m[r], max_row(top[r]) - kUp);
                 const float keep = now == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[r] - now);
                 m[r] = now;
                 l[r] = l[r] * keep;
