@@ -432,19 +432,19 @@ __device__ __forceinline__ u32x2 read_column(const u32x4* tile, uint32_t lane, u
 // i; the weights of the former are the second operand of the latter as they
 // lie, if the values' keys are taken in the same order.
 //
-// FINE: a weight goes to the matrix cores as two 16-bit numbers, its rounding
+// KP = 2: a weight goes to the matrix cores as two 16-bit numbers, its rounding
 // and the rest, so that only the output's rounding is left: with one, the two
 // roundings together are 1.4 times the output's.  Where few rows wait for memory
 // the second product costs nothing (32 x 16k tokens 217 us with it and without,
-// one sequence of 8k 16).
+// one sequence of 8k 16), but with 256 channels, where one wavefront has all of it
+// to do, 3 to 6% (32 x 8k tokens 330 us with it, 316 without).
 //
 // The largest weight of a row so far lies between 2^kUp and 2^(kUp + kSlack).  bf16
 // has the exponents of the sums, so kUp = 0 does.  fp16 weights end below 2^16 and
 // lose bits below 2^-14: as far up as they go, a weight keeps its 11 bits down to 2^-25
 // of the largest (17 nats below it), and what is smaller is off by 2^-36 of it at most.
-template <int TYPE, int DP, int TM, bool FINE>
+template <int TYPE, int DP, int TM>
 struct Rows {
-    static constexpr int kP = FINE ? 2 : 1;
     static constexpr float kUp = TYPE == RAC_CACHE_FP16 ? 11.0f : 0.0f, kSlack = TYPE == RAC_CACHE_FP16 ? 4.0f : 8.0f;
     u32x4 q[TM][DP / 32];
     f32x4 o[TM][DP / 16];
@@ -506,9 +506,9 @@ struct Rows {
     // Scores of NT tiles to weights, in the type and order that the values'
     // product takes.  c: factors of the scores, with log2(e) in them; vs: factors
     // of the values (8-bit pages).
-    template <int NT>
+    template <int NT, int KP>
     __device__ __forceinline__ void weights(const f32x4 (&s)[NT][TM][2], const float (&c)[NT], const float (&vs)[NT],
-                                            u32x4 (&p)[NT][TM][kP]) {
+                                            u32x4 (&p)[NT][TM][KP]) {
         float top[TM];
         bool grow = false;
 #pragma unroll
@@ -552,13 +552,14 @@ struct Rows {
                     }
                     const uint32_t u = pack2<TYPE>(x, y);
                     p[n][r][0][i] = u;
-                    if constexpr (FINE) p[n][r][1][i] = pack2<TYPE>(x - widen2<TYPE>(u, 0), y - widen2<TYPE>(u, 1));
+                    if constexpr (KP == 2) p[n][r][1][i] = pack2<TYPE>(x - widen2<TYPE>(u, 0), y - widen2<TYPE>(u, 1));
                 }
             }
     }
 
     // Adds the values of the tile in LDS by their weights.
-    __device__ __forceinline__ void values(const u32x4* vl, const u32x4 (&p)[TM][kP]) {
+    template <int KP>
+    __device__ __forceinline__ void values(const u32x4* vl, const u32x4 (&p)[TM][KP]) {
         const uint32_t lane = threadIdx.x & 63u;
         constexpr int kAtOnce = TM > 1 || DP == 64 ? 4 : 8;
 #pragma unroll
@@ -574,7 +575,7 @@ struct Rows {
 #pragma unroll
                 for (int r = 0; r < TM; ++r)
 #pragma unroll
-                    for (int x = 0; x < kP; ++x) o[r][t0 + t] = mma<TYPE>(v[t], p[r][x], o[r][t0 + t]);
+                    for (int x = 0; x < KP; ++x) o[r][t0 + t] = mma<TYPE>(v[t], p[r][x], o[r][t0 + t]);
         }
     }
 
@@ -632,7 +633,8 @@ struct Rows {
         }
         return x;
     }
-    __device__ __forceinline__ void values_of(ValueStep now, const u32x4* v0, const u32x4* v1, const u32x4 (&p)[2][TM][kP]) {
+    template <int KP>
+    __device__ __forceinline__ void values_of(ValueStep now, const u32x4* v0, const u32x4* v1, const u32x4 (&p)[2][TM][KP]) {
         constexpr int kEach = DP / 64;
 #pragma unroll
         for (int i = 0; i < 2 * kEach; ++i) {
@@ -645,7 +647,7 @@ struct Rows {
 #pragma unroll
                 for (int r = 0; r < TM; ++r)
 #pragma unroll
-                    for (int x = 0; x < kP; ++x) o[r][t0 + t] = mma<TYPE>(now.v[t], p[n][r][x], o[r][t0 + t]);
+                    for (int x = 0; x < KP; ++x) o[r][t0 + t] = mma<TYPE>(now.v[t], p[n][r][x], o[r][t0 + t]);
             now = next;
         }
     }
@@ -1064,8 +1066,8 @@ struct Reach {
     }
 };
 
-template <int TYPE, int DP, int TM, bool FINE>
-__device__ __forceinline__ Reach take_rows(const TreeArgs& a, const Work& w, int row0, Rows<TYPE, DP, TM, FINE>& rows, Seen* seen) {
+template <int TYPE, int DP, int TM>
+__device__ __forceinline__ Reach take_rows(const TreeArgs& a, const Work& w, int row0, Rows<TYPE, DP, TM>& rows, Seen* seen) {
     const uint32_t lane = threadIdx.x & 63u;
     Reach x{1 << 30, 0, 1 << 30, 0, 0, 1 << 30};
 #pragma unroll
@@ -1112,7 +1114,7 @@ __global__ __launch_bounds__(64 * kWaves, TM == 1 && DP == 64 ? 4 : TM == 1 && T
     __shared__ Work work;
     const uint32_t lane = threadIdx.x & 63u;
     const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
-    Rows<TYPE, DP, TM, true> rows;
+    Rows<TYPE, DP, TM> rows;
     Axis ax;
     Reach x;
     {
@@ -1257,8 +1259,10 @@ __global__ __launch_bounds__(64 * kWaves, TM == 1 && DP == 64 ? 4 : TM == 1 && T
 // (310 GF): 369 us, 840 TF/s, where a product of two 8192 x 8192 matrices reaches
 // 1210.  16 trees of up to 64 nodes over up to 8k tokens, four query heads a key-value
 // head (34 GF, 211 MB): 81 us and a join of 13.
-template <int TYPE, int DP, int TM, int W>
-__global__ __launch_bounds__(64 * W, TM * DP <= 256 && DP < 256 ? 2 : 1) void tree_many_kernel(TreeArgs a) {
+//
+// KP: 16-bit numbers of a weight.
+template <int TYPE, int DP, int TM, int W, int KP>
+__device__ __forceinline__ void many_rows(const TreeArgs& a) {
     // Fragments read ahead need registers: four wavefronts of 32 rows have none left.
     constexpr bool kAhead = W == 8 || TM == 1;
     constexpr int M = 16 * TM * W, kBring = 2 * kTile / W, kParts = kTile / kBring, kTileP = kTile * DP / 8;
@@ -1269,7 +1273,7 @@ __global__ __launch_bounds__(64 * W, TM * DP <= 256 && DP < 256 ? 2 : 1) void tr
     __shared__ Work work;
     const uint32_t lane = threadIdx.x & 63u;
     const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
-    Rows<TYPE, DP, TM, false> rows;
+    Rows<TYPE, DP, TM> rows;
     Axis ax;
     Reach x;
     bool busy;  // whether this wavefront has rows
@@ -1360,9 +1364,9 @@ again:
                 if (rows.hide(s[y], bits, now)) rows.look(buf[y][1]);
             }
         }
-        u32x4 p[2][TM][1];
         const bool n0 = TYPE == RAC_CACHE_FP8 && i < ax.committed, n1 = TYPE == RAC_CACHE_FP8 && i + 1 < ax.committed;
         const float c[2] = {n0 ? c8 : c16, n1 ? c8 : c16}, vs[2] = {n0 ? v8 : 1.0f, n1 ? v8 : 1.0f};
+        u32x4 p[2][TM][KP];
         if constexpr (kAhead) {
             const auto first = rows.read_values(buf[0][1], 0);
             __builtin_amdgcn_sched_barrier(0);
@@ -1421,6 +1425,20 @@ again:
         for (int in = r0; in < r0 + 16 * TM && w.row_tile * M + in < w.q.m * b.group; ++in)
             row_alone<TYPE>(b, w, ax, w.row_tile * M + in, part, in, M, DP);
     }
+}
+
+// (with 256 channels for up to 16 rows: tree_few_kernel has no registers for their
+// outputs and its tiles)
+template <int TYPE, int DP, int TM, int W>
+__global__ __launch_bounds__(64 * W, TM * DP <= 256 && DP < 256 ? 2 : 1) void tree_many_kernel(TreeArgs a) {
+    many_rows<TYPE, DP, TM, W, DP == 256 ? 2 : 1>(a);
+}
+
+// More than 16 rows of 144 to 256 channels: a weight rounded once (chunks of prompts of
+// 2048 tokens, 8 query heads of 256 channels, 115 GF: 301 us, 380 TF/s).
+template <int TYPE>
+__global__ __launch_bounds__(64 * kWaves, 1) void tree_wide_kernel(TreeArgs a) {
+    many_rows<TYPE, 256, 1, kWaves, 1>(a);
 }
 
 // Joins the parts of the sequences that were split:
@@ -1576,7 +1594,8 @@ void choose_form(int rows, int mean, Choice& c) {
         // (64 rows on up to 8k tokens 142 us, 151 with 128 rows a workgroup; 24 rows 240 and 252;
         // 256 channels leave registers for 16 rows a wavefront)
         c.m = 64;
-        c.kernel = reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP, 1, 4>);
+        c.kernel = DP == 256 && rows > 16 ? reinterpret_cast<const void*>(tree_wide_kernel<TYPE>)
+                                          : reinterpret_cast<const void*>(tree_many_kernel<TYPE, DP, 1, 4>);
     } else if (rows < 512 || DP == 64) {
         // (trees of 64 nodes, 256 rows: 93 us, 108 with 256 rows a workgroup, which leaves too few;
         // prompts, 4900 to 14000 rows: 386 and 369)

@@ -78,6 +78,25 @@ def check(kind, scale, scores, values, out, lse, dim, two):
     return off
 
 
+@pytest.mark.parametrize("kind", [R.BF16, R.FP16, R.FP8])
+@pytest.mark.parametrize("dim,rows,heads", [
+    (16, 1, 1), (64, 1, 8), (64, 16, 1), (80, 1, 5), (128, 2, 8), (128, 1, 1), (144, 1, 1), (192, 3, 4), (256, 1, 16),
+    (256, 16, 1)])
+@pytest.mark.parametrize("keys,seqs", [(700, 1), (9001, 1), (330, 70)])
+def test_few_rows_keep_what_rounding_a_weight_leaves(kind, dim, rows, heads, keys, seqs):
+    """Every second key has the largest weight, the others one that lies half way
+    between two 16-bit numbers, with values of the other sign that cancel the former."""
+    u = R.ROUND[kind] / 2  # between two numbers below 1 there are u, half way is u / 2 off
+    w = (math.floor((1 / 1.75) / u) + 0.5) * u
+    scores = torch.zeros(keys)
+    scores[1::2] = -1.0
+    values = torch.ones(keys)
+    values[1::2] = -1.75
+    out, lse = attend(kind, scores, values, rows, heads, dim, seqs)(-math.log(w))
+    off = check(kind, -math.log(w), scores, values, out, lse, dim, two=True)
+    say(f"[gpu] weights half way, type {kind}, {rows} x {heads} rows of {dim}, {seqs} x {keys} keys: {off:.2f} of the bound")
+
+
 @pytest.mark.parametrize("dim,rows,heads", [(64, 1, 1), (64, 8, 4), (64, 40, 1), (64, 70, 4), (128, 1, 8), (128, 24, 2),
                                             (128, 130, 1), (128, 130, 4), (256, 1, 1), (256, 40, 2)])
 @pytest.mark.parametrize("below", [8.0, 12.5, 14.25, 17.375])
