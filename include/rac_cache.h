@@ -153,7 +153,8 @@ size_t rac_cache_commit_workspace(const rac_cache_config* cfg);
  * were free before the call, one for every page_tokens positions it newly
  * enters, and a last page that it shares is first copied (its committed tokens
  * only) and let go; a sequence whose demand exceeds what those before it left,
- * or whose tokens exceed the table, keeps its state and has committed = 0.
+ * or whose tokens exceed the table, keeps its state, takes no page and has
+ * committed = 0.
  * RAC_CACHE_FP8 stores x / k_scale (v_scale), clamped to +-448 and rounded to
  * nearest even; other types store the bits.  workspace 256-byte aligned.  Two
  * kernel launches. */

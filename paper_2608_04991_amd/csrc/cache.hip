@@ -115,7 +115,8 @@ __global__ __launch_bounds__(kForkThreads) void cache_fork_kernel(ForkArgs a) {
 // Bound by the latency of dependent reads (lengths, table, count, path) and of the
 // sums over the workgroup: 7 us for 8 sequences, 12 for 128 with paths of 40 nodes.  Pages and
 // the order of the sequences are those of a serial loop, so one workgroup has to
-// see all of it.
+// see all of it.  Where there are pages enough, a sequence's place in them is the
+// sum of the demands before it; where there are not, the loop itself finds it.
 struct CommitRecord {
     int32_t length;      // before the call
     int32_t tokens;      // appended
@@ -157,9 +158,33 @@ __device__ __forceinline__ int path_length(const int32_t* p, int most, int draft
     }
 }
 
+// More is asked for than there is: who gets none leaves his to those behind him.  A
+// wavefront goes through the demands (`turn`) 64 at a time and leaves where each one's
+// pages begin among the `found`, or -1.  What is left never grows, so who asks for more
+// than is left is refused for good, and of the others all up to the first that does
+// not fit are served at once.
+__device__ __forceinline__ void serve_in_turn(int32_t* turn, int seqs, int found) {
+    const int lane = (int)threadIdx.x & 63;
+    int left = found;
+    for (int s0 = 0; s0 < seqs; s0 += 64) {
+        const int n = s0 + lane < seqs ? turn[s0 + lane] : 0;
+        int at = -1;
+        for (int first = 0; first < 64;) {  // (lanes from `first` on are not served yet)
+            const bool can = lane >= first && n <= left;
+            const int sum = scan_wave(can ? n : 0);
+            const uint64_t over = __ballot(can && sum > left);
+            first = over ? __builtin_ctzll(over) : 64;
+            if (can && lane < first) at = found - left + sum - n;
+            left -= __builtin_amdgcn_readlane(sum, first - 1);  // (the first that can fits)
+        }
+        if (s0 + lane < seqs) turn[s0 + lane] = at;
+    }
+}
+
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
     __shared__ int sums[kPlanWaves];
     __shared__ int32_t near[kNear];  // the first free pages (the others through memory)
+    __shared__ int32_t turn[4 * kPlanThreads];
     const int t = (int)threadIdx.x, lane = t & 63, page = 1 << a.log_page;
     // A wavefront looks at 1024 pages a step, 64 at a time, in ascending order.
     constexpr int kEach = 16, kStep = kPlanThreads * kEach;
@@ -237,13 +262,25 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
         }
     }
     __syncthreads();  // (the list is read by other threads of this workgroup)
+    if (demand > found) {
+        // (seldom: 27 us with it for 4096 sequences and no free page, 14 where none is asked for)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (t + i * kPlanThreads < a.seqs) turn[t + i * kPlanThreads] = need[i];
+        __syncthreads();
+        if (t < 64) serve_in_turn(turn, a.seqs, found);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (t + i * kPlanThreads < a.seqs) base[i] = turn[t + i * kPlanThreads];
+    }
     const auto free_page = [&](int k) { return k < kNear ? near[k] : a.free_list[k]; };
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int s = t + i * kPlanThreads;
         if (s >= a.seqs) continue;
         CommitRecord r{length[i], tokens[i], -1, -1};
-        if (base[i] + need[i] > found) r.tokens = 0;
+        if (base[i] < 0) r.tokens = 0;
         if (r.tokens > 0) {
             int32_t* row = a.table + (size_t)s * a.max_pages;
             int at = ((length[i] + page - 1) >> a.log_page) - (fresh[i] ? 1 : 0);

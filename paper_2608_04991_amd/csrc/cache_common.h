@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "rac_cache.h"
 
 namespace {
@@ -34,6 +36,23 @@ inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintp
 inline int log2_of(int v) { return __builtin_ctz((unsigned)v); }
 
 __device__ __forceinline__ int clamp_int(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+// Sums over the lanes up to this one, by moves between neighbouring lanes.
+template <class T>
+__device__ __forceinline__ T scan_wave(T v) {
+    const auto from = [](T x, auto ctrl, auto rows) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value,
+                                                                 decltype(rows)::value, 0xF, false));
+    };
+    using std::integral_constant;
+    using all = integral_constant<int, 0xF>;
+    v = v + from(v, integral_constant<int, 0x111>{}, all{});                          // row_shr:1
+    v = v + from(v, integral_constant<int, 0x112>{}, all{});
+    v = v + from(v, integral_constant<int, 0x114>{}, all{});
+    v = v + from(v, integral_constant<int, 0x118>{}, all{});
+    v = v + from(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});  // row_bcast:15
+    return v + from(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});  // row_bcast:31
+}
 
 // Sum over the threads of a workgroup of WAVES wavefronts before this one, and
 // over all of them (sums: LDS).

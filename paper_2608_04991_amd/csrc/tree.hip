@@ -2,8 +2,6 @@
 // the paged cache.  The contract is in include/rac_cache.h.
 #include <math.h>
 
-#include <type_traits>
-
 #include "cache_common.h"
 
 namespace {
@@ -205,23 +203,6 @@ struct Cut {
 __device__ __forceinline__ Cut cut_of(const TreeArgs& a, const Seq& q, int most) {
     const int keys = key_tiles(a, q);
     return Cut{(q.m * a.group + a.m - 1) / a.m, keys > most ? (keys + most - 1) / most : 1};
-}
-
-// Sums over the lanes up to this one, by moves between neighbouring lanes.
-template <class T>
-__device__ __forceinline__ T scan_wave(T v) {
-    const auto from = [](T x, auto ctrl, auto rows) {
-        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value,
-                                                                 decltype(rows)::value, 0xF, false));
-    };
-    using std::integral_constant;
-    using all = integral_constant<int, 0xF>;
-    v = v + from(v, integral_constant<int, 0x111>{}, all{});                          // row_shr:1
-    v = v + from(v, integral_constant<int, 0x112>{}, all{});
-    v = v + from(v, integral_constant<int, 0x114>{}, all{});
-    v = v + from(v, integral_constant<int, 0x118>{}, all{});
-    v = v + from(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});  // row_bcast:15
-    return v + from(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});  // row_bcast:31
 }
 
 // Parts of at most this many key tiles: all parts of all sequences together just
