@@ -224,11 +224,12 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
                     fresh[i] = shared || tail[i] < 0;
                     need[i] += fresh[i];
                 }
+                if (need[i] > a.pages) tokens[i] = need[i] = 0;
             }
         }
         int all;
-        base[i] = demand + scan_workgroup<kPlanWaves>(need[i], sums, &all);
-        demand += all;
+        base[i] = (int)((uint32_t)demand + (uint32_t)scan_workgroup<kPlanWaves>(need[i], sums, &all));
+        demand = all < kMostSum - demand ? demand + all : kMostSum;  // (more than any pool has)
     }
     // the free pages, lowest first, until the demand is met
     int found = 0;

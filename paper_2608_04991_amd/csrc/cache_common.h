@@ -54,8 +54,12 @@ __device__ __forceinline__ T scan_wave(T v) {
     return v + from(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});  // row_bcast:31
 }
 
+constexpr int kMostSum = 1 << 29;
+
 // Sum over the threads of a workgroup of WAVES wavefronts before this one, and
-// over all of them (sums: LDS).
+// over all of them (sums: LDS).  With up to 2^24 a thread no sum of a wavefront
+// wraps; the whole one stays at kMostSum where it is more, and then the sums before
+// a thread mean nothing.
 template <int WAVES>
 __device__ __forceinline__ int scan_workgroup(int v, int* sums, int* total) {
     const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
@@ -67,13 +71,14 @@ __device__ __forceinline__ int scan_workgroup(int v, int* sums, int* total) {
     __syncthreads();
     if (lane == 63) sums[w] = x;
     __syncthreads();
-    int before = 0, all = 0;
+    uint32_t before = 0;
+    int all = 0;
     for (int i = 0; i < WAVES; ++i) {
         before += i < w ? sums[i] : 0;
-        all += sums[i];
+        all = sums[i] < kMostSum - all ? all + sums[i] : kMostSum;
     }
     *total = all;
-    return before + x - v;
+    return (int)(before + (uint32_t)x - (uint32_t)v);
 }
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

@@ -105,3 +105,33 @@ def test_more_than_4096_pages_from_a_pool_of_more_than_16384():
     p.fork([0, -1, 1, 2, 0], keep_to=[80001, 0, 0, 60000, 70000])
     # (most free pages lie behind the first 16384)
     assert p.commit([30000, 100000, 40000, 1, 3]) == [30000, 100000, 40000, 1, 3]
+
+
+def test_demands_that_add_up_to_more_than_32_bits():
+    """Ranges of drafted rows that overlap, as a broken draft_start has them: 2047
+    sequences that ask for 2^20 + 1024 pages each, of a pool of 64."""
+    rows, seqs = (1 << 23) + 8192, 4096
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("24 GiB of device memory are not free")
+    say("[gpu] a demand of 2^31 pages")
+    cfg = rac.CacheConfig(1, 1, 16, 8, 64, seqs, rows // 8, R.BF16)
+    table, lengths, refs = rac.rac_cache_new(cfg)  # (16 GiB)
+    pool = torch.full((rac.rac_cache_pool_bytes(cfg) // 2,), 7, dtype=torch.int16, device="cuda")
+    k = torch.randn(1, rows, 1, 16, device="cuda").bfloat16()
+    start = torch.tensor([0, rows] * (seqs // 2) + [0], dtype=torch.int32, device="cuda")
+    start[-3:] = torch.tensor([rows - 9, rows, rows], dtype=torch.int32)
+    out = torch.full((seqs,), -3, dtype=torch.int32, device="cuda")
+    ws = torch.empty(rac.rac_cache_commit_workspace(cfg), dtype=torch.uint8, device="cuda")
+    rac.rac_cache_commit(cfg, pool, table, lengths, refs, k, k, start, out, ws)
+    torch.cuda.synchronize()
+    want = [0] * seqs
+    want[-2] = 9  # (the last rows once more)
+    assert out.tolist() == want and lengths.tolist() == want
+    assert refs.tolist() == [1, 1] + [0] * 62 and table[-2, :3].tolist() == [0, 1, -1]
+    assert int((table >= 0).sum()) == 2
+    pages = pool.view(64, 2, 8, 16)
+    got = torch.cat([pages[0], pages[1, :, :1]], 1)
+    assert torch.equal(got, k[0, -9:, 0].view(torch.int16).expand(2, 9, 16))
+    assert (pages[1, :, 1:] == 7).all() and (pages[2:] == 7).all()
+    del table, k
+    torch.cuda.empty_cache()
