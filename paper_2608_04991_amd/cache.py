@@ -154,6 +154,14 @@ def _rows(t, what: str, rows: int, heads: int, dim: int):
                      "contiguous")
 
 
+def _drafts(t, what: str, rows: int, heads: int, dim: int):
+    """_rows of drafted keys or values.  How many there are comes from the tensor,
+    so an address is not enough."""
+    if isinstance(t, int):
+        raise ValueError(f"{what}: expected a GPU tensor, not an address: its rows are counted")
+    return _rows(t, what, rows, heads, dim)
+
+
 def rac_cache_pool_bytes(cfg: CacheConfig) -> int:
     return cfg._pool_bytes
 
@@ -187,8 +195,8 @@ def rac_tree_attention(cfg: CacheConfig, tree: TreeConfig, layer: int, pool, tab
     R, Q, H, D, S = tree.rows, tree.q_heads, cfg.kv_heads, cfg.head_dim, cfg.seqs
     qp, qs, _ = _rows(q, "q", R, Q, D)
     op, os_, _ = _rows(out, "out", R, Q, D)
-    kp, ks, drafted = _rows(k, "k", 0, H, D)
-    vp, vs, _ = _rows(v, "v", drafted, H, D)
+    kp, ks, drafted = _drafts(k, "k", 0, H, D)
+    vp, vs, _ = _drafts(v, "v", drafted, H, D)
     if ks != vs and drafted > 1 and v is not None:
         raise ValueError("k and v: expected the same distance between rows")
     words = 0
@@ -281,8 +289,8 @@ def rac_predictor_tree_step(cfg, cache: CacheConfig, tree: TreeConfig, weights, 
     value in row slot[r] of draft_k and draft_v (bf16 [draft_rows][heads][64]) and
     predicts ref_out[r]."""
     dev, R, S, need = _rac._dev, tree.rows, cache.seqs, rac_predictor_tree_workspace(cfg, cache, tree)
-    kp, ks, drafted = _rows(draft_k, "draft_k", 0, cfg.heads, 64)
-    vp, vs, _ = _rows(draft_v, "draft_v", drafted, cfg.heads, 64)
+    kp, ks, drafted = _drafts(draft_k, "draft_k", 0, cfg.heads, 64)
+    vp, vs, _ = _drafts(draft_v, "draft_v", drafted, cfg.heads, 64)
     if drafted > 1 and (ks != cfg.model or vs != cfg.model):
         raise ValueError("draft_k and draft_v: expected contiguous rows")
     words = 0 if mask is None else int(mask.shape[-1])

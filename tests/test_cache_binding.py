@@ -1,0 +1,60 @@
+"""What the binding of the paged cache does with its arguments, without a GPU: a
+library that records the calls, and tensors without memory."""
+from __future__ import annotations
+
+import pytest
+
+import paper_2608_04991_amd as rac
+from tests.test_cache_abi import CFG, P, TREE, _Fake as F, lib  # noqa: F401
+
+PRED = rac.PredictorConfig(512, 128, 2, 256, 16, 8)
+PRED_CACHE, PRED_TREE = rac.CacheConfig(1, 2, 64, 16, 20, 4, 5), rac.TreeConfig(2, 6, 3, 3, 16)
+
+
+@pytest.fixture
+def calls(lib, monkeypatch):  # noqa: F811
+    """The arguments of every call that reaches the library."""
+    called = []
+    fake = type("L", (), {})()
+    for name in ("rac_tree_attention", "rac_cache_commit", "rac_predictor_tree_step"):
+        setattr(fake, name, lambda *a, name=name: called.append((name, a)) or 0)
+    for name in ("rac_cache_pool_bytes", "rac_tree_attention_workspace", "rac_cache_commit_workspace",
+                 "rac_predictor_tree_workspace"):
+        setattr(fake, name, getattr(lib, name))
+    monkeypatch.setattr(rac, "library", lambda: fake)
+    return called
+
+
+def attend(**change):
+    a = dict(pool=P, table=P, lengths=P, q=F((20, 8, 64)), q_start=P, k=F((20, 4, 64)), v=F((20, 4, 64)),
+             out=F((20, 8, 64)), workspace=P, mask=None)
+    a.update(change)
+    mask = a.pop("mask")
+    rac.rac_tree_attention(CFG, TREE, 0, *a.values(), mask=mask, stream=0)
+
+
+def step(**change):
+    a = dict(weights=P, pool=P, table=P, lengths=P, q_start=P, draft_start=P, slot=P, pos=P, h_prev=P,
+             draft_k=F((9, 2, 64)), draft_v=F((9, 2, 64)), ref_out=P, workspace=P, mask=None)
+    a.update(change)
+    mask = a.pop("mask")
+    rac.rac_predictor_tree_step(PRED, PRED_CACHE, PRED_TREE, *a.values(), mask=mask, stream=0)
+
+
+def test_drafted_keys_and_values_are_counted(calls):
+    attend()
+    attend(q=P, out=P)
+    attend(k=None, v=None)
+    step()
+    tensors = [a[6]._obj for name, a in calls[:3]]
+    assert [t.draft_rows for t in tensors] == [20, 20, 0] and calls[3][1][16] == 9
+
+
+@pytest.mark.parametrize("names", [("k",), ("v",), ("k", "v")])
+def test_addresses_of_drafts_are_refused(calls, names):
+    # (their rows are unknown: the drafted tokens would be left out)
+    with pytest.raises(ValueError, match="address"):
+        attend(**{n: P for n in names})
+    with pytest.raises(ValueError, match="address"):
+        step(**{"draft_" + n: P for n in names})
+    assert not calls
