@@ -162,6 +162,13 @@ def _drafts(t, what: str, rows: int, heads: int, dim: int):
     return _rows(t, what, rows, heads, dim)
 
 
+def _words(mask) -> int:
+    """Words of a mask's row, 0 without a mask."""
+    if isinstance(mask, int):
+        raise ValueError("mask: expected a GPU tensor, not an address: the words of its rows are counted")
+    return 0 if mask is None else int(mask.shape[-1])
+
+
 def rac_cache_pool_bytes(cfg: CacheConfig) -> int:
     return cfg._pool_bytes
 
@@ -199,9 +206,7 @@ def rac_tree_attention(cfg: CacheConfig, tree: TreeConfig, layer: int, pool, tab
     vp, vs, _ = _drafts(v, "v", drafted, H, D)
     if ks != vs and drafted > 1 and v is not None:
         raise ValueError("k and v: expected the same distance between rows")
-    words = 0
-    if mask is not None:
-        words = mask if isinstance(mask, int) else int(mask.shape[-1])
+    words = _words(mask)
     t = _TreeTensors(qp, kp, vp, dev(q_start, "q_start", 4, S + 1), dev(draft_start, "draft_start", 4, S + 1),
                      dev(mask, "mask", 8, R * words), op, dev(lse, "lse", 4, R * Q), qs, ks, os_, drafted, words)
     need = rac_tree_attention_workspace(cfg, tree)
@@ -293,7 +298,7 @@ def rac_predictor_tree_step(cfg, cache: CacheConfig, tree: TreeConfig, weights, 
     vp, vs, _ = _drafts(draft_v, "draft_v", drafted, cfg.heads, 64)
     if drafted > 1 and (ks != cfg.model or vs != cfg.model):
         raise ValueError("draft_k and draft_v: expected contiguous rows")
-    words = 0 if mask is None else int(mask.shape[-1])
+    words = _words(mask)
     _rac._check(_rac.library().rac_predictor_tree_step(
         ctypes.byref(cfg._c()), cache._ref, tree._ref, dev(weights, "weights", 1, 0), _pool(cache, pool),
         dev(table, "table", 4, S * cache.max_pages), dev(lengths, "lengths", 4, S), dev(q_start, "q_start", 4, S + 1),

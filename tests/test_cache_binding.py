@@ -58,3 +58,13 @@ def test_addresses_of_drafts_are_refused(calls, names):
     with pytest.raises(ValueError, match="address"):
         step(**{"draft_" + n: P for n in names})
     assert not calls
+
+
+def test_an_address_of_a_mask_is_refused(calls):
+    # (it was taken as the number of a row's words)
+    attend(mask=F((20, 2), 8))
+    assert calls[0][1][6]._obj.mask_words == 2
+    for call in (attend, step):
+        with pytest.raises(ValueError, match="address"):
+            call(mask=P)
+    assert len(calls) == 1
