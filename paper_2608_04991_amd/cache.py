@@ -16,7 +16,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
-from dataclasses import dataclass
+from dataclasses import dataclass, fields
 
 import paper_2608_04991_amd as _rac
 
@@ -49,8 +49,16 @@ class _TreeTensors(ctypes.Structure):
                [(n, ctypes.c_int32) for n in ("draft_rows", "mask_words")]
 
 
+class _Kept:
+    """A configuration that keeps what its fields fix: the library's struct, a
+    reference to it, sizes.  A copy or a pickle has the fields alone."""
+
+    def __getstate__(self) -> dict:
+        return {f.name: getattr(self, f.name) for f in fields(self)}
+
+
 @dataclass(frozen=True)
-class CacheConfig:
+class CacheConfig(_Kept):
     layers: int
     kv_heads: int
     head_dim: int
@@ -86,7 +94,7 @@ class CacheConfig:
 
 
 @dataclass(frozen=True)
-class TreeConfig:
+class TreeConfig(_Kept):
     q_heads: int
     rows: int
     max_rows: int

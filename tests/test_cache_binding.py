@@ -2,6 +2,9 @@
 library that records the calls, and tensors without memory."""
 from __future__ import annotations
 
+import copy
+import pickle
+
 import pytest
 
 import paper_2608_04991_amd as rac
@@ -68,3 +71,15 @@ def test_an_address_of_a_mask_is_refused(calls):
         with pytest.raises(ValueError, match="address"):
             call(mask=P)
     assert len(calls) == 1
+
+
+@pytest.mark.parametrize("again", [copy.copy, copy.deepcopy, lambda x: pickle.loads(pickle.dumps(x))],
+                         ids=["copy", "deepcopy", "pickle"])
+def test_configurations_are_copied_after_their_use(lib, again):  # noqa: F811
+    cfg, tree = rac.CacheConfig(2, 4, 64, 16, 100, 8, 10, 2, 0.5, 0.25), rac.TreeConfig(8, 20, 5, 5, 7, 0.5)
+    sizes = lambda c, t: (rac.rac_cache_pool_bytes(c), rac.rac_cache_commit_workspace(c),
+                          rac.rac_tree_attention_workspace(c, t))
+    want = sizes(cfg, tree)
+    c, t = again(cfg), again(tree)
+    assert c == cfg and t == tree and c._ref._obj is not cfg._ref._obj and t._ref._obj is not tree._ref._obj
+    assert sizes(c, t) == want and bytes(c._c()) == bytes(cfg._c()) and bytes(t._c()) == bytes(tree._c())
