@@ -272,7 +272,11 @@ def rac_cache_commit(cfg: CacheConfig, pool, table, lengths, refs, k, v, draft_s
     if vrows != rows or vrow != row or vlayer != layer:
         raise ValueError("k and v: expected the same rows, apart by the same distances")
     if max_path is None:
+        if isinstance(path, int):
+            raise ValueError("path: an address needs max_path beside it")
         max_path = rows if path is None else int(path.shape[-1])
+    elif S > 1 and path is not None and not isinstance(path, int) and path.dim() > 1 and path.shape[-1] != max_path:
+        raise ValueError(f"path: its rows have {path.shape[-1]} entries, but max_path is {max_path}")
     _rac._check(_rac.library().rac_cache_commit(
         cfg._ref, _pool(cfg, pool), dev(table, "table", 4, S * cfg.max_pages),
         dev(lengths, "lengths", 4, S), dev(refs, "refs", 4, cfg.pages), kp, vp, row, layer, rows,

@@ -3,6 +3,7 @@ library that records the calls, and tensors without memory."""
 from __future__ import annotations
 
 import copy
+import dataclasses
 import pickle
 
 import pytest
@@ -83,3 +84,24 @@ def test_configurations_are_copied_after_their_use(lib, again):  # noqa: F811
     c, t = again(cfg), again(tree)
     assert c == cfg and t == tree and c._ref._obj is not cfg._ref._obj and t._ref._obj is not tree._ref._obj
     assert sizes(c, t) == want and bytes(c._c()) == bytes(cfg._c()) and bytes(t._c()) == bytes(tree._c())
+
+
+def test_rows_of_a_path(calls):
+    kv = F((2, 20, 4, 64))
+    commit = lambda path, **kw: rac.rac_cache_commit(CFG, P, P, P, P, kv, kv, P, P, P, path=path, stream=0, **kw)
+    commit(F((8, 5), 4))
+    commit(F((8, 5), 4), max_path=5)
+    commit(F((40,), 4), max_path=5)
+    commit(P, max_path=3)
+    commit(None)
+    commit(None, max_path=7)
+    one = lambda path, **kw: rac.rac_cache_commit(dataclasses.replace(CFG, seqs=1), P, P, P, P, kv, kv, P, P, P, path=path,
+                                                  stream=0, **kw)
+    one(F((5,), 4))
+    one(F((1, 5), 4), max_path=3)  # (the first entries of one row)
+    assert [a[12] for _, a in calls] == [5, 5, 5, 3, 20, 7, 5, 3]
+    for path, kw in ((F((8, 5), 4), dict(max_path=3)), (F((8, 5), 4), dict(max_path=6)), (F((40,), 4), {}),
+                     (F((40,), 4), dict(max_path=6)), (P, {})):
+        with pytest.raises(ValueError):
+            commit(path, **kw)
+    assert len(calls) == 8
