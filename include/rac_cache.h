@@ -87,7 +87,7 @@ size_t rac_cache_pool_bytes(const rac_cache_config* cfg);
  * well.  The output is rounded once. */
 typedef struct {
     int32_t q_heads;   /* a multiple of kv_heads, at most 64 times as many        */
-    int32_t rows;      /* rows of q and out, 0..2^20                              */
+    int32_t rows;      /* rows of q and out, 0..2^20; rows * q_heads below 2^26   */
     int32_t max_rows;  /* most query rows of a sequence; further ones are ignored */
     int32_t max_draft; /* most drafted tokens of a sequence; further ones unseen  */
     int32_t window;    /* 0: none                                                 */
@@ -109,14 +109,15 @@ typedef struct {
     int32_t mask_words;         /* 0 without a mask                                */
 } rac_tree_tensors;
 
-/* Host-only, pure.  Bytes of the call's device scratch, or 0 for a bad
- * configuration. */
+/* Host-only, pure.  Bytes of the call's device scratch, or 0 for a
+ * configuration outside the ranges above. */
 size_t rac_tree_attention_workspace(const rac_cache_config* cfg, const rac_tree_config* tree);
 
 /* Attention of layer `layer`.  q, k, v and out 16-byte aligned, mask 8-byte,
  * the int32 and fp32 arrays 4-byte, workspace 256-byte.  Rows of q outside
- * every sequence's range keep their out and lse.  RAC_ERR_INVALID, _ALIGN and
- * _CAPACITY (workspace) before any launch. */
+ * every sequence's range keep their out and lse.  RAC_ERR_INVALID, _ALIGN,
+ * _UNSUPPORTED (2^26 or more rows * q_heads: split the call) and _CAPACITY
+ * (workspace) before any launch. */
 rac_status rac_tree_attention(const rac_cache_config* cfg, const rac_tree_config* tree, int32_t layer,
                               const void* pool, const int32_t* table, const int32_t* lengths,
                               const rac_tree_tensors* t, void* workspace, size_t workspace_bytes,
@@ -166,7 +167,8 @@ rac_status rac_cache_commit(const rac_cache_config* cfg, void* pool, int32_t* ta
 /* Copies page src[i] of one pool to page dst[i] of another (or the same) of
  * the same configuration, all layers, i < n.  The dst differ from each other
  * and, within one pool, from every src; a pair with a number outside the pool
- * is skipped.  One kernel launch. */
+ * is skipped.  One kernel launch; RAC_ERR_UNSUPPORTED where it would take 2^24
+ * pieces of 16 KiB or more (n times those of a page). */
 rac_status rac_cache_copy(const rac_cache_config* cfg, const void* src_pool, const int32_t* src, void* dst_pool,
                           const int32_t* dst, int32_t n, rac_stream_t stream);
 

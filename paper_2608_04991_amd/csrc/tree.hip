@@ -1537,6 +1537,9 @@ bool tree_valid(const rac_cache_config* c, const rac_tree_config* t) {
            t->scale >= 0.0f && t->scale < __builtin_inff();
 }
 
+// (row, query head) pairs that the kernels' 32-bit counts of workgroups and slots hold.
+bool tree_counted(const rac_tree_config* t) { return (int64_t)t->rows * t->q_heads < (int64_t(1) << 26); }
+
 // Which kernel a call takes, how its work is split, and what that needs.
 struct Choice {
     const void* kernel;
@@ -1657,7 +1660,7 @@ Choice choose(const rac_cache_config* cfg, const rac_tree_config* tree) {
 extern "C" {
 
 size_t rac_tree_attention_workspace(const rac_cache_config* cfg, const rac_tree_config* tree) {
-    return tree_valid(cfg, tree) ? (size_t)choose(cfg, tree).bytes : 0;
+    return tree_valid(cfg, tree) && tree_counted(tree) ? (size_t)choose(cfg, tree).bytes : 0;
 }
 
 rac_status rac_tree_attention(const rac_cache_config* cfg, const rac_tree_config* tree, int32_t layer,
@@ -1676,6 +1679,7 @@ rac_status rac_tree_attention(const rac_cache_config* cfg, const rac_tree_config
         !aligned(table, 4) || !aligned(lengths, 4) || !aligned(t->q_start, 4) || !aligned(t->draft_start, 4) ||
         !aligned(t->lse, 4) || !aligned(t->mask, 8) || !aligned(workspace, 256))
         return RAC_ERR_ALIGN;
+    if (!tree_counted(tree)) return RAC_ERR_UNSUPPORTED;
     if (workspace_bytes < rac_tree_attention_workspace(cfg, tree)) return RAC_ERR_CAPACITY;
     const bool drafted = t->k && t->draft_rows > 0;
     TreeArgs a{};
@@ -1716,7 +1720,6 @@ rac_status rac_tree_attention(const rac_cache_config* cfg, const rac_tree_config
     a.min_chunk = kMinChunk;
     a.parts = static_cast<float*>(workspace);
     a.slots = c.slots;
-    if ((int64_t)tree->rows * tree->q_heads >= (int64_t(1) << 26)) return RAC_ERR_UNSUPPORTED;
     a.plan = cfg->seqs > 64 ? reinterpret_cast<SeqPlan*>(static_cast<uint8_t*>(workspace) + c.plan) : nullptr;
     a.m = c.m;
     void* p[] = {&a};
