@@ -84,7 +84,12 @@ size_t rac_cache_pool_bytes(const rac_cache_config* cfg);
  * of each; fp16 weights below 2^-25 of the row's largest by at most 2^-36 of that
  * one); where a sequence has few rows a key-value head (max_rows * q_heads /
  * kv_heads <= 16, and up to 32 in some types) what the rounding left goes in as
- * well.  The output is rounded once. */
+ * well.  The output is rounded once.
+ *
+ * A call gives the same bits every time.  Which kernel runs, and how long
+ * sequences are cut into parts, follows from the whole call (the configurations,
+ * all lengths and row counts), so the last bits of a row may change with the
+ * sequences beside it. */
 typedef struct {
     int32_t q_heads;   /* a multiple of kv_heads, at most 64 times as many        */
     int32_t rows;      /* rows of q and out, 0..2^20; rows * q_heads below 2^26   */
@@ -177,12 +182,18 @@ rac_status rac_cache_copy(const rac_cache_config* cfg, const void* src_pool, con
  * and whose inputs are nodes of drafted trees.  Sender and receiver run it
  * level by level: the states of a level are coded against the references that
  * their parents' reconstructions predict, and become the inputs of the next.
+ * They hold the same references bit for bit if they make the same calls: a
+ * reference's last bits follow from the whole call (see rac_tree_attention), so
+ * a receiver must not batch other sequences with them than the sender does.
  * Row r is one input (the reconstruction of a node, or the last committed one):
  * its key and value go to row slot[r] of draft_k and draft_v, and it sees what
  * rac_tree_attention says for these drafted rows, mask, window (that of cfg) and
  * cache; every row should see its own.  The layers and their roundings are
- * those of rac_predictor_step, except that the turned queries are bf16.  The
- * accepted path's keys and values are committed with rac_cache_commit.
+ * those of rac_predictor_step, except that the turned queries are bf16 and that
+ * rac_tree_attention rounds the weights as it says (the mean error of a
+ * reference against the definition, which does neither, is 1.2 times that of
+ * rac_predictor_step).  The accepted path's keys and values are committed with
+ * rac_cache_commit.
  *   cfg       : batch sizes aside, the predictor; tree->rows <= cfg->max_batch
  *   cache     : one layer, kv_heads = cfg->heads, head_dim 64, not FP16
  *   tree      : q_heads = cfg->heads, window = cfg->window, scale 0
