@@ -138,6 +138,10 @@ rac_status rac_tree_attention(const rac_cache_config* cfg, const rac_tree_config
  * outside 0 .. seqs - 1).  Pages are shared, none is copied; refs follow.
  *   parents            : int32 [seqs]
  *   keep_from, keep_to : int32 [seqs], or NULL (0; the parent's length)
+ * Positions before keep_from in a page that stays are still seen.  A keep_from
+ * past the new length lets go of the last page too: the page that a later
+ * commit takes for it has unspecified contents ahead of the appended tokens,
+ * which the attention would see.
  * One kernel launch. */
 rac_status rac_cache_fork(const rac_cache_config* cfg, const int32_t* parents, const int32_t* keep_from,
                           const int32_t* keep_to, int32_t* table, int32_t* lengths, int32_t* refs,
