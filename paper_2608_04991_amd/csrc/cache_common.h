@@ -54,7 +54,7 @@ __device__ __forceinline__ T scan_wave(T v) {
     return v + from(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});  // row_bcast:31
 }
 
-constexpr int kMostSum = 1 << 29;
+constexpr int kMostSum = 1 << 30;
 
 // Sum over the threads of a workgroup of WAVES wavefronts before this one, and
 // over all of them (sums: LDS).  With up to 2^24 a thread no sum of a wavefront
