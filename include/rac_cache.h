@@ -195,8 +195,8 @@ rac_status rac_cache_copy(const rac_cache_config* cfg, const void* src_pool, con
  * cache; every row should see its own.  The layers and their roundings are
  * those of rac_predictor_step, except that the turned queries are bf16 and that
  * rac_tree_attention rounds the weights as it says (the mean error of a
- * reference against the definition, which does neither, is 1.2 times that of
- * rac_predictor_step).  The accepted path's keys and values are committed with
+ * reference against the definition, which does neither, is 1.1 to 1.4 times that
+ * of rac_predictor_step).  The accepted path's keys and values are committed with
  * rac_cache_commit.
  *   cfg       : batch sizes aside, the predictor; tree->rows <= cfg->max_batch
  *   cache     : one layer, kv_heads = cfg->heads, head_dim 64, not FP16

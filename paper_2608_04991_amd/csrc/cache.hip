@@ -113,10 +113,12 @@ __global__ __launch_bounds__(kForkThreads) void cache_fork_kernel(ForkArgs a) {
 // second launch moves the data by the records this one leaves.
 //
 // Bound by the latency of dependent reads (lengths, table, count, path) and of the
-// sums over the workgroup: 7 us for 8 sequences, 12 for 128 with paths of 40 nodes.  Pages and
-// the order of the sequences are those of a serial loop, so one workgroup has to
-// see all of it.  Where there are pages enough, a sequence's place in them is the
-// sum of the demands before it; where there are not, the loop itself finds it.
+// sums over the workgroup: 7 us for 8 sequences, 12 for 128 with paths of up to 4
+// nodes.  One thread enters a sequence's new pages, 0.12 us each (a prompt of 131k
+// tokens in pages of 16: 1 ms).  Pages and the order of the sequences are those of a
+// serial loop, so one workgroup has to see all of it.  Where there are pages enough, a
+// sequence's place in them is the sum of the demands before it; where there are not,
+// the loop itself finds it.
 struct CommitRecord {
     int32_t length;      // before the call
     int32_t tokens;      // appended

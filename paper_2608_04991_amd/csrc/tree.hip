@@ -1083,8 +1083,10 @@ __device__ __forceinline__ Reach take_rows(const TreeArgs& a, const Work& w, int
 // values of its next tile on their way while it works on one, and one tile of LDS a
 // wavefront, not two, lets more of them run on a compute unit.  32 sequences of up to 16k tokens, 8 heads of 128 channels
 // (1.18 GB): 211 us, 5.6 TB/s; one of 131k in 8 bits (268 MB): 48 us, 5.6 TB/s; a
-// copy that reads and writes reaches 4.9.  Short sequences are latency: 200 of up
-// to 1000 tokens in a window (44 MB) 42 us, 8 trees over up to 64 tokens 7.7.
+// copy that reads and writes reaches 4.9.  8 trees over up to 64 tokens: 7.7 us, latency.
+// 200 sequences of up to 1000 tokens in a window (44 MB): 42 us; 1100 workgroups have
+// work where 768 fit at once, in no order of length, and 75 sequences of more than 16
+// rows read every key twice.
 template <int TYPE, int DP, int TM>
 __global__ __launch_bounds__(64 * kWaves, TM == 1 && DP == 64 ? 4 : TM == 1 && TYPE == RAC_CACHE_FP8 ? 3 : 2) void tree_few_kernel(TreeArgs a) {
     constexpr int M = 16 * TM, kTileP = kTile * DP / 8, kPad = DP + 4;
@@ -1232,14 +1234,16 @@ __global__ __launch_bounds__(64 * kWaves, TM == 1 && DP == 64 ? 4 : TM == 1 && T
 // pair's loads are under way during the products of this one, and one barrier a
 // pair is enough.
 //
-// Bound by the matrix cores together with what feeds them: a fragment of keys or
-// values read from LDS (16 bytes a lane) serves TM products of 16 x 16 x 32.
-// Without its exponentials the prompt's case would take 335 us instead of 369; four
-// tiles of rows a wavefront would halve the reads, but do not fit in the registers
+// Bound by no unit alone: of the prompt's cycles the matrix cores are busy for 35%,
+// vector instructions are issued in 42% and LDS is read in 33%.  Products, exponentials
+// and LDS reads mostly follow each other, with two wavefronts a SIMD and a barrier a
+// pair.  Without its exponentials the prompt's case would take 339 us instead of 363; four
+// tiles of rows a wavefront would halve the LDS reads, but do not fit in the registers
 // (755 us).  Chunks of prompts of up to 2048 tokens, 28 query heads of 128 channels
-// (310 GF): 369 us, 840 TF/s, where a product of two 8192 x 8192 matrices reaches
+// (310 GF): 363 us, 855 TF/s, where a product of two 8192 x 8192 matrices reaches
 // 1210.  16 trees of up to 64 nodes over up to 8k tokens, four query heads a key-value
-// head (34 GF, 211 MB): 81 us and a join of 13.
+// head (34 GF, 211 MB): 79 us and a join of 13; matrix cores 22%, vector 37%, LDS 25%,
+// its tiles of 128 rows are 77% full, and 12 sequences read their keys for two of them.
 //
 // KP: 16-bit numbers of a weight.
 template <int TYPE, int DP, int TM, int W, int KP>
