@@ -160,11 +160,11 @@ __device__ __forceinline__ int path_length(const int32_t* p, int most, int draft
     }
 }
 
-// More is asked for than there is: who gets none leaves his to those behind him.  A
-// wavefront goes through the demands (`turn`) 64 at a time and leaves where each one's
-// pages begin among the `found`, or -1.  What is left never grows, so who asks for more
-// than is left is refused for good, and of the others all up to the first that does
-// not fit are served at once.
+// More pages are asked for than there are: a sequence that gets none takes none from
+// those behind it.  A wavefront goes through the demands (`turn`) 64 at a time and leaves
+// where each one's pages begin among the `found`, or -1.  What is left never grows, so a
+// demand of more than is left is refused for good, and of the others all up to the
+// first that does not fit are served at once.
 __device__ __forceinline__ void serve_in_turn(int32_t* turn, int seqs, int found) {
     const int lane = (int)threadIdx.x & 63;
     int left = found;
