@@ -181,6 +181,88 @@ rac_status rac_cache_commit(const rac_cache_config* cfg, void* pool, int32_t* ta
 rac_status rac_cache_copy(const rac_cache_config* cfg, const void* src_pool, const int32_t* src, void* dst_pool,
                           const int32_t* dst, int32_t n, rac_stream_t stream);
 
+/* ---- A bounded cache: what a token is worth, and eviction ------------------
+ * A cache that is full lets go of the tokens that received least attention.  The
+ * caller keeps, for every sequence, sums of the attention weight that each position
+ * received: one for all layers and heads (sets = 1), or one for every layer and
+ * key-value head (sets = layers * kv_heads, number layer * kv_heads + head), whose
+ * evictions may then choose different tokens:
+ *   weight       : fp32 [seqs][sets][positions], positions = max_pages * page_tokens
+ *   draft_weight : fp32 [sets][draft_rows], the drafted tokens'
+ * A round is rac_tree_attention and rac_tree_weights for every layer, rac_cache_commit,
+ * rac_cache_weights_commit, and rac_cache_evict.  rac_cache_fork knows nothing of
+ * weights: those of a sequence are those of its parent, a copy of rows. */
+
+/* Adds to the sums of layer `layer` what the rows of rac_tree_attention's call give
+ * to every key they see, with t, tree and cfg as there (t->v and t->out are not looked
+ * at, t->lse is read: the call's own):
+ *   weight[s][set][j] += sum_r sum_h exp(scale q_r,h . k_j - lse[r][h])
+ * over the sequence's rows and the query heads of the set (those of key-value head
+ * h, or all), for the committed positions j that have a page; in the same way
+ * draft_weight for the drafted tokens (NULL: not wanted).  Sums of what no row sees,
+ * positions without a page and rows outside every sequence are left as they are or get
+ * 0 added.  A row whose lse is -infinity gives nothing.  Products of 16-bit numbers,
+ * sums fp32.  A call gives the same bits every time; the order of a sum follows from
+ * the whole call.  Every drafted row counts, also one that is later not accepted.
+ *
+ * Alignments as in rac_tree_attention, weights 4-byte.  RAC_ERR_INVALID (also sets
+ * other than 1 or layers * kv_heads), _ALIGN, _UNSUPPORTED (as there, and seqs * sets *
+ * positions of 2^36 and more) and _CAPACITY.  Two kernel launches. */
+size_t rac_tree_weights_workspace(const rac_cache_config* cfg, const rac_tree_config* tree);
+
+rac_status rac_tree_weights(const rac_cache_config* cfg, const rac_tree_config* tree, int32_t layer, int32_t sets,
+                            const void* pool, const int32_t* table, const int32_t* lengths, const rac_tree_tensors* t,
+                            float* weight, float* draft_weight, void* workspace, size_t workspace_bytes,
+                            rac_stream_t stream);
+
+/* After rac_cache_commit: the sums of the committed[s] tokens at the end of every
+ * sequence become those of the drafted rows they came from (draft_weight NULL: 0).
+ * draft_start, path, max_path and draft_rows as given to the commit; lengths and
+ * committed as it left them.  One kernel launch. */
+rac_status rac_cache_weights_commit(const rac_cache_config* cfg, int32_t sets, const int32_t* lengths,
+                                    const int32_t* committed, const int32_t* draft_start, const int32_t* path,
+                                    int32_t max_path, const float* draft_weight, int32_t draft_rows, float* weight,
+                                    rac_stream_t stream);
+
+/* Every sequence s of more than keep[s] tokens (keep[s] >= 0) is cut to keep[s] of
+ * them, in all layers.  Let c_0 < c_1 < .. < c_(m-1) be its positions that have a page (m of them,
+ * the call's `places`) and n = keep[s] < m.  The last r = min(recent, n) places and the
+ * first f = min(first, n - r) stay; of those between, the n - f - r of the largest weight,
+ * ties to the lower place, a NaN below all numbers, for every set by itself.  Then
+ *   - the last r places move, in order, to positions n - r .. n - 1,
+ *   - of the others, those at a place below n - r are at that position, and
+ *   - those above it take the positions that are still free, in ascending order both.
+ * So most tokens stay where they are, and the last r keep their order; the attention
+ * does not depend on the order of what it sees, but a `window` and a later keep_from or
+ * keep_to count positions.  A sequence of no more places than keep[s] keeps its state.
+ *   keep    : int32 [seqs], negative: the sequence is not asked
+ *   evicted : int32 [seqs], receives m - n; 0 where the state was kept; -1 where it was
+ *             for want of pages
+ *   source  : int32 [seqs][sets][positions] or NULL, receives for every position below n
+ *             of a cut sequence where its token was (rotary positions and ages move along)
+ * weight moves along; the sums from n to the former length become 0.  A page that changes and
+ * that other sequences or entries share is replaced by a free one, so what they hold
+ * stays; sequences are served in order, each with the lowest-numbered pages that were
+ * free before the call, and one whose demand exceeds what those before it left keeps its
+ * state.  A sequence's pages that it shares with nobody are changed in place; pages past the
+ * cut are let go.  No other byte of the pool changes.
+ *
+ * pool 16-byte aligned, workspace 256-byte, the others 4-byte.  Five kernel launches at
+ * most.  RAC_ERR_INVALID, _ALIGN, _UNSUPPORTED (seqs * sets * positions of 2^36 and more)
+ * and _CAPACITY. */
+typedef struct {
+    int32_t sets;   /* 1, or layers * kv_heads                                      */
+    int32_t first;  /* first places that stay, 0..2^30 (attention sinks)            */
+    int32_t recent; /* last places that stay, 0..2^30                               */
+} rac_evict_config;
+
+/* Host-only, pure.  Bytes of the call's device scratch, or 0. */
+size_t rac_cache_evict_workspace(const rac_cache_config* cfg, const rac_evict_config* evict);
+
+rac_status rac_cache_evict(const rac_cache_config* cfg, const rac_evict_config* evict, void* pool, int32_t* table,
+                           int32_t* lengths, int32_t* refs, float* weight, const int32_t* keep, int32_t* evicted,
+                           int32_t* source, void* workspace, size_t workspace_bytes, rac_stream_t stream);
+
 /* ---- The reference predictor over drafted trees ---------------------------
  * rac_predictor_step (rac.h) for sequences whose history lies in a paged cache
  * and whose inputs are nodes of drafted trees.  Sender and receiver run it

@@ -179,6 +179,7 @@ def library():
         L.rac_status_string.argtypes = [ctypes.c_int]
         L.rac_status_string.restype = ctypes.c_char_p
         cache.declare(L)
+        tokens.declare(L)
         _lib = L
     return _lib
 
@@ -513,7 +514,8 @@ def rac_predictor_step(cfg: PredictorConfig, weights, cache, pos, h_prev, ref_ou
                                         rac_predictor_workspace_bytes(cfg), _stream(stream)), "rac_predictor_step")
 
 
-from . import cache  # noqa: E402  (its functions call the ones above)
+from . import cache, tokens  # noqa: E402  (their functions call the ones above)
 from .cache import *  # noqa: E402,F401,F403
+from .tokens import *  # noqa: E402,F401,F403
 
-__all__ += cache.__all__
+__all__ += cache.__all__ + tokens.__all__

@@ -25,6 +25,9 @@ HOST_SRC = os.path.join(HERE, "csrc", "spans.cpp")   # host-only C++ (reference 
 PRED_SRC = os.path.join(HERE, "csrc", "predictor.hip")  # decode-phase reference predictor
 CACHE_SRC = os.path.join(HERE, "csrc", "cache.hip")  # paged key-value cache
 TREE_SRC = os.path.join(HERE, "csrc", "tree.hip")    # attention of drafted trees over it
+WEIGHTS_SRC = os.path.join(HERE, "csrc", "weights.hip")  # attention weight that cached tokens receive
+EVICT_SRC = os.path.join(HERE, "csrc", "evict.hip")  # eviction by it
+TOKENS_SRC = os.path.join(HERE, "csrc", "tokens.hip")  # rotary positions, log probabilities of tokens
 INC = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "lib", "librac.so")
 
@@ -52,10 +55,10 @@ def build(verbose: bool = True) -> str:
         jobs.append([HIPCC, *compile_flags, *define, "-c", "-I", INC, "-o", objs[-1], SRC])
         jobs.append([HIPCC, *[f for f in compile_flags if f != "-fPIC"], *define, "--cuda-device-only", "-S",
                      "-I", INC, "-o", asms[-1], SRC])
-    for src in (PRED_SRC, HOST_SRC, CACHE_SRC, TREE_SRC):
+    for src in (PRED_SRC, HOST_SRC, CACHE_SRC, TREE_SRC, WEIGHTS_SRC, EVICT_SRC, TOKENS_SRC):
         objs.append(os.path.join(out, os.path.basename(src) + ".o"))
         jobs.append([HIPCC, *compile_flags, "-c", "-I", INC, "-o", objs[-1], src])
-    for src in (CACHE_SRC, TREE_SRC):
+    for src in (CACHE_SRC, TREE_SRC, WEIGHTS_SRC, EVICT_SRC, TOKENS_SRC):
         asms.append(os.path.join(out, os.path.basename(src) + ".s"))
         jobs.append([HIPCC, *[f for f in compile_flags if f != "-fPIC"], "--cuda-device-only", "-S", "-I", INC, "-o",
                      asms[-1], src])

@@ -24,7 +24,8 @@ __all__ = [
     "RAC_CACHE_BF16", "RAC_CACHE_FP16", "RAC_CACHE_FP8", "CacheConfig", "TreeConfig", "rac_cache_pool_bytes",
     "rac_cache_new", "rac_tree_attention_workspace", "rac_tree_attention", "rac_cache_fork",
     "rac_cache_commit_workspace", "rac_cache_commit", "rac_cache_copy", "rac_predictor_tree_workspace",
-    "rac_predictor_tree_step",
+    "rac_predictor_tree_step", "EvictConfig", "rac_tree_weights_workspace", "rac_tree_weights",
+    "rac_cache_weights_commit", "rac_cache_evict_workspace", "rac_cache_evict",
 ]
 
 RAC_CACHE_BF16 = 0
@@ -47,6 +48,10 @@ class _TreeTensors(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "q_start", "draft_start", "mask", "out", "lse")] + \
                [(n, ctypes.c_int64) for n in ("q_stride", "kv_stride", "out_stride")] + \
                [(n, ctypes.c_int32) for n in ("draft_rows", "mask_words")]
+
+
+class _EvictConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("sets", "first", "recent")]
 
 
 class _Kept:
@@ -114,10 +119,29 @@ class TreeConfig(_Kept):
         return ctypes.byref(self._struct)
 
 
+@dataclass(frozen=True)
+class EvictConfig(_Kept):
+    sets: int = 1
+    first: int = 0
+    recent: int = 0
+
+    def _c(self) -> _EvictConfig:
+        return self._struct
+
+    @functools.cached_property
+    def _struct(self) -> _EvictConfig:
+        return _EvictConfig(self.sets, self.first, self.recent)
+
+    @functools.cached_property
+    def _ref(self):
+        return ctypes.byref(self._struct)
+
+
 def declare(L) -> None:
     """The argument types of the library's cache functions."""
     cp, tp, vp, i32, i64 = (ctypes.POINTER(_CacheConfig), ctypes.POINTER(_TreeConfig), ctypes.c_void_p,
                             ctypes.c_int32, ctypes.c_int64)
+    ep = ctypes.POINTER(_EvictConfig)
     sz = ctypes.c_size_t
     for name, args, res in (
             ("rac_cache_pool_bytes", [cp], sz),
@@ -128,6 +152,12 @@ def declare(L) -> None:
             ("rac_cache_commit", [cp, vp, vp, vp, vp, vp, vp, i64, i64, i32, vp, vp, i32, vp, vp, sz, vp],
              ctypes.c_int),
             ("rac_cache_copy", [cp, vp, vp, vp, vp, i32, vp], ctypes.c_int),
+            ("rac_tree_weights_workspace", [cp, tp], sz),
+            ("rac_tree_weights", [cp, tp, i32, i32, vp, vp, vp, ctypes.POINTER(_TreeTensors), vp, vp, vp, sz, vp],
+             ctypes.c_int),
+            ("rac_cache_weights_commit", [cp, i32, vp, vp, vp, vp, i32, vp, i32, vp, vp], ctypes.c_int),
+            ("rac_cache_evict_workspace", [cp, ep], sz),
+            ("rac_cache_evict", [cp, ep, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp], ctypes.c_int),
             ("rac_predictor_tree_workspace", [ctypes.POINTER(_rac._PredConfig), cp, tp], sz),
             ("rac_predictor_tree_step", [ctypes.POINTER(_rac._PredConfig), cp, tp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32,
                                          vp, vp, vp, i32, vp, vp, sz, vp], ctypes.c_int)):
@@ -292,6 +322,105 @@ def rac_cache_copy(cfg: CacheConfig, src_pool, src, dst_pool, dst, n: int | None
         cfg._ref, _pool(cfg, src_pool, "src_pool"), _rac._dev(src, "src", 4, count),
         _pool(cfg, dst_pool, "dst_pool"), _rac._dev(dst, "dst", 4, count), count, _rac._stream(stream)),
         "rac_cache_copy")
+
+
+def _sums(cfg: CacheConfig, weight, what: str = "weight") -> int:
+    """Sets of a tensor of sums, [seqs][sets][positions]."""
+    try:
+        seqs, sets, positions = weight.shape
+    except (AttributeError, ValueError):
+        raise ValueError(f"{what}: expected a GPU tensor, [{cfg.seqs}][sets][{cfg.max_pages * cfg.page_tokens}]") from None
+    if seqs != cfg.seqs or positions != cfg.max_pages * cfg.page_tokens or sets not in (1, cfg.layers * cfg.kv_heads):
+        raise ValueError(f"{what}: expected [{cfg.seqs}][1 or {cfg.layers * cfg.kv_heads}]"
+                         f"[{cfg.max_pages * cfg.page_tokens}], got {list(weight.shape)}")
+    return sets
+
+
+def _draft_sums(draft_weight, sets: int, rows: int):
+    """Address of the drafted tokens' sums, [sets][rows]."""
+    if draft_weight is not None and tuple(getattr(draft_weight, "shape", ())) != (sets, rows):
+        raise ValueError(f"draft_weight: expected a GPU tensor, [{sets}][{rows}]")
+    return _rac._dev(draft_weight, "draft_weight", 4, sets * rows)
+
+
+def rac_tree_weights_workspace(cfg: CacheConfig, tree: TreeConfig) -> int:
+    # (as that of the attention)
+    last = tree.__dict__.get("_weights_workspace")
+    if last is None or last[0] is not cfg:
+        last = cfg, int(_rac.library().rac_tree_weights_workspace(cfg._ref, tree._ref))
+        tree.__dict__["_weights_workspace"] = last
+    return last[1]
+
+
+def rac_tree_weights(cfg: CacheConfig, tree: TreeConfig, layer: int, pool, table, lengths, q, q_start, k, lse, weight,
+                     workspace, *, draft_weight=None, draft_start=None, mask=None, stream=None) -> None:
+    """Adds the attention weight that the call of rac_tree_attention with the same
+    arguments gives to the committed tokens to weight (fp32 [seqs][sets][positions],
+    sets 1 or layers * kv_heads) and to the drafted ones to draft_weight (fp32
+    [sets][draft_rows]).  lse: fp32 [rows][q_heads], from that call."""
+    dev = _rac._dev
+    R, Q, H, D, S = tree.rows, tree.q_heads, cfg.kv_heads, cfg.head_dim, cfg.seqs
+    sets = _sums(cfg, weight)
+    qp, qs, _ = _rows(q, "q", R, Q, D)
+    kp, ks, drafted = _drafts(k, "k", 0, H, D)
+    words = _words(mask)
+    t = _TreeTensors(qp, kp, None, dev(q_start, "q_start", 4, S + 1), dev(draft_start, "draft_start", 4, S + 1),
+                     dev(mask, "mask", 8, R * words), None, dev(lse, "lse", 4, R * Q), qs, ks, Q * D, drafted, words)
+    need = rac_tree_weights_workspace(cfg, tree)
+    status = _rac.library().rac_tree_weights(
+        cfg._ref, tree._ref, layer, sets, _pool(cfg, pool), dev(table, "table", 4, S * cfg.max_pages),
+        dev(lengths, "lengths", 4, S), ctypes.byref(t), dev(weight, "weight", 4, 0),
+        _draft_sums(draft_weight, sets, drafted), dev(workspace, "workspace", 1, need), need, _rac._stream(stream))
+    if status:
+        _rac._check(status, "rac_tree_weights")
+
+
+def rac_cache_weights_commit(cfg: CacheConfig, lengths, committed, draft_start, draft_weight, weight, *, path=None,
+                             max_path: int | None = None, draft_rows: int | None = None, stream=None) -> None:
+    """After rac_cache_commit: the sums of the appended tokens in weight become those
+    of the rows they came from in draft_weight (None: zeros; then draft_rows says how
+    many rows there were)."""
+    dev, S, sets = _rac._dev, cfg.seqs, _sums(cfg, weight)
+    if draft_rows is None:
+        draft_rows = 0 if draft_weight is None else int(draft_weight.shape[-1])
+    if max_path is None:
+        if isinstance(path, int):
+            raise ValueError("path: an address needs max_path beside it")
+        max_path = draft_rows if path is None else int(path.shape[-1])
+    elif S > 1 and path is not None and not isinstance(path, int) and path.dim() > 1 and path.shape[-1] != max_path:
+        raise ValueError(f"path: its rows have {path.shape[-1]} entries, but max_path is {max_path}")
+    _rac._check(_rac.library().rac_cache_weights_commit(
+        cfg._ref, sets, dev(lengths, "lengths", 4, S), dev(committed, "committed", 4, S),
+        dev(draft_start, "draft_start", 4, S + 1), dev(path, "path", 4, S * int(max_path)), int(max_path),
+        _draft_sums(draft_weight, sets, draft_rows), int(draft_rows), dev(weight, "weight", 4, 0), _rac._stream(stream)),
+        "rac_cache_weights_commit")
+
+
+def rac_cache_evict_workspace(cfg: CacheConfig, evict: EvictConfig) -> int:
+    last = evict.__dict__.get("_workspace")
+    if last is None or last[0] is not cfg:
+        last = cfg, int(_rac.library().rac_cache_evict_workspace(cfg._ref, evict._ref))
+        evict.__dict__["_workspace"] = last
+    return last[1]
+
+
+def rac_cache_evict(cfg: CacheConfig, evict: EvictConfig, pool, table, lengths, refs, weight, keep, evicted, workspace, *,
+                    source=None, stream=None) -> None:
+    """Cuts every sequence s to keep[s] tokens (int32 [seqs], negative: not asked): the
+    first and last ones of `evict` and those of the largest weight (fp32 [seqs][sets]
+    [positions]).  evicted: int32 [seqs], tokens let go, -1 for want of pages; source:
+    int32, as weight, former positions."""
+    dev, S = _rac._dev, cfg.seqs
+    if _sums(cfg, weight) != evict.sets:
+        raise ValueError(f"weight: expected {evict.sets} sets, got {weight.shape[1]}")
+    need = rac_cache_evict_workspace(cfg, evict)
+    status = _rac.library().rac_cache_evict(
+        cfg._ref, evict._ref, _pool(cfg, pool), dev(table, "table", 4, S * cfg.max_pages), dev(lengths, "lengths", 4, S),
+        dev(refs, "refs", 4, cfg.pages), dev(weight, "weight", 4, 0), dev(keep, "keep", 4, S),
+        dev(evicted, "evicted", 4, S), dev(source, "source", 4, weight.numel()), dev(workspace, "workspace", 1, need), need,
+        _rac._stream(stream))
+    if status:
+        _rac._check(status, "rac_cache_evict")
 
 
 def rac_predictor_tree_workspace(cfg, cache: CacheConfig, tree: TreeConfig) -> int:

@@ -160,29 +160,6 @@ __device__ __forceinline__ int path_length(const int32_t* p, int most, int draft
     }
 }
 
-// More pages are asked for than there are: a sequence that gets none takes none from
-// those behind it.  A wavefront goes through the demands (`turn`) 64 at a time and leaves
-// where each one's pages begin among the `found`, or -1.  What is left never grows, so a
-// demand of more than is left is refused for good, and of the others all up to the
-// first that does not fit are served at once.
-__device__ __forceinline__ void serve_in_turn(int32_t* turn, int seqs, int found) {
-    const int lane = (int)threadIdx.x & 63;
-    int left = found;
-    for (int s0 = 0; s0 < seqs; s0 += 64) {
-        const int n = s0 + lane < seqs ? turn[s0 + lane] : 0;
-        int at = -1;
-        for (int first = 0; first < 64;) {  // (lanes from `first` on are not served yet)
-            const bool can = lane >= first && n <= left;
-            const int sum = scan_wave(can ? n : 0);
-            const uint64_t over = __ballot(can && sum > left);
-            first = over ? __builtin_ctzll(over) : 64;
-            if (can && lane < first) at = found - left + sum - n;
-            left -= __builtin_amdgcn_readlane(sum, first - 1);  // (the first that can fits)
-        }
-        if (s0 + lane < seqs) turn[s0 + lane] = at;
-    }
-}
-
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
     __shared__ int sums[kPlanWaves];
     __shared__ int32_t near[kNear];  // the first free pages (the others through memory)

@@ -31,6 +31,14 @@ inline uint64_t cache_page_bytes(const rac_cache_config* c) {
            (uint64_t)cache_elem_bytes(c);
 }
 
+// Sums of attention weight: one for all layers and heads, or one for each.
+inline bool sets_valid(const rac_cache_config* c, int32_t sets) {
+    return sets == 1 || sets == c->layers * c->kv_heads;
+}
+inline bool sums_counted(const rac_cache_config* c, int32_t sets) {
+    return (int64_t)c->seqs * sets <= ((int64_t(1) << 36) - 1) / ((int64_t)c->max_pages * c->page_tokens);
+}
+
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 inline int log2_of(int v) { return __builtin_ctz((unsigned)v); }
@@ -79,6 +87,29 @@ __device__ __forceinline__ int scan_workgroup(int v, int* sums, int* total) {
     }
     *total = all;
     return (int)(before + (uint32_t)x - (uint32_t)v);
+}
+
+// More pages are asked for than there are: a sequence that gets none takes none from
+// those behind it.  A wavefront goes through the demands (`turn`) 64 at a time and leaves
+// where each one's pages begin among the `found`, or -1.  What is left never grows, so a
+// demand of more than is left is refused for good, and of the others all up to the
+// first that does not fit are served at once.
+__device__ __forceinline__ void serve_in_turn(int32_t* turn, int seqs, int found) {
+    const int lane = (int)threadIdx.x & 63;
+    int left = found;
+    for (int s0 = 0; s0 < seqs; s0 += 64) {
+        const int n = s0 + lane < seqs ? turn[s0 + lane] : 0;
+        int at = -1;
+        for (int first = 0; first < 64;) {  // (lanes from `first` on are not served yet)
+            const bool can = lane >= first && n <= left;
+            const int sum = scan_wave(can ? n : 0);
+            const uint64_t over = __ballot(can && sum > left);
+            first = over ? __builtin_ctzll(over) : 64;
+            if (can && lane < first) at = found - left + sum - n;
+            left -= __builtin_amdgcn_readlane(sum, first - 1);  // (the first that can fits)
+        }
+        if (s0 + lane < seqs) turn[s0 + lane] = at;
+    }
 }
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

@@ -1,0 +1,609 @@
+// evict.hip - gfx950 kernels and C ABI of eviction from the paged cache by
+// accumulated attention weight.  The contract is in include/rac_cache.h.
+//
+// A kept token moves only if it lies past the cut, into a place that an evicted one
+// left: so a round that evicts a few tokens moves a few, sources and targets never
+// meet, and most shared pages stay shared.  Only the last `recent` tokens shift, in order.
+#include "cache_common.h"
+
+namespace {
+
+// What the first launch finds out about a sequence.  Places are its positions that
+// have a page, in order.
+struct EvictRecord {
+    int32_t cut;      // whether it is to be cut
+    int32_t n, m;     // tokens that stay, places before
+    int32_t length;   // positions before
+    int32_t border;   // n - recent: from here on the last tokens go, in order
+    int32_t pages;    // that it has
+    int32_t gaps;     // whether some position has no page
+    int32_t demand;   // pages to be replaced
+    int32_t base;     // where its pages begin in the list of free ones, -1: refused
+};
+
+struct EvictArgs {
+    uint8_t* pool;
+    int32_t* table;
+    int32_t* lengths;
+    int32_t* refs;
+    float* weight;
+    const int32_t* keep;
+    int32_t* evicted;
+    int32_t* source;
+    EvictRecord* record;  // [seqs]
+    int32_t* old_page;    // [seqs][max_pages], of the places' pages: number,
+    int32_t* old_at;      // where in the table,
+    int32_t* fresh;       // and which of the demanded pages replaces it, or -1
+    int32_t* free_list;   // [pages]
+    int32_t* list;        // [seqs][sets][positions]: holes from the front, what fills them from the back
+    int32_t* holes;       // [seqs][sets]
+    uint64_t* hole_bits;  // [seqs][sets][words]
+    int64_t positions, words;
+    int32_t layers, heads, row_bytes, log_page, pages, seqs, max_pages, sets, first, recent, parts;
+
+    __device__ __forceinline__ int64_t sums(int s, int set) const { return ((int64_t)s * sets + set); }
+    // The position of a place.
+    __device__ __forceinline__ int position(const EvictRecord& r, int s, int place) const {
+        if (!r.gaps) return place;
+        return (old_at[(int64_t)s * max_pages + (place >> log_page)] << log_page) | (place & ((1 << log_page) - 1));
+    }
+    __device__ __forceinline__ int page_now(const EvictRecord& r, int s, int d) const {
+        const int64_t at = (int64_t)s * max_pages + d;
+        const int f = fresh[at];
+        return f < 0 ? old_page[at] : free_list[r.base + f];
+    }
+    __device__ __forceinline__ uint8_t* row_of(int page, int layer, int side, int head, int place) const {
+        const uint64_t plane = ((uint64_t)page * layers + layer) * 2 * heads + (uint64_t)side * heads + head;
+        return pool + (plane << log_page) * row_bytes + (uint64_t)(place & ((1 << log_page) - 1)) * row_bytes;
+    }
+};
+
+// Weights in an order of whole numbers; a NaN is below all.
+__device__ __forceinline__ uint32_t rank_of(float x) {
+    const uint32_t u = __float_as_uint(x + 0.0f);  // (-0 is 0)
+    return x != x ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// ---------------------------------------------------------------------------
+// First launch: a workgroup a sequence and set.  The places of the sequence; the
+// weight that divides what stays from what goes, digit by digit from the top (counts of
+// 2048 values in LDS); and, in one ordered pass, the holes and what fills them.
+constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64, kDigit = 2048;
+
+__global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a) {
+    __shared__ int32_t count[kDigit];
+    __shared__ int32_t sums[kPickWaves], more[kPickWaves], found[3];
+    const int t = (int)threadIdx.x, lane = t & 63, wv = t / 64, page = 1 << a.log_page;
+    const uint64_t below = (uint64_t(1) << lane) - 1;
+    const int s = (int)blockIdx.y;
+    for (int set = (int)blockIdx.x; set < a.sets; set += (int)gridDim.x) {
+        EvictRecord r{};
+        r.length = clamp_int(a.lengths[s], 0, a.max_pages << a.log_page);
+        const int keep = a.keep[s], used = (r.length + page - 1) >> a.log_page;
+        const int32_t* const row = a.table + (int64_t)s * a.max_pages;
+        __syncthreads();
+        // how many positions have a page
+        int mine = 0, all;
+        for (int d = t; d < used; d += kPickThreads) mine += (uint32_t)row[d] < (uint32_t)a.pages;
+        scan_workgroup<kPickWaves>(mine, sums, &all);
+        r.pages = all;
+        r.gaps = all != used;
+        const int tail = r.length & (page - 1);
+        const bool whole = tail == 0 || (uint32_t)row[used - 1] >= (uint32_t)a.pages;
+        r.m = (all << a.log_page) - (whole ? 0 : page - tail);
+        r.cut = keep >= 0 && r.m > keep;
+        r.n = r.cut ? keep : r.m;
+        const int recent = a.recent < r.n ? a.recent : r.n, first = a.first < r.n - recent ? a.first : r.n - recent;
+        r.border = r.n - recent;
+        if (set == 0 && t == 0) a.record[s] = r;
+        if (!r.cut) continue;
+        if (set == 0 || r.gaps) {  // (with gaps every set needs the places: they write the same)
+            int at = 0;
+            for (int d0 = 0; d0 < used; d0 += kPickThreads) {
+                const int p = d0 + t < used ? row[d0 + t] : -1;
+                const bool is = (uint32_t)p < (uint32_t)a.pages;
+                const int to = at + scan_workgroup<kPickWaves>(is, sums, &all);
+                if (is) {
+                    a.old_page[(int64_t)s * a.max_pages + to] = p;
+                    a.old_at[(int64_t)s * a.max_pages + to] = d0 + t;
+                }
+                at += all;
+            }
+            __syncthreads();
+        }
+        const float* const w = a.weight + a.sums(s, set) * a.positions;
+        const int lo = first, hi = r.m - recent;  // the places to choose from
+        int left = r.n - recent - first;          // how many of them stay
+        uint32_t bar = ~0u;                       // (no weight has this rank)
+        bool ties = false;                        // whether not all of those at the bar stay
+        if (left > 0) {
+            bar = 0;
+            for (int digit = 0; digit < 3; ++digit) {
+                const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
+                for (int i = t; i < kDigit; i += kPickThreads) count[i] = 0;
+                __syncthreads();
+                for (int p0 = lo; p0 < hi; p0 += kPickThreads) {
+                    const int p = p0 + t;
+                    bool in = p < hi;
+                    uint32_t v = 0;
+                    if (in) {
+                        const uint32_t k = rank_of(w[a.position(r, s, p)]);
+                        in = digit == 0 || (k >> (shift + bits)) == (bar >> (shift + bits));
+                        v = (k >> shift) & ((1u << bits) - 1);
+                    }
+                    // (weights that are alike, zeros for one, would queue up at one counter)
+                    const uint64_t who = __ballot(in);
+                    if (!who) continue;
+                    const uint32_t one = __builtin_amdgcn_readlane(v, __builtin_ctzll(who));
+                    const uint64_t same = __ballot(in && v == one);
+                    if (lane == __builtin_ctzll(who)) atomicAdd(count + one, __popcll(same));
+                    if (in && v != one) atomicAdd(count + v, 1);
+                }
+                __syncthreads();
+                // the digit at which the counts from the top reach `left`
+                const int c1 = count[kDigit - 1 - 2 * t], c0 = count[kDigit - 2 - 2 * t];
+                const int above = scan_workgroup<kPickWaves>(c0 + c1, sums, &all);
+                if (above < left && left <= above + c1) {
+                    found[0] = kDigit - 1 - 2 * t;
+                    found[1] = above;
+                    found[2] = c1;
+                } else if (above + c1 < left && left <= above + c1 + c0) {
+                    found[0] = kDigit - 2 - 2 * t;
+                    found[1] = above + c1;
+                    found[2] = c0;
+                }
+                __syncthreads();
+                bar |= (uint32_t)found[0] << shift;
+                left -= found[1];
+                ties = found[2] > left;
+                __syncthreads();
+            }
+        }
+        // in the order of places: holes before the border, what stays behind it
+        int32_t* const list = a.list + a.sums(s, set) * a.positions;
+        uint64_t* const bits = a.hole_bits + a.sums(s, set) * a.words;
+        constexpr int kSteps = 4;
+        int nh = 0, nf = 0, nt = 0;
+        for (int p0 = 0; p0 < hi; p0 += kPickThreads * kSteps) {
+            uint64_t hole[kSteps], fill[kSteps], tie[kSteps];
+            uint32_t k[kSteps];
+            int h = 0, f = 0, e = 0;
+#pragma unroll
+            for (int y = 0; y < kSteps; ++y) {
+                const int p = p0 + wv * 64 * kSteps + 64 * y + lane;
+                k[y] = 0;
+                if (p >= lo && p < hi) k[y] = rank_of(w[a.position(r, s, p)]);
+            }
+#pragma unroll
+            for (int y = 0; y < kSteps; ++y) {
+                const int p = p0 + wv * 64 * kSteps + 64 * y + lane;
+                tie[y] = __ballot(p >= lo && p < hi && k[y] == bar);
+                e += __popcll(tie[y]);
+            }
+            int before = nt;
+            if (ties) {
+                __syncthreads();
+                if (lane == 0) sums[wv] = e;
+                __syncthreads();
+                for (int x = 0; x < kPickWaves; ++x) {
+                    before += x < wv ? sums[x] : 0;
+                    nt += sums[x];
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < kSteps; ++y) {
+                const int p = p0 + wv * 64 * kSteps + 64 * y + lane;
+                const bool at_bar = (tie[y] >> lane) & 1;
+                const bool stays = p < lo || k[y] > bar || (at_bar && (!ties || before + __popcll(tie[y] & below) < left));
+                before += __popcll(tie[y]);
+                hole[y] = __ballot(p < r.border && !stays);
+                fill[y] = __ballot(p >= r.border && p < hi && stays);
+                h += __popcll(hole[y]);
+                f += __popcll(fill[y]);
+            }
+            __syncthreads();
+            if (lane == 0) {
+                sums[wv] = h;
+                more[wv] = f;
+            }
+            __syncthreads();
+            int ah = nh, af = nf;
+            for (int x = 0; x < kPickWaves; ++x) {
+                ah += x < wv ? sums[x] : 0;
+                af += x < wv ? more[x] : 0;
+                nh += sums[x];
+                nf += more[x];
+            }
+#pragma unroll
+            for (int y = 0; y < kSteps; ++y) {
+                const int q = p0 + wv * 64 * kSteps + 64 * y, p = q + lane;
+                if ((hole[y] >> lane) & 1) list[ah + __popcll(hole[y] & below)] = p;
+                if ((fill[y] >> lane) & 1) list[a.positions - 1 - (af + __popcll(fill[y] & below))] = p;
+                if (lane == 0 && q < r.border) bits[q / 64] = hole[y];
+                ah += __popcll(hole[y]);
+                af += __popcll(fill[y]);
+            }
+        }
+        if (t == 0) a.holes[a.sums(s, set)] = nh;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Second launch: a workgroup a sequence finds the shared pages that change in any set.
+constexpr int kDemandThreads = 256;
+
+__global__ __launch_bounds__(kDemandThreads) void evict_demand_kernel(EvictArgs a) {
+    __shared__ int32_t sums[kDemandThreads / 64];
+    const int s = (int)blockIdx.y, t = (int)threadIdx.x, page = 1 << a.log_page;
+    const EvictRecord r = a.record[s];
+    if (!r.cut) return;
+    const int used = (r.n + page - 1) >> a.log_page;
+    int demand = 0;
+    for (int d0 = 0; d0 < used; d0 += kDemandThreads) {
+        const int d = d0 + t;
+        bool change = false;
+        if (d < used && a.refs[a.old_page[(int64_t)s * a.max_pages + d]] > 1) {
+            change = ((d + 1) << a.log_page) > r.border && r.border < r.n;
+            const int p0 = d << a.log_page, p1 = p0 + page < r.border ? p0 + page : r.border;
+            for (int set = 0; set < a.sets && !change; ++set) {
+                const uint64_t* const bits = a.hole_bits + a.sums(s, set) * a.words;
+                for (int p = p0; p < p1; p += 64) {
+                    const uint64_t b = bits[p / 64] >> (p & 63);
+                    change |= (page >= 64 ? b : b & ((uint64_t(1) << page) - 1)) != 0;
+                }
+            }
+        }
+        int all;
+        const int at = demand + scan_workgroup<kDemandThreads / 64>(change, sums, &all);
+        if (d < used) a.fresh[(int64_t)s * a.max_pages + d] = change ? at : -1;
+        demand += all;
+    }
+    if (t == 0) a.record[s].demand = demand;
+}
+
+// ---------------------------------------------------------------------------
+// Third launch: one workgroup hands out the free pages, the lowest first, to the
+// sequences in order.
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+
+__global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
+    constexpr int kPer = 4;  // sequences a thread (4096 / 1024)
+    __shared__ int32_t sums[kPlanWaves];
+    __shared__ int32_t turn[kPer * kPlanThreads];
+    const int t = (int)threadIdx.x, lane = t & 63;
+    EvictRecord r[kPer];
+    int need[kPer], base[kPer], demand = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int s = t + i * kPlanThreads;
+        need[i] = base[i] = 0;
+        r[i].cut = 0;
+        if (i * kPlanThreads >= a.seqs) continue;
+        if (s < a.seqs) {
+            r[i] = a.record[s];
+            if (r[i].cut) need[i] = r[i].demand;
+        }
+        int all;
+        base[i] = (int)((uint32_t)demand + (uint32_t)scan_workgroup<kPlanWaves>(need[i], sums, &all));
+        demand = all < kMostSum - demand ? demand + all : kMostSum;
+    }
+    int found = 0;
+    constexpr int kEach = 16, kStep = kPlanThreads * kEach;
+    for (int p0 = 0; p0 < a.pages && found < demand; p0 += kStep) {
+        uint64_t free[kEach];
+        int mine = 0;
+        const int own = p0 + t / 64 * (64 * kEach) + lane;
+        int ref[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) ref[i] = own + 64 * i < a.pages ? a.refs[own + 64 * i] : 1;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            free[i] = __ballot(ref[i] == 0);
+            mine += __popcll(free[i]);
+        }
+        __syncthreads();
+        if (lane == 0) sums[t / 64] = mine;
+        __syncthreads();
+        int at = found;
+        for (int w = 0; w < kPlanWaves; ++w) {
+            at += w < t / 64 ? sums[w] : 0;
+            found += sums[w];
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int k = at + __popcll(free[i] & ((uint64_t(1) << lane) - 1));
+            if (ref[i] == 0 && k < demand) a.free_list[k] = own + 64 * i;
+            at += __popcll(free[i]);
+        }
+    }
+    if (demand > found) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (t + i * kPlanThreads < a.seqs) turn[t + i * kPlanThreads] = need[i];
+        __syncthreads();
+        if (t < 64) serve_in_turn(turn, a.seqs, found);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (t + i * kPlanThreads < a.seqs) base[i] = turn[t + i * kPlanThreads];
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int s = t + i * kPlanThreads;
+        if (s >= a.seqs) continue;
+        a.record[s].base = base[i];
+        a.evicted[s] = !r[i].cut ? 0 : base[i] < 0 ? -1 : r[i].m - r[i].n;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Fourth launch: keys and values that fill holes, and those of replaced pages that
+// stay where they are.  `parts` workgroups a (sequence, layer, head).
+//
+// Bound by the bytes that move, each read and written once.
+constexpr int kMoveThreads = 256;
+
+// A thread's part of the rows that move: 16 bytes of a row's keys or values, always the
+// same, and every how many-th row.
+struct Lane {
+    int first, step;  // row, rows at once
+    int side, byte;
+    bool on;
+
+    __device__ __forceinline__ explicit Lane(int row_bytes, int threads) {
+        const int each = row_bytes / 8;  // pieces of keys and values
+        step = threads / each;
+        first = (int)threadIdx.x / each;
+        const int in = (int)threadIdx.x - first * each;
+        side = in >= each / 2;
+        byte = (in - side * (each / 2)) * 16;
+        on = first < step;
+    }
+};
+
+__device__ void move_unit(const EvictArgs& a, const EvictRecord& r, int s, int lh, int part) {
+    const int layer = lh / a.heads, head = lh - layer * a.heads, set = a.sets > 1 ? lh : 0, page = 1 << a.log_page;
+    const Lane l(a.row_bytes, kMoveThreads);
+    if (!l.on) return;
+    const int32_t* const list = a.list + a.sums(s, set) * a.positions;
+    const int32_t* const old_page = a.old_page + (int64_t)s * a.max_pages;
+    const int holes = a.holes[a.sums(s, set)];
+    constexpr int kAtOnce = 4;
+    for (int64_t e0 = part * l.step + l.first; e0 < holes; e0 += (int64_t)a.parts * l.step * kAtOnce) {
+        u32x4 x[kAtOnce];
+        uint8_t* to[kAtOnce];
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) {
+            const int64_t e = e0 + (int64_t)y * a.parts * l.step;
+            if (e >= holes) continue;
+            const int from = list[a.positions - 1 - e], hole = list[e];
+            x[y] = *reinterpret_cast<const u32x4*>(a.row_of(old_page[from >> a.log_page], layer, l.side, head, from) + l.byte);
+            to[y] = a.row_of(a.page_now(r, s, hole >> a.log_page), layer, l.side, head, hole) + l.byte;
+        }
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y)
+            if (e0 + (int64_t)y * a.parts * l.step < holes) *reinterpret_cast<u32x4*>(to[y]) = x[y];
+    }
+    if (r.demand == 0) return;
+    const uint64_t* const bits = a.hole_bits + a.sums(s, set) * a.words;
+    for (int d = part; (d << a.log_page) < r.border; d += a.parts) {
+        if (a.fresh[(int64_t)s * a.max_pages + d] < 0) continue;
+        const int now = a.page_now(r, s, d), was = old_page[d], p0 = d << a.log_page;
+        const int p1 = p0 + page < r.border ? p0 + page : r.border;
+        for (int p = p0 + l.first; p < p1; p += l.step) {
+            if ((bits[p / 64] >> (p & 63)) & 1) continue;
+            *reinterpret_cast<u32x4*>(a.row_of(now, layer, l.side, head, p) + l.byte) =
+                *reinterpret_cast<const u32x4*>(a.row_of(was, layer, l.side, head, p) + l.byte);
+        }
+    }
+}
+
+__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
+    const int s = (int)blockIdx.y;
+    const EvictRecord r = a.record[s];
+    if (!r.cut || r.base < 0) return;
+    for (int i = (int)blockIdx.x; i < a.layers * a.heads * a.parts; i += (int)gridDim.x) {
+        const int lh = i / a.parts;
+        move_unit(a, r, s, lh, i - lh * a.parts);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Last launch, what the moves had to be ahead of: the last tokens shift, a workgroup a
+// (sequence, layer, head), read ahead of where they are written; the sums of weights,
+// a workgroup a (sequence, set); table, counts and lengths, a workgroup a sequence.
+constexpr int kEndThreads = 256;
+
+__device__ void shift_recent(const EvictArgs& a, const EvictRecord& r, int s, int layer, int head) {
+    const int by = r.m - r.n;
+    const Lane l(a.row_bytes, kEndThreads);
+    const int32_t* const old_page = a.old_page + (int64_t)s * a.max_pages;
+    constexpr int kAtOnce = 4;
+    for (int p0 = r.border; p0 < r.n; p0 += l.step * kAtOnce) {
+        u32x4 x[kAtOnce];
+        uint8_t* to[kAtOnce];
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) {
+            const int p = p0 + y * l.step + l.first, from = p + by;
+            if (!l.on || p >= r.n) continue;
+            x[y] = *reinterpret_cast<const u32x4*>(a.row_of(old_page[from >> a.log_page], layer, l.side, head, from) + l.byte);
+            to[y] = a.row_of(a.page_now(r, s, p >> a.log_page), layer, l.side, head, p) + l.byte;
+        }
+        __syncthreads();  // (a token's place may be the source of an earlier one's)
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y)
+            if (l.on && p0 + y * l.step + l.first < r.n) *reinterpret_cast<u32x4*>(to[y]) = x[y];
+    }
+}
+
+// w[to + i] = w[at(i)], i < n, where no at(i) lies before to + i, or before an at of a smaller i.
+template <class At>
+__device__ __forceinline__ void shift_sums(float* w, int to, int n, At at) {
+    constexpr int kAtOnce = 4;
+    for (int i0 = 0; i0 < n; i0 += kEndThreads * kAtOnce) {
+        float x[kAtOnce];
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) {
+            const int i = i0 + y * kEndThreads + (int)threadIdx.x;
+            if (i < n) x[y] = w[at(i)];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) {
+            const int i = i0 + y * kEndThreads + (int)threadIdx.x;
+            if (i < n) w[to + i] = x[y];
+        }
+    }
+    __syncthreads();
+}
+
+__device__ void move_sums(const EvictArgs& a, const EvictRecord& r, int s, int set) {
+    const int t = (int)threadIdx.x;
+    const int64_t of = a.sums(s, set) * a.positions;
+    float* const w = a.weight + of;
+    const int32_t* const list = a.list + of;
+    const int holes = a.holes[a.sums(s, set)], by = r.m - r.n;
+    if (a.source) {
+        int32_t* const source = a.source + of;
+        for (int p = t; p < r.n; p += kEndThreads) source[p] = a.position(r, s, p < r.border ? p : p + by);
+        __syncthreads();
+        for (int e = t; e < holes; e += kEndThreads) source[list[e]] = a.position(r, s, list[a.positions - 1 - e]);
+    }
+    if (r.gaps) shift_sums(w, 0, r.m, [&](int i) { return a.position(r, s, i); });
+    for (int e = t; e < holes; e += kEndThreads) w[list[e]] = w[list[a.positions - 1 - e]];
+    __syncthreads();
+    shift_sums(w, r.border, r.n - r.border, [&](int i) { return r.border + by + i; });
+    for (int p = r.n + t; p < r.length; p += kEndThreads) w[p] = 0.0f;
+}
+
+__device__ void enter_pages(const EvictArgs& a, const EvictRecord& r, int s) {
+    const int t = (int)threadIdx.x, page = 1 << a.log_page;
+    const int used = (r.n + page - 1) >> a.log_page, before = (r.length + page - 1) >> a.log_page;
+    int32_t* const row = a.table + (int64_t)s * a.max_pages;
+    for (int d = t; d < before; d += kEndThreads) {
+        const int64_t at = (int64_t)s * a.max_pages + d;
+        int now = -1;
+        if (d < r.pages) {
+            const int was = a.old_page[at];
+            now = d < used ? a.page_now(r, s, d) : -1;
+            if (now != was) atomicAdd(a.refs + was, -1);
+            if (now >= 0 && now != was) a.refs[now] = 1;
+        }
+        row[d] = now;
+    }
+    if (t == 0) a.lengths[s] = r.n;
+}
+
+__global__ __launch_bounds__(kEndThreads) void evict_end_kernel(EvictArgs a) {
+    const int s = (int)blockIdx.y, units = a.layers * a.heads;
+    const EvictRecord r = a.record[s];
+    if (!r.cut || r.base < 0) return;
+    for (int i = (int)blockIdx.x; i < units + a.sets + 1; i += (int)gridDim.x) {
+        if (i < units)
+            shift_recent(a, r, s, i / a.heads, i % a.heads);
+        else if (i < units + a.sets)
+            move_sums(a, r, s, i - units);
+        else
+            enter_pages(a, r, s);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+
+uint64_t up256(uint64_t v) { return (v + 255u) & ~uint64_t(255); }
+
+bool evict_valid(const rac_cache_config* c, const rac_evict_config* e) {
+    return cache_valid(c) && e && sets_valid(c, e->sets) && e->first >= 0 && e->first <= (1 << 30) && e->recent >= 0 &&
+           e->recent <= (1 << 30);
+}
+
+// The scratch, in order; returns its bytes.
+uint64_t lay_out(const rac_cache_config* c, EvictArgs& a, uint8_t* ws) {
+    uint64_t at = 0;
+    const auto take = [&](auto*& p, uint64_t count) {
+        p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(ws + at);
+        at += up256(count * sizeof(*p));
+    };
+    const uint64_t sums = (uint64_t)c->seqs * a.sets, entries = (uint64_t)c->seqs * c->max_pages;
+    take(a.record, c->seqs);
+    take(a.old_page, entries);
+    take(a.old_at, entries);
+    take(a.fresh, entries);
+    take(a.free_list, c->pages);
+    take(a.list, sums * a.positions);
+    take(a.holes, sums);
+    take(a.hole_bits, sums * a.words);
+    return at;
+}
+
+EvictArgs args_of(const rac_cache_config* c, const rac_evict_config* e) {
+    EvictArgs a{};
+    a.positions = (int64_t)c->max_pages * c->page_tokens;
+    a.words = (a.positions + 63) / 64;
+    a.sets = e->sets;
+    return a;
+}
+
+// A row of workgroups for every sequence.
+rac_status launch(void (*kernel)(EvictArgs), int64_t each, int64_t seqs, int threads, EvictArgs a, hipStream_t st) {
+    void* p[] = {&a};
+    const int64_t most = (1 << 20) / seqs;  // (they go on with further work)
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)(each < most ? each : most), (unsigned)seqs), dim3((unsigned)threads), p, 0, st) ==
+                   hipSuccess
+               ? RAC_OK
+               : RAC_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t rac_cache_evict_workspace(const rac_cache_config* cfg, const rac_evict_config* evict) {
+    if (!evict_valid(cfg, evict) || !sums_counted(cfg, evict->sets)) return 0;
+    EvictArgs a = args_of(cfg, evict);
+    return (size_t)lay_out(cfg, a, nullptr);
+}
+
+rac_status rac_cache_evict(const rac_cache_config* cfg, const rac_evict_config* evict, void* pool, int32_t* table,
+                           int32_t* lengths, int32_t* refs, float* weight, const int32_t* keep, int32_t* evicted,
+                           int32_t* source, void* workspace, size_t workspace_bytes, rac_stream_t stream) {
+    if (!evict_valid(cfg, evict) || !pool || !table || !lengths || !refs || !weight || !keep || !evicted || !workspace)
+        return RAC_ERR_INVALID;
+    if (!aligned(pool, 16) || !aligned(table, 4) || !aligned(lengths, 4) || !aligned(refs, 4) || !aligned(weight, 4) ||
+        !aligned(keep, 4) || !aligned(evicted, 4) || !aligned(source, 4) || !aligned(workspace, 256))
+        return RAC_ERR_ALIGN;
+    if (!sums_counted(cfg, evict->sets)) return RAC_ERR_UNSUPPORTED;
+    if (workspace_bytes < rac_cache_evict_workspace(cfg, evict)) return RAC_ERR_CAPACITY;
+    EvictArgs a = args_of(cfg, evict);
+    lay_out(cfg, a, static_cast<uint8_t*>(workspace));
+    a.pool = static_cast<uint8_t*>(pool);
+    a.table = table;
+    a.lengths = lengths;
+    a.refs = refs;
+    a.weight = weight;
+    a.keep = keep;
+    a.evicted = evicted;
+    a.source = source;
+    a.layers = cfg->layers;
+    a.heads = cfg->kv_heads;
+    a.row_bytes = cfg->head_dim * cache_elem_bytes(cfg);
+    a.log_page = log2_of(cfg->page_tokens);
+    a.pages = cfg->pages;
+    a.seqs = cfg->seqs;
+    a.max_pages = cfg->max_pages;
+    a.first = evict->first;
+    a.recent = evict->recent;
+    // (a few workgroups for every compute unit where the sequences and heads are few)
+    const int64_t units = (int64_t)cfg->layers * cfg->kv_heads, parts = 2048 / (units * cfg->seqs);
+    a.parts = (int32_t)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    rac_status st = launch(evict_pick_kernel, evict->sets, cfg->seqs, kPickThreads, a, stream);
+    if (st == RAC_OK) st = launch(evict_demand_kernel, 1, cfg->seqs, kDemandThreads, a, stream);
+    if (st == RAC_OK) st = launch(evict_plan_kernel, 1, 1, kPlanThreads, a, stream);
+    if (st == RAC_OK) st = launch(evict_move_kernel, units * a.parts, cfg->seqs, kMoveThreads, a, stream);
+    if (st == RAC_OK) st = launch(evict_end_kernel, units + evict->sets + 1, cfg->seqs, kEndThreads, a, stream);
+    return st;
+}
+
+}  // extern "C"

@@ -2,7 +2,7 @@
 // the paged cache.  The contract is in include/rac_cache.h.
 #include <math.h>
 
-#include "cache_common.h"
+#include "tree_common.h"
 
 namespace {
 
@@ -35,94 +35,6 @@ struct TreeArgs {
     SeqPlan* plan;      // [seqs + 1], or null: every workgroup finds its work by itself
     int32_t m;          // query rows a workgroup
 };
-
-// What a sequence brings to the call, whatever the device arrays hold.
-struct Seq {
-    int q0, m;    // first query row, rows
-    int d0, n;    // first drafted row, drafted tokens
-    int length;   // committed tokens
-};
-
-__device__ __forceinline__ Seq seq_of(const TreeArgs& a, int s) {
-    Seq r;
-    r.q0 = clamp_int(a.q_start[s], 0, a.rows);
-    r.m = clamp_int(a.q_start[s + 1], r.q0, a.rows) - r.q0;
-    r.m = r.m < a.max_rows ? r.m : a.max_rows;
-    r.d0 = r.n = 0;
-    if (a.k) {
-        r.d0 = clamp_int(a.draft_start[s], 0, a.draft_rows);
-        r.n = clamp_int(a.draft_start[s + 1], r.d0, a.draft_rows) - r.d0;
-        r.n = r.n < a.max_draft ? r.n : a.max_draft;
-    }
-    r.length = clamp_int(a.lengths[s], 0, a.max_pages << a.log_page);
-    return r;
-}
-
-// What a query row sees: committed positions from `from` on, and the drafted
-// tokens of [first, end) that its mask names (all of them without a mask).
-struct Sight {
-    int from, first, end;
-};
-
-__device__ __forceinline__ Sight sight_of(const TreeArgs& a, const Seq& s, int i) {
-    Sight r{0, 0, s.n};
-    int c;  // drafted tokens it sees
-    const uint64_t* words = a.mask ? a.mask + (size_t)(s.q0 + i) * a.mask_words : nullptr;
-    if (words) {
-        const int most = a.mask_words * 64;
-        r.end = s.n < most ? s.n : most;
-        c = 0;
-        for (int w = 0; 64 * w < r.end; ++w) {
-            const int left = r.end - 64 * w;
-            c += __popcll(left >= 64 ? words[w] : words[w] & ((uint64_t(1) << left) - 1));
-        }
-    } else {
-        r.end = clamp_int(s.n - s.m + i + 1, 0, s.n);
-        c = r.end;
-    }
-    if (a.window > 0) {
-        if (c < a.window) {
-            r.from = s.length - (a.window - c);
-            r.from = r.from < 0 ? 0 : r.from;
-        } else {
-            r.from = s.length;
-            int drop = c - a.window;  // the first ones that fall out of the window
-            if (!words) {
-                r.first = drop;
-            } else {
-                int w = 0;
-                for (; drop > 0; ++w) {
-                    const int in = __popcll(words[w]);
-                    if (in > drop) break;
-                    drop -= in;
-                }
-                if (drop > 0) {
-                    uint64_t bits = words[w];
-                    for (; drop > 0; --drop) bits &= bits - 1;
-                    r.first = 64 * w + __builtin_ctzll(bits);
-                } else {
-                    r.first = 64 * w;
-                }
-            }
-        }
-    }
-    return r;
-}
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-template <int TYPE>
-__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
-    if constexpr (TYPE == RAC_CACHE_FP16)
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
 
 // Two floats in the 16-bit type, round to nearest even.
 template <int TYPE>
@@ -871,16 +783,6 @@ struct Load {
             v[i] &= (v[i] & (kExp << 16)) == (kExp << 16) ? 0xFFFFu : ~0u;
         }
         return v;
-    }
-
-    // Eight e4m3 as bf16 (exact).
-    static __device__ __forceinline__ u32x4 widen8(uint32_t a, uint32_t b) {
-        u32x4 r;
-        r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false));
-        r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true));
-        r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false));
-        r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true));
-        return r;
     }
 };
 
