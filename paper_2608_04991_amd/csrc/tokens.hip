@@ -51,6 +51,12 @@ struct Block {
         }
         return v;
     }
+    static __device__ __forceinline__ float top(const float (&x)[kN]) {
+        float m = x[0];
+#pragma unroll
+        for (int i = 1; i < kN; ++i) m = __builtin_fmaxf(m, x[i]);
+        return m;
+    }
     static __device__ __forceinline__ float one(const uint8_t* p) {
         if constexpr (TYPE == RAC_TYPE_FP32) return *reinterpret_cast<const float*>(p);
         if constexpr (TYPE == RAC_TYPE_FP16) return (float)*reinterpret_cast<const _Float16*>(p);
@@ -202,6 +208,28 @@ struct Row {
     }
 };
 
+// Over the lanes of a wavefront, by moves between neighbouring lanes, for all lanes.
+template <class F>
+__device__ __forceinline__ float over_wave(float v, bool zero, F f) {
+    const auto from = [&](auto ctrl, auto rows) {
+        const float x = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
+            zero ? 0 : __builtin_bit_cast(int, v), __builtin_bit_cast(int, v), decltype(ctrl)::value, decltype(rows)::value, 0xF, false));
+        v = f(v, x);
+    };
+    using std::integral_constant;
+    using all = integral_constant<int, 0xF>;
+    from(integral_constant<int, 0x111>{}, all{});  // row_shr:1, 2, 4, 8
+    from(integral_constant<int, 0x112>{}, all{});
+    from(integral_constant<int, 0x114>{}, all{});
+    from(integral_constant<int, 0x118>{}, all{});
+    from(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});  // row_bcast:15, 31
+    from(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+__device__ __forceinline__ float sum_wave(float v) { return over_wave(v, true, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ float max_wave(float v) { return over_wave(v, false, [](float a, float b) { return __builtin_fmaxf(a, b); }); }
+__device__ __forceinline__ float min_wave(float v) { return over_wave(v, false, [](float a, float b) { return __builtin_fminf(a, b); }); }
+
 // Partial sums of a softmax, in powers of two: sum of e = 2^(c (x - m)) and of
 // c (x - m) e.  m need not be the largest logit, only no more than kSlack / c below it.
 // (The difference comes before the factor: a mask of the type's lowest value stays in
@@ -210,9 +238,9 @@ struct Sums {
     float m, s, t;
     static constexpr float kSlack = 8.0f;
 
-    // slack: kSlack / c
-    template <int N, bool ENTROPY>
-    __device__ __forceinline__ void add(const float (&x)[N], float top, float c, float slack) {
+    // Ready for logits of up to `top`; slack: kSlack / c.
+    template <bool ENTROPY>
+    __device__ __forceinline__ void grow(float top, float c, float slack) {
         if (__any(top > m + slack)) {
             const float now = top > m + slack ? top : m, by = (m - now) * c;
             const float keep = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(by);
@@ -220,6 +248,9 @@ struct Sums {
             s = s * keep;
             m = now;
         }
+    }
+    template <int N, bool ENTROPY>
+    __device__ __forceinline__ void add(const float (&x)[N], float c) {
         const float ref = m == -INFINITY ? 0.0f : m;
         float e[N], u[N];
 #pragma unroll
@@ -245,15 +276,9 @@ struct Sums {
         m = to;
     }
     __device__ __forceinline__ void join_wave(float c) {
-        float top = m;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o));
-        rebase(top, c);
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            s = s + __shfl_xor(s, o);
-            t = t + __shfl_xor(t, o);
-        }
+        rebase(max_wave(m), c);
+        s = sum_wave(s);
+        t = sum_wave(t);
     }
     __device__ __forceinline__ float lse(float scale) const {
         return s == 0.0f ? -INFINITY : (float)((double)m * (double)scale + (double)log2f(s) * 0.6931471805599453);
@@ -267,15 +292,14 @@ struct Sums {
 
 // Logits in the order of alternatives: the larger first, ties to the lower word.
 // 0 is none.
-__device__ __forceinline__ uint64_t key_of(float x, int word) {
+__device__ __forceinline__ uint32_t order_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.0f);  // (-0 is 0)
-    return (uint64_t)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (uint32_t)~word;
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ float float_of(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7FFFFFFFu : ~u); }
+__device__ __forceinline__ uint64_t key_of(float x, int word) { return (uint64_t)order_of(x) << 32 | (uint32_t)~word; }
 __device__ __forceinline__ int word_of(uint64_t key) { return (int)~(uint32_t)key; }
-__device__ __forceinline__ float logit_of(uint64_t key) {
-    const uint32_t u = (uint32_t)(key >> 32);
-    return __uint_as_float(u & 0x80000000u ? u & 0x7FFFFFFFu : ~u);
-}
+__device__ __forceinline__ float logit_of(uint64_t key) { return float_of((uint32_t)(key >> 32)); }
 
 struct LogprobArgs {
     const uint8_t* logits;
@@ -291,6 +315,8 @@ struct LogprobArgs {
     uint64_t* part_top;   // [rows][parts][top]
     int64_t rows;
     int32_t vocab, count, top, parts;
+    int32_t part_blocks;  // blocks of a part
+    int32_t each;  // alternatives of a part that make up the row's with as many of others
     float scale, scale2, slack;  // scale2: times log2(e); slack: Sums::kSlack over that
 };
 
@@ -298,61 +324,190 @@ __device__ __forceinline__ float logprob_of(float x, float scale, float lse) {
     return (x == -INFINITY || lse == -INFINITY) && lse == lse ? -INFINITY : __builtin_fmaf(x, scale, -lse);
 }
 
-constexpr int kLogThreads = 256, kLogWaves = kLogThreads / 64, kMostTop = 64, kMostParts = 64, kCandidates = 1024;
+constexpr int kLogThreads = 256, kMostTop = 64, kMostParts = 64, kCandidates = 1024;
 
-// The `top` largest of blocks [b0, b1) into best[], descending, 0 where there are
-// fewer.  Every thread knows the largest of its own blocks: `top` threads have one of
-// at least `bar`, so no more than their logits can be among the largest, and those
-// that reach it, few as a rule, are ranked by counting.
-template <int TYPE>
-struct Top {
+// The blocks of a thread: every T-th of [b0, b1).  Held in registers, kHeld at most
+// (what is outside is -infinity), or read anew each time.  (One more than 8: a row of 8 T
+// blocks that does not begin at one has a part of another.)
+constexpr int kHeld = 9;
+
+template <int TYPE, int T>
+struct Held {
     using B = Block<TYPE>;
-    uint64_t buffer[kCandidates];
-    uint64_t best[kMostTop];
-    alignas(16) float most[kLogThreads];
-    uint64_t wave_key[kLogWaves];
-    float wave_bar[kLogWaves];
-    int count, wave_count[kLogWaves];
+    u32x4 raw[kHeld];
+    float tops[kHeld];  // the largest logit of each
+    int first, size;
 
-    template <class Take>
-    __device__ __forceinline__ void each(const Row<TYPE>& row, int b0, int b1, Take take) {
-        for (int b = b0 + (int)threadIdx.x; b < b1; b += kLogThreads) {
-            float x[B::kN];
-            row.get(b, x);
+    __device__ __forceinline__ Held(const Row<TYPE>& row, int b0, int b1) {
+        constexpr uint32_t kNone = TYPE == RAC_TYPE_FP32 ? 0xFF800000u : TYPE == RAC_TYPE_FP16 ? 0xFC00FC00u : 0xFF80FF80u;
+        first = b0 + (int)threadIdx.x;
+        size = b1 - b0;
 #pragma unroll
-            for (int i = 0; i < B::kN; ++i) take(x[i], row.word(b, i));
+        for (int k = 0; k < kHeld; ++k) {
+            const int b = first + k * T;
+            raw[k] = u32x4{kNone, kNone, kNone, kNone};
+            if (b < b1 && row.whole(b)) raw[k] = row.raw(b);
+        }
+        // (the first and the last of the row)
+        if (b0 == 0 && row.phase > 0 && threadIdx.x == 0) raw[0] = part_of(row, 0);
+        if (b1 == row.blocks && !row.whole(b1 - 1) && (uint32_t)(size - 1) % T == threadIdx.x) {
+            const u32x4 last = part_of(row, b1 - 1);
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k) raw[k] = k == (size - 1) / T ? last : raw[k];
         }
     }
+    static __device__ __forceinline__ u32x4 part_of(const Row<TYPE>& row, int b) {
+        float x[B::kN];
+        row.some(b, x);
+        return B::narrow(x);
+    }
+    // f(logits, the largest of them).
+    template <class F>
+    __device__ __forceinline__ void each(const Row<TYPE>&, F f) {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) tops[k] = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            if (k * T >= size) break;
+            float x[B::kN];
+            B::widen(raw[k], x);
+            tops[k] = B::top(x);
+            f(x, tops[k]);
+        }
+    }
+    // f(logit, word) of those of at least bar, -infinity not.  (Few: their blocks are marked
+    // and picked out one by one, so that there is one copy of what is done with them.)
+    template <class F>
+    __device__ __forceinline__ void reach(const Row<TYPE>& row, float bar, F f) const {
+        uint32_t marks = 0;
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) marks |= tops[k] >= bar ? 1u << k : 0u;
+        while (__any(marks)) {
+            const int k = marks ? __builtin_ctz(marks) : kHeld;
+            u32x4 v = raw[0];
+#pragma unroll
+            for (int j = 1; j < kHeld; ++j) {
+                const bool is = k == j;
+                v = u32x4{is ? raw[j][0] : v[0], is ? raw[j][1] : v[1], is ? raw[j][2] : v[2], is ? raw[j][3] : v[3]};
+            }
+            float x[B::kN];
+            B::widen(v, x);
+            uint32_t hits = 0;
+#pragma unroll
+            for (int i = 0; i < B::kN; ++i) hits |= marks && x[i] >= bar && x[i] > -INFINITY ? 1u << i : 0u;
+            while (__any(hits)) {
+                const int i = hits ? __builtin_ctz(hits) : 0;
+                float y = x[0];
+#pragma unroll
+                for (int j = 1; j < B::kN; ++j) y = i == j ? x[j] : y;
+                if (hits) f(y, row.word(first + k * T, i));
+                hits &= hits - 1u;
+            }
+            marks &= marks - 1u;
+        }
+    }
+};
+
+template <int TYPE, int T, int AT_ONCE>
+struct Streamed {
+    using B = Block<TYPE>;
+    int b0, b1;
+
+    __device__ __forceinline__ Streamed(const Row<TYPE>&, int from, int to) : b0(from), b1(to) {}
+    // f(logits, their first word).
+    template <class F>
+    __device__ __forceinline__ void blocks(const Row<TYPE>& row, F f) const {
+        for (int b = b0 + (int)threadIdx.x; b < b1; b += AT_ONCE * T) {
+            u32x4 v[AT_ONCE];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k)
+                if (b + k * T < b1 && row.whole(b + k * T)) v[k] = row.raw(b + k * T);
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int at = b + k * T;
+                if (at >= b1) break;
+                float x[B::kN];
+                if (row.whole(at))
+                    B::widen(v[k], x);
+                else
+                    row.some(at, x);
+                f(x, row.word(at, 0));
+            }
+        }
+    }
+    template <class F>
+    __device__ __forceinline__ void each(const Row<TYPE>& row, F f) const {
+        blocks(row, [&](const float (&x)[B::kN], int) { f(x, B::top(x)); });
+    }
+    template <class F>
+    __device__ __forceinline__ void reach(const Row<TYPE>& row, float bar, F f) const {
+        blocks(row, [&](const float (&x)[B::kN], int word) {
+            if (!(B::top(x) >= bar)) return;  // (most blocks)
+#pragma unroll
+            for (int i = 0; i < B::kN; ++i)
+                if (x[i] >= bar && x[i] > -INFINITY) f(x[i], word + i);
+        });
+    }
+    // f(logits, their first word), by all threads at once, in the order of words; f that returns
+    // false ends it.
+    template <class F>
+    __device__ __forceinline__ void in_order(const Row<TYPE>& row, F f) const {
+        for (int b = b0; b < b1; b += T) {
+            float x[B::kN];
+#pragma unroll
+            for (int i = 0; i < B::kN; ++i) x[i] = -INFINITY;
+            if (b + (int)threadIdx.x < b1) row.get(b + (int)threadIdx.x, x);
+            if (!f(x, row.word(b + (int)threadIdx.x, 0))) return;
+        }
+    }
+};
+
+// The `top` largest logits into best[], descending, 0 where there are fewer.  Every
+// thread knows its own largest.  With the d-th largest of these in each of g wavefronts,
+// d g >= top, there are enough: the g-th largest of the wavefronts' d-th ones is a bar
+// that few logits reach as a rule, and they are ranked by counting.
+template <int TYPE, int T>
+struct Top {
+    using B = Block<TYPE>;
+    static constexpr int kWaves = T / 64;
+    uint64_t buffer[kCandidates];
+    uint64_t best[kMostTop];
+    uint64_t wave_key[kWaves];
+    float wave_bar[kWaves];
+    int count, wave_count[kWaves];
+
     __device__ __forceinline__ void push(float x, int word) {
         const int at = atomicAdd(&count, 1);  // (any order: the keys are ranked)
         if (at < kCandidates) buffer[at] = key_of(x, word);
     }
-    __device__ __forceinline__ void find(const Row<TYPE>& row, int b0, int b1, int top, float mine) {
-        const int t = (int)threadIdx.x;
-        most[t] = mine;
+    template <class Blocks>
+    __device__ __forceinline__ void find(const Row<TYPE>& row, const Blocks& blocks, int b0, int b1, int top, float mine) {
+        const int t = (int)threadIdx.x, lane = t & 63;
+        const int d = (top + kWaves - 1) / kWaves, g = (top + d - 1) / d;
+        float bar = max_wave(mine), rest = mine;
+        for (int have = __popcll(__ballot(rest == bar)); have < d; have += __popcll(__ballot(rest == bar))) {
+            if (rest == bar) rest = -INFINITY;
+            bar = max_wave(rest);
+            if (bar == -INFINITY) break;
+        }
+        if (lane == 0) wave_bar[t / 64] = bar;
         if (t < kMostTop) best[t] = 0;
         if (t == 0) count = 0;
         __syncthreads();
-        int above = 0;
-#pragma unroll 4
-        for (int i = 0; i < kLogThreads; i += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(most + i);
-            above += (v.x > mine) + (v.y > mine) + (v.z > mine) + (v.w > mine);
-        }
-        float bar = above < top ? mine : INFINITY;
+        const float own = lane < kWaves ? wave_bar[lane] : -INFINITY;
+        int above = 0;  // wavefronts with a bar of at least this one
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) bar = __builtin_fminf(bar, __shfl_xor(bar, o));
-        if ((t & 63) == 0) wave_bar[t / 64] = bar;
+        for (int w = 0; w < kWaves; ++w)
+            above += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, own), w)) >= own;
+        bar = max_wave(lane < kWaves && above >= g ? own : -INFINITY);
+        if (mine >= bar && mine > -INFINITY) blocks.reach(row, bar, [&](float x, int word) { push(x, word); });
         __syncthreads();
-        for (int w = 0; w < kLogWaves; ++w) bar = __builtin_fminf(bar, wave_bar[w]);
-        if (mine >= bar && mine > -INFINITY)
-            each(row, b0, b1, [&](float x, int word) { if (x >= bar && x > -INFINITY) push(x, word); });
-        __syncthreads();
-        if (count > kCandidates) many(row, b0, b1, top, mine, bar);
+        if (count > kCandidates) many(row, Streamed<TYPE, T, 1>(row, b0, b1), top, mine, bar);
         const int n = count;
-        for (int c = t; c < n; c += kLogThreads) {
+        for (int c = t; c < n; c += T) {
             const uint64_t key = buffer[c];
             int rank = 0;
+#pragma unroll 8
             for (int i = 0; i < n; ++i) rank += buffer[i] > key;
             if (rank < top) best[rank] = key;
         }
@@ -360,50 +515,54 @@ struct Top {
     }
     // More reach the bar than there is room for: as a rule words that tie with it, of
     // which the first will do.
-    __device__ __noinline__ void many(const Row<TYPE>& row, int b0, int b1, int top, float mine, float bar) {
+    __device__ __forceinline__ void many(const Row<TYPE>& row, const Streamed<TYPE, T, 1>& blocks, int top, float mine, float bar) {
         const int t = (int)threadIdx.x;
         __syncthreads();
         if (t == 0) count = 0;
         __syncthreads();
-        if (mine > bar) each(row, b0, b1, [&](float x, int word) { if (x > bar) push(x, word); });
+        if (mine > bar) blocks.reach(row, bar, [&](float x, int word) { if (x > bar) push(x, word); });
         __syncthreads();
         int n = count;
+        __syncthreads();
         if (n <= kCandidates - kMostTop) {
-            for (int b = b0; b < b1 && n < top; b += kLogThreads) {  // (in the order of words)
-                float x[B::kN];
-                int own = 0;
-                if (b + t < b1) row.get(b + t, x);
+            if (n < top)
+                blocks.in_order(row, [&](const float (&x)[B::kN], int word) {
+                    int own = 0;
 #pragma unroll
-                for (int i = 0; i < B::kN; ++i) own += b + t < b1 && x[i] == bar;
-                int before = own;
-                for (int o = 1; o < 64; o <<= 1) {
-                    const int y = __shfl_up(before, o);
-                    before += (t & 63) >= o ? y : 0;
-                }
-                if ((t & 63) == 63) wave_count[t / 64] = before;
-                __syncthreads();
-                int at = n + before - own;
-                for (int w = 0; w < kLogWaves; ++w) {
-                    at += w < t / 64 ? wave_count[w] : 0;
-                    n += wave_count[w];
-                }
-#pragma unroll
-                for (int i = 0; i < B::kN; ++i)
-                    if (b + t < b1 && x[i] == bar) {
-                        if (at < top) buffer[at] = key_of(bar, row.word(b + t, i));
-                        ++at;
+                    for (int i = 0; i < B::kN; ++i) own += x[i] == bar;
+                    int before = own;
+                    for (int o = 1; o < 64; o <<= 1) {
+                        const int y = __shfl_up(before, o);
+                        before += (t & 63) >= o ? y : 0;
                     }
-                __syncthreads();
-            }
+                    if ((t & 63) == 63) wave_count[t / 64] = before;
+                    __syncthreads();
+                    int at = n + before - own;
+                    for (int w = 0; w < kWaves; ++w) {
+                        at += w < t / 64 ? wave_count[w] : 0;
+                        n += wave_count[w];
+                    }
+#pragma unroll
+                    for (int i = 0; i < B::kN; ++i)
+                        if (x[i] == bar) {
+                            if (at < top) buffer[at] = key_of(bar, word + i);
+                            ++at;
+                        }
+                    __syncthreads();
+                    return n < top;
+                });
             if (t == 0 && count < top) count = n < top ? n : top;
         } else {  // (a few threads have most of the large ones) one after the other
             uint64_t last = ~uint64_t(0);
             n = 0;
             for (; n < top; ++n) {
                 uint64_t next = 0;
-                each(row, b0, b1, [&](float x, int word) {
-                    const uint64_t key = key_of(x, word);
-                    if (x > -INFINITY && key < last && key > next) next = key;
+                blocks.blocks(row, [&](const float (&x)[B::kN], int word) {
+#pragma unroll
+                    for (int i = 0; i < B::kN; ++i) {
+                        const uint64_t key = x[i] > -INFINITY ? key_of(x[i], word + i) : 0;
+                        if (key < last && key > next) next = key;
+                    }
                 });
 #pragma unroll
                 for (int o = 1; o < 64; o <<= 1) {
@@ -413,7 +572,7 @@ struct Top {
                 __syncthreads();
                 if ((t & 63) == 0) wave_key[t / 64] = next;
                 __syncthreads();
-                for (int w = 0; w < kLogWaves; ++w) next = wave_key[w] > next ? wave_key[w] : next;
+                for (int w = 0; w < kWaves; ++w) next = wave_key[w] > next ? wave_key[w] : next;
                 if (next == 0) break;
                 last = next;
                 if (t == 0) buffer[n] = next;
@@ -427,15 +586,25 @@ struct Top {
 // Nothing, where no alternatives are wanted.
 struct NoTop {};
 
+// The scored token of a row and its logit, read ahead of the sums.
 template <int TYPE>
-__device__ __forceinline__ void finish_row(const LogprobArgs& a, int64_t row, const Sums& x) {
+struct Scored {
+    bool there;
+    float logit;
+
+    __device__ __forceinline__ Scored(const LogprobArgs& a, int64_t row) {
+        const int token = a.token_rows || a.count == 0 ? -1 : a.tokens[row];
+        there = token >= 0 && token < a.vocab;
+        logit = there ? Block<TYPE>::one(a.logits + row * a.stride + (int64_t)token * Block<TYPE>::kBytes) : 0.0f;
+    }
+};
+
+template <int TYPE>
+__device__ __forceinline__ void finish_row(const LogprobArgs& a, int64_t row, const Sums& x, const Scored<TYPE>& y) {
     const float lse = x.lse(a.scale);
     a.lse[row] = lse;
     if (a.entropy) a.entropy[row] = x.entropy();
-    if (a.token_rows || a.count == 0) return;
-    const int token = a.tokens[row];
-    a.logprob[row] = token < 0 || token >= a.vocab ? 0.0f :
-        logprob_of(Block<TYPE>::one(a.logits + row * a.stride + (int64_t)token * Block<TYPE>::kBytes), a.scale, lse);
+    if (!a.token_rows && a.count > 0) a.logprob[row] = y.there ? logprob_of(y.logit, a.scale, lse) : 0.0f;
 }
 
 __device__ __forceinline__ void finish_top(const LogprobArgs& a, int64_t row, int i, uint64_t key, float lse) {
@@ -443,64 +612,48 @@ __device__ __forceinline__ void finish_top(const LogprobArgs& a, int64_t row, in
     a.top_logprobs[row * a.top + i] = key ? logprob_of(logit_of(key), a.scale, lse) : -INFINITY;
 }
 
-// A workgroup a row, or a part of one: one pass with a running reference and sums.
+// A workgroup a row, or a part of one: one pass with a running reference and sums.  With
+// alternatives the blocks stay in registers for the second look where they fit (HELD).
 //
 // Bound by the logits' bytes.
-template <int TYPE, bool ENTROPY, bool TOP>
-__global__ __launch_bounds__(kLogThreads) void logprob_kernel(LogprobArgs a) {
+template <int TYPE, bool ENTROPY, bool TOP, int T, bool HELD>
+__global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
     using B = Block<TYPE>;
-    constexpr int kAtOnce = 4;
-    __shared__ Sums waves[kLogWaves];
-    __shared__ typename std::conditional<TOP, Top<TYPE>, NoTop>::type alternatives;
-    const int t = (int)threadIdx.x;
-    const int part = (int)blockIdx.x;
+    using Blocks = typename std::conditional<HELD, Held<TYPE, T>, Streamed<TYPE, T, 4>>::type;
+    constexpr int kWaves = T / 64;
+    __shared__ Sums waves[kWaves];
+    __shared__ typename std::conditional<TOP, Top<TYPE, T>, NoTop>::type alternatives;
+    const int t = (int)threadIdx.x, part = (int)blockIdx.x;
     for (int64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
         const int64_t item = r * a.parts + part;
         const Row<TYPE> row(a.logits + r * a.stride, a.vocab);
-        const int per = (row.blocks + a.parts - 1) / a.parts;
-        const int b0 = part * per < row.blocks ? part * per : row.blocks, b1 = b0 + per < row.blocks ? b0 + per : row.blocks;
+        const int b0 = part * a.part_blocks < row.blocks ? part * a.part_blocks : row.blocks;
+        const int b1 = b0 + a.part_blocks < row.blocks ? b0 + a.part_blocks : row.blocks;
+        Blocks blocks(row, b0, b1);
+        const Scored<TYPE> scored(a, r);
         Sums x{-INFINITY, 0.0f, 0.0f};
         float most = -INFINITY;
-        const auto take = [&](const float (&v)[B::kN]) {
-            float top = v[0];
-#pragma unroll
-            for (int i = 1; i < B::kN; ++i) top = __builtin_fmaxf(top, v[i]);
+        blocks.each(row, [&](const float (&v)[B::kN], float top) {
             if constexpr (TOP) most = __builtin_fmaxf(most, top);
-            x.add<B::kN, ENTROPY>(v, top, a.scale2, a.slack);
-        };
-        for (int b = b0 + t; b < b1; b += kAtOnce * kLogThreads) {
-            u32x4 v[kAtOnce];
-#pragma unroll
-            for (int k = 0; k < kAtOnce; ++k)
-                if (b + k * kLogThreads < b1 && row.whole(b + k * kLogThreads)) v[k] = row.raw(b + k * kLogThreads);
-#pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) {
-                const int at = b + k * kLogThreads;
-                if (at >= b1) break;
-                float y[B::kN];
-                if (row.whole(at))
-                    B::widen(v[k], y);
-                else
-                    row.some(at, y);
-                take(y);
-            }
-        }
+            x.grow<ENTROPY>(top, a.scale2, a.slack);
+            x.add<B::kN, ENTROPY>(v, a.scale2);
+        });
         x.join_wave(a.scale2);
         if ((t & 63) == 0) waves[t / 64] = x;
-        if constexpr (TOP) alternatives.find(row, b0, b1, a.top, most + 0.0f);
+        if constexpr (TOP) alternatives.find(row, blocks, b0, b1, a.top, most + 0.0f);
         __syncthreads();
-        x = waves[t % kLogWaves];
+        x = waves[t % kWaves];
         float top = x.m;
 #pragma unroll
-        for (int o = 1; o < kLogWaves; o <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o));
+        for (int o = 1; o < kWaves; o <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o));
         x.rebase(top, a.scale2);
 #pragma unroll
-        for (int o = 1; o < kLogWaves; o <<= 1) {
+        for (int o = 1; o < kWaves; o <<= 1) {
             x.s = x.s + __shfl_xor(x.s, o);
             x.t = x.t + __shfl_xor(x.t, o);
         }
         if (a.parts == 1) {
-            if (t == 0) finish_row<TYPE>(a, r, x);
+            if (t == 0) finish_row<TYPE>(a, r, x, scored);
             if constexpr (TOP)
                 if (t < a.top) finish_top(a, r, t, alternatives.best[t], x.lse(a.scale));
         } else {
@@ -512,41 +665,58 @@ __global__ __launch_bounds__(kLogThreads) void logprob_kernel(LogprobArgs a) {
     }
 }
 
-// Joins the parts of a row: a wavefront has the sums, and an alternative's rank is
-// the sum of its ranks in the parts' lists.
+// Joins the parts of a row: a wavefront has the sums.  With d alternatives of each of
+// top / d parts there are enough: so the top / d-th largest of the parts' d-th ones bounds
+// the row's from below, and the few keys that reach it are ranked by counting.
 template <int TYPE>
 __global__ __launch_bounds__(kLogThreads) void logprob_join_kernel(LogprobArgs a) {
     __shared__ uint64_t keys[kMostParts * kMostTop];
     __shared__ uint64_t best[kMostTop];
-    const int t = (int)threadIdx.x;
+    __shared__ int count;
+    const int t = (int)threadIdx.x, all = a.parts * a.top;
     const int64_t r = blockIdx.x;
+    const Scored<TYPE> scored(a, r);
+    constexpr int kAtOnce = kMostParts * kMostTop / kLogThreads;
+    uint64_t key[kAtOnce], bar = 0;
+    if (a.top > 0) {
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            key[i] = 0;
+            if (i * kLogThreads < all && t + i * kLogThreads < all) key[i] = a.part_top[r * all + t + i * kLogThreads];
+        }
+        if ((t & 63) < a.parts) bar = a.part_top[r * all + (t & 63) * a.top + a.each - 1];
+    }
     Sums x{-INFINITY, 0.0f, 0.0f};
     if ((t & 63) < a.parts) {
         const float4 v = *reinterpret_cast<const float4*>(a.part_sums + 4 * (r * a.parts + (t & 63)));
         x = Sums{v.x, v.y, v.z};
     }
     x.join_wave(a.scale2);
-    if (t == 0) finish_row<TYPE>(a, r, x);
+    if (t == kLogThreads - 64) finish_row<TYPE>(a, r, x, scored);
     if (a.top == 0) return;
-    const int all = a.parts * a.top;
-    for (int i = t; i < all; i += kLogThreads) keys[i] = a.part_top[r * all + i];
+    int above = 0;
+    for (int p = 0; p < a.parts; ++p) {
+        const uint64_t y = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(bar >> 32), p) << 32 |
+                           (uint32_t)__builtin_amdgcn_readlane((int)bar, p);
+        above += y > bar || (y == bar && p < (t & 63));
+    }
+    const int at = __builtin_ctzll(__ballot((t & 63) < a.parts && above == (a.top + a.each - 1) / a.each - 1));
+    bar = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(bar >> 32), at) << 32 |
+          (uint32_t)__builtin_amdgcn_readlane((int)bar, at);
     if (t < kMostTop) best[t] = 0;
+    if (t == 0) count = 0;
     __syncthreads();
-    for (int i = t; i < all; i += kLogThreads) {
-        const uint64_t key = keys[i];
-        if (!key) continue;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i)
+        if (key[i] && key[i] >= bar) keys[atomicAdd(&count, 1)] = key[i];  // (any order: they are ranked)
+    __syncthreads();
+    const int n = count;
+    for (int i = t; i < n; i += kLogThreads) {
+        const uint64_t k = keys[i];
         int rank = 0;
-        for (int p = 0; p < a.parts && rank < a.top; ++p) {
-            int lo = 0, n = a.top;  // how many of the part's list are larger
-            while (n > 0) {
-                const int half = n / 2;
-                const bool more = keys[p * a.top + lo + half] > key;
-                lo = more ? lo + half + 1 : lo;
-                n = more ? n - half - 1 : half;
-            }
-            rank += lo;
-        }
-        if (rank < a.top) best[rank] = key;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) rank += keys[j] > k;
+        if (rank < a.top) best[rank] = k;
     }
     __syncthreads();
     if (t < a.top) finish_top(a, r, t, best[t], x.lse(a.scale));
@@ -674,21 +844,39 @@ bool logprob_valid(const rac_logprob_config* c) {
            c->type <= RAC_TYPE_FP32 && (c->scale == 0.0f || (c->scale >= 0x1p-40f && c->scale <= 0x1p40f));
 }
 
-// Parts of a row: few rows are cut so that every compute unit has work, into parts of
-// at least four steps of a workgroup.
-int logprob_parts(const rac_logprob_config* c) {
-    if (c->rows == 0) return 1;
-    const int64_t blocks = ((int64_t)c->vocab * type_bytes(c->type) + 15) / 16 + 1;
-    int64_t parts = c->rows >= 512 ? 1 : 1024 / c->rows;
-    const int64_t most = blocks / (4 * kLogThreads);
+// How rows are cut.  Few rows: so that every compute unit has work, into parts of at
+// least two blocks a thread.  With alternatives: into parts that a workgroup of 256
+// threads, or 512, holds in registers.
+struct LogprobCut {
+    int parts, part_blocks, threads;
+    bool held;
+};
+
+LogprobCut cut_of(const rac_logprob_config* c) {
+    const int64_t blocks = ((int64_t)c->vocab * type_bytes(c->type) + 15) / 16 + 1, rows = c->rows > 0 ? c->rows : 1;
+    int64_t parts = rows >= 512 ? 1 : 1024 / rows;
+    const int64_t most = blocks / (2 * kLogThreads);
     parts = parts < most ? parts : most;
-    return (int)(parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts);
+    parts = parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts;
+    const int64_t hold = (blocks + kHeld * 512 - 1) / (kHeld * 512);
+    LogprobCut r{};
+    r.held = c->top > 0 && hold <= kMostParts;
+    if (r.held && parts < hold) parts = hold;
+    r.parts = (int)parts;
+    r.part_blocks = (int)((blocks + parts - 1) / parts);
+    r.threads = r.held && r.part_blocks > kHeld * 256 ? 512 : 256;
+    return r;
 }
 
+template <int TYPE, bool ENTROPY>
+void (*logprob_of_form(const LogprobCut& cut, bool top))(LogprobArgs) {
+    if (!top) return logprob_kernel<TYPE, ENTROPY, false, 256, false>;
+    if (!cut.held) return logprob_kernel<TYPE, ENTROPY, true, 256, false>;
+    return cut.threads == 512 ? logprob_kernel<TYPE, ENTROPY, true, 512, true> : logprob_kernel<TYPE, ENTROPY, true, 256, true>;
+}
 template <int TYPE>
-void (*logprob_of_type(bool entropy, bool top))(LogprobArgs) {
-    return entropy ? top ? logprob_kernel<TYPE, true, true> : logprob_kernel<TYPE, true, false>
-                   : top ? logprob_kernel<TYPE, false, true> : logprob_kernel<TYPE, false, false>;
+void (*logprob_of_type(const LogprobCut& cut, bool entropy, bool top))(LogprobArgs) {
+    return entropy ? logprob_of_form<TYPE, true>(cut, top) : logprob_of_form<TYPE, false>(cut, top);
 }
 
 template <int TYPE>
@@ -775,7 +963,7 @@ rac_status rac_rotary(const rac_rotary_config* cfg, const int32_t* pos, const do
 
 size_t rac_logprobs_workspace(const rac_logprob_config* cfg) {
     if (!logprob_valid(cfg)) return 0;
-    const int parts = logprob_parts(cfg);
+    const int parts = cut_of(cfg).parts;
     const uint64_t items = parts > 1 ? (uint64_t)cfg->rows * parts : 0;
     return (size_t)(256 + up256(items * 16) + up256(items * cfg->top * 8));
 }
@@ -794,20 +982,21 @@ rac_status rac_logprobs(const rac_logprob_config* cfg, const rac_logprob_tensors
         return RAC_ERR_ALIGN;
     if (cfg->rows > 0 && workspace_bytes < rac_logprobs_workspace(cfg)) return RAC_ERR_CAPACITY;
     const float scale = cfg->scale == 0.0f ? 1.0f : cfg->scale;
-    const int parts = logprob_parts(cfg);
+    const LogprobCut cut = cut_of(cfg);
+    const int parts = cut.parts;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     LogprobArgs a{static_cast<const uint8_t*>(t->logits), t->stride * bytes, t->tokens, t->token_rows, t->logprob, t->lse,
                   t->entropy, t->top_ids, t->top_logprobs, reinterpret_cast<float*>(ws),
                   reinterpret_cast<uint64_t*>(ws + up256((uint64_t)cfg->rows * parts * 16)), cfg->rows, cfg->vocab,
-                  cfg->tokens, cfg->top, parts, scale, scale * 1.44269504f, Sums::kSlack / (scale * 1.44269504f)};
+                  cfg->tokens, cfg->top, parts, cut.part_blocks, (cfg->top + parts - 1) / parts, scale, scale * 1.44269504f, Sums::kSlack / (scale * 1.44269504f)};
     const int type = cfg->type;
     rac_status st = RAC_OK;
     if (cfg->rows > 0) {
         const bool e = t->entropy != nullptr, top = cfg->top > 0;
-        const auto kernel = type == RAC_TYPE_FP32 ? logprob_of_type<RAC_TYPE_FP32>(e, top)
-                          : type == RAC_TYPE_FP16 ? logprob_of_type<RAC_TYPE_FP16>(e, top)
-                                                  : logprob_of_type<RAC_TYPE_BF16>(e, top);
-        st = launch(kernel, parts, a.rows, kLogThreads, a, stream);
+        const auto kernel = type == RAC_TYPE_FP32 ? logprob_of_type<RAC_TYPE_FP32>(cut, e, top)
+                          : type == RAC_TYPE_FP16 ? logprob_of_type<RAC_TYPE_FP16>(cut, e, top)
+                                                  : logprob_of_type<RAC_TYPE_BF16>(cut, e, top);
+        st = launch(kernel, parts, a.rows, cut.threads, a, stream);
         if (st == RAC_OK && parts > 1)
             st = launch(type == RAC_TYPE_FP32 ? logprob_join_kernel<RAC_TYPE_FP32>
                       : type == RAC_TYPE_FP16 ? logprob_join_kernel<RAC_TYPE_FP16> : logprob_join_kernel<RAC_TYPE_BF16>,

@@ -108,7 +108,7 @@ def some_tokens(rows, vocab, seed, odd=True):
 
 @pytest.mark.parametrize("dtype", list(TYPES.values()), ids=str)
 @pytest.mark.parametrize("rows,vocab", [(1, 1), (1, 2), (3, 7), (5, 8), (4, 9), (2, 63), (7, 1000), (64, 1025), (600, 517),
-                                        (1, 50001), (3, 131071), (65, 32003), (513, 8191)])
+                                        (1, 50001), (3, 131071), (65, 32003), (513, 8191), (520, 33001), (2, 2400001)])
 def test_rows_and_vocabularies(dtype, rows, vocab):
     say(f"[gpu] log probabilities {rows} x {vocab} {dtype}")
     x, t = normal(rows, vocab, dtype, rows + vocab), some_tokens(rows, vocab, rows)
@@ -156,7 +156,7 @@ def test_masked_words(dtype, vocab):
 
 
 def test_ties_go_to_the_lower_word():
-    for rows, vocab in ((3, 50000), (600, 5000)):
+    for rows, vocab in ((3, 50000), (600, 5000), (3, 2400000)):
         x = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
         x[1, ::3] = -0.0                    # (the same as 0)
         x[2] = normal(1, vocab, torch.bfloat16, 1)[0].round()  # few different values

@@ -83,7 +83,7 @@ def calls_of_the_gpu_tests():
     for type in (0, 1, 2):
         for layout in (0, 1):
             calls.append(("rotary", [17, 8, 8, 64, 32, type, layout], None))
-        for rows, vocab in ((5, 8), (64, 1025), (600, 517), (3, 131071), (513, 8191)):
+        for rows, vocab in ((5, 8), (64, 1025), (600, 517), (3, 131071), (513, 8191), (520, 33001), (2, 2400001)):
             for top in (0, 5):
                 for entropy in (0, 1):
                     calls.append(("logprobs", [rows, vocab, rows, top, type], [0, entropy]))
