@@ -297,18 +297,6 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(TreeArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// LDS: a tile of 16-bit keys or values is kTile rows of DP / 8 pieces of 16
-// bytes; piece c of a row sits at c ^ swizzle(row), so that 16 lanes that read
-// the same piece of 16 rows, or write the pieces of one row, touch every bank
-// once.
-template <int DP>
-__device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t c) {
-    if constexpr (DP == 64)
-        return row * 8u + (c ^ ((row >> 1) & 7u));
-    else
-        return row * (DP / 8) + (c ^ (row & 15u));
-}
-
 // Four of eight keys of channel 16 dt + lane % 16: the transposing read takes
 // from the 16 lanes of a group the four 8-byte parts of four rows.
 template <int DP>

@@ -106,4 +106,16 @@ __device__ __forceinline__ u32x4 widen8(uint32_t a, uint32_t b) {
     return r;
 }
 
+// LDS: a tile of 16-bit queries, keys or values is rows of DP / 8 pieces of 16
+// bytes; piece c of a row sits at c ^ swizzle(row), so that 16 lanes that read
+// the same piece of 16 rows, or write the pieces of one row, touch every bank
+// once.
+template <int DP>
+__device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t c) {
+    if constexpr (DP == 64)
+        return row * 8u + (c ^ ((row >> 1) & 7u));
+    else
+        return row * (DP / 8) + (c ^ (row & 15u));
+}
+
 }  // namespace

@@ -24,48 +24,32 @@ struct WeightsArgs {
     int32_t rows, max_rows, draft_rows, max_draft, window, mask_words;
     int32_t sets, first_set, unit_heads;  // heads with units of their own (1: a unit has all)
     int32_t item_heads;                   // heads of a unit
-    int32_t slots;
     uint32_t by_group;  // 2^32 / group, rounded up
     float scale2;       // of the scores, times log2(e)
     float k_scale;
 };
 
 // ---------------------------------------------------------------------------
-// The work.  A unit is a tile of 64 keys of a sequence, for one key-value head or
-// all of them; its items are tiles of 16 query rows (rows of a key-value head are the
-// (node, query head) pairs of a sequence, node by node) of its heads, one head after the
-// other.  A wavefront takes a unit, or a part of one where units are few and long: parts
-// of at most `size` items, which about kWant wavefronts share out.
-constexpr int kWant = 16384;  // parts of the work wanted: a few for every wavefront that runs at once
-constexpr int kKeys = 64, kRowTile = 16, kThreads = 256, kWavesEach = kThreads / 64;
+// The work.  A unit is a tile of keys of a sequence, for one key-value head or all of
+// them; its items are blocks of query rows (rows of a key-value head are the (node, query
+// head) pairs of a sequence, node by node) of its heads, one head after the other.
+constexpr int kThreads = 256, kWavesEach = kThreads / 64;
 
 struct Units {
     int tile0, committed, drafted;  // first tile that the window reaches, tiles
-    int rows;                       // tiles of rows of a head
+    int rows;                       // blocks of rows of a head
 };
 
+template <int KEYS, int ROWS>
 __device__ __forceinline__ Units units_of(const WeightsArgs& a, const Seq& q) {
     Units u;
-    u.tile0 = a.window > 0 && q.length > a.window ? (q.length - a.window) / kKeys : 0;
-    u.committed = (q.length + kKeys - 1) / kKeys - u.tile0;
-    u.drafted = a.draft_weight ? (q.n + kKeys - 1) / kKeys : 0;
-    u.rows = (q.m * a.group + kRowTile - 1) / kRowTile;
+    u.tile0 = a.window > 0 && q.length > a.window ? (q.length - a.window) / KEYS : 0;
+    u.committed = (q.length + KEYS - 1) / KEYS - u.tile0;
+    u.drafted = a.draft_weight ? (q.n + KEYS - 1) / KEYS : 0;
+    u.rows = (q.m * a.group + ROWS - 1) / ROWS;
     if (u.rows == 0) u.committed = u.drafted = 0;
     return u;
 }
-
-// What a sequence has: units, and parts of each.
-struct Share {
-    int64_t units;
-    int items;
-};
-__device__ __forceinline__ Share share_of(const WeightsArgs& a, int s) {
-    const Units u = units_of(a, seq_of(a, s));
-    return Share{(int64_t)(u.committed + u.drafted) * a.unit_heads, u.rows * a.item_heads};
-}
-__device__ __forceinline__ int parts_of(int items, int size) { return items > size ? (items + size - 1) / size : 1; }
-
-constexpr int kNoMore = 0x7FFFFFFF;
 
 __device__ __forceinline__ int64_t sum_before(int64_t v, int64_t* sums, int64_t* total) {
     const int lane = (int)threadIdx.x & 63, w = (int)threadIdx.x / 64;
@@ -88,42 +72,29 @@ __device__ __forceinline__ int64_t sum_before(int64_t v, int64_t* sums, int64_t*
     return before + x - v;
 }
 
-// Where the work of every sequence begins, in LDS, as every workgroup finds it by itself:
-// base[s] of parts (with JOIN: of units that were cut), slot[s] of partial results.
-// Returns the size of a part; base[seqs] is the end.
-template <bool JOIN>
-__device__ __forceinline__ int lay_out(const WeightsArgs& a, int32_t* base, int32_t* slot) {
+constexpr int kNoMore = 0x7FFFFFFF;
+__device__ __forceinline__ int held_int(int64_t v) { return v < kNoMore ? (int)v : kNoMore; }
+
+// Where the units of every sequence begin, in LDS, as every workgroup finds it by itself;
+// base[seqs] is the end.
+template <int KEYS, int ROWS>
+__device__ __forceinline__ void lay_out(const WeightsArgs& a, int32_t* base) {
     __shared__ int64_t sums[kWavesEach];
     const int each = (a.seqs + kThreads - 1) / kThreads, s0 = (int)threadIdx.x * each;
     const int s1 = s0 + each < a.seqs ? s0 + each : a.seqs;
-    int64_t work = 0, all;
-    Share one{0, 0};  // (with one sequence a thread it is kept)
+    const auto units = [&](int s) {
+        const Units u = units_of<KEYS, ROWS>(a, seq_of(a, s));
+        return (int64_t)(u.committed + u.drafted) * a.unit_heads;
+    };
+    int64_t mine = 0, all;
+    for (int s = s0; s < s1; ++s) mine += units(s);
+    int64_t at = sum_before(mine, sums, &all);
     for (int s = s0; s < s1; ++s) {
-        one = share_of(a, s);
-        work += one.units * one.items;
+        base[s] = held_int(at);
+        at += each > 1 ? units(s) : 0;  // (with one sequence a thread it is not needed)
     }
-    sum_before(work, sums, &all);
-    const int64_t even = all / kWant + 1;
-    const int size = even < (1 << 30) ? (int)even : 1 << 30;
-    int64_t mine = 0, split = 0;
-    for (int s = s0; s < s1; ++s) {
-        if (each > 1) one = share_of(a, s);
-        const int p = parts_of(one.items, size);
-        mine += JOIN ? p > 1 ? one.units : 0 : one.units * p;
-        split += p > 1 ? one.units * p : 0;
-    }
-    int64_t b = sum_before(mine, sums, &all), ignored, at = sum_before(split, sums, &ignored);
-    for (int s = s0; s < s1; ++s) {
-        if (each > 1) one = share_of(a, s);
-        const int p = parts_of(one.items, size);
-        base[s] = b < kNoMore ? (int)b : kNoMore;
-        slot[s] = at < kNoMore ? (int)at : kNoMore;
-        b += JOIN ? p > 1 ? one.units : 0 : one.units * p;
-        at += p > 1 ? one.units * p : 0;
-    }
-    if (threadIdx.x == 0) base[a.seqs] = all < kNoMore ? (int)all : kNoMore;
+    if (threadIdx.x == 0) base[a.seqs] = held_int(all);
     __syncthreads();
-    return size;
 }
 
 // The last sequence whose work begins at or before x.
@@ -140,78 +111,97 @@ __device__ __forceinline__ int seq_at(const int32_t* base, int n, int x) {
 }
 
 __device__ __forceinline__ uint64_t low64(int n) { return n >= 64 ? ~uint64_t(0) : n <= 0 ? 0 : (uint64_t(1) << n) - 1; }
-
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // A unit's keys and where their sums go.
 struct Unit {
-    int seq, tile, head;  // the tile of 64 (of the committed or the drafted), -1: all heads
+    int seq, key0, head;  // first key (of the committed or the drafted); -1: all heads
     bool past;
 };
 
+template <int KEYS>
 __device__ __forceinline__ Unit unit_at(const WeightsArgs& a, int s, const Units& u, int i) {
     Unit r;
     r.seq = s;
     const int t = a.unit_heads > 1 ? uniform(i / a.unit_heads) : i;
     r.head = a.unit_heads > 1 ? i - t * a.unit_heads : a.heads > 1 ? -1 : 0;
     r.past = t < u.committed;
-    r.tile = r.past ? u.tile0 + t : t - u.committed;
+    r.key0 = (r.past ? u.tile0 + t : t - u.committed) * KEYS;
     return r;
 }
 
-// Of the keys of a unit, those that exist.  (Lanes of a column of 16 ask for the same.)
-__device__ __forceinline__ uint64_t exist_in(const WeightsArgs& a, const Unit& u, const Seq& q, int (&page)[4]) {
-    if (!u.past) return low64(q.n - u.tile * kKeys);
+// Of the 16 NT keys from u.key0 on, those that exist, and the pages of the committed ones.
+// (Lanes of a column of 16 ask for the same.)
+template <int NT>
+__device__ __forceinline__ uint64_t exist_in(const WeightsArgs& a, const Unit& u, const Seq& q, int (&page)[NT]) {
+    if (!u.past) return low64(q.n - u.key0) & low64(16 * NT);
     const int lane = (int)threadIdx.x & 63;
     uint64_t r = 0;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const int j = u.tile * kKeys + 16 * t + (lane & 15);
+    for (int t = 0; t < NT; ++t) {
+        const int j = u.key0 + 16 * t + (lane & 15);
         page[t] = -1;
         if (j < q.length) page[t] = a.table[(size_t)u.seq * a.max_pages + (j >> a.log_page)];
         if ((uint32_t)page[t] >= (uint32_t)a.pages) page[t] = -1;
-        r |= (uint64_t)(__ballot(page[t] >= 0) & 0xFFFFu) << (16 * t);
     }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) r |= (uint64_t)(__ballot(page[t] >= 0) & 0xFFFFu) << (16 * t);
     return r;
 }
 
-// Adds a lane's sum of key `key` of the unit.
+// Adds a sum of key u.key0 + key.
 __device__ __forceinline__ void add_to(const WeightsArgs& a, const Unit& u, const Seq& q, uint64_t exist, int key, float v) {
     if (!((exist >> key) & 1)) return;
-    const int64_t set = a.first_set + (u.head > 0 && a.sets > 1 ? u.head : 0), j = (int64_t)u.tile * kKeys + key;
+    const int64_t set = a.first_set + (u.head > 0 && a.sets > 1 ? u.head : 0), j = (int64_t)u.key0 + key;
     float* const to = u.past ? a.weight + ((int64_t)u.seq * a.sets + set) * a.positions + j
                              : a.draft_weight + set * a.draft_rows + q.d0 + j;
     *to = *to + v;
 }
 
-// A wavefront keeps the keys of its tile in registers, as the first operand of the matrix
-// cores, and takes the rows 16 at a time as the second: lane l then holds the scores
-// of row l % 16 with keys 16 t + 4 (l / 16) + i, so a row's lse is one number a lane,
-// and the sums over rows are additions in place; the 16 lanes of a key are added at the end.
-template <int TYPE, int DP>
+// Which of the keys from k0 on a row sees (those that exist aside).
+__device__ __forceinline__ uint64_t sees(const WeightsArgs& a, const Seq& q, const Unit& u, int node, const Sight& see) {
+    if (u.past) return ~low64(see.from - u.key0);
+    uint64_t bits = low64(see.end - u.key0) & ~low64(see.first - u.key0);
+    if (a.mask && bits)  // (a mask reaches see.end)
+        bits &= a.mask[(int64_t)(q.q0 + node) * a.mask_words + u.key0 / 64] >> (u.key0 % 64);
+    return bits;
+}
+
+// First channel of lane group g in step u: the order of channels is free, and with 8 bits
+// the 16 bytes of a load serve two steps.
+template <int TYPE>
+__device__ __forceinline__ int channel(int u, int g) {
+    return TYPE == RAC_CACHE_FP8 ? 64 * (u / 2) + 16 * g + 8 * (u % 2) : 32 * u + 8 * g;
+}
+
+// A wavefront keeps 16 NT keys in registers, as the first operand of the matrix cores, and
+// takes the rows 16 at a time as the second: lane l then holds the scores of row l % 16
+// with keys 16 t + 4 (l / 16) + i, so a row's lse is one number a lane, and the sums over
+// rows are additions in place; the 16 lanes of a key are added at the end.
+template <int TYPE, int DP, int NT>
 struct Keys {
     static constexpr int kSteps = DP / 32;
-    u32x4 k[4][kSteps];
+    u32x4 k[NT][kSteps];
 
-    // First channel of lane group g in step u: the order of channels is free, and with 8
-    // bits the 16 bytes of a load serve two steps.
-    static __device__ __forceinline__ int channel(int u, int g) {
-        return TYPE == RAC_CACHE_FP8 ? 64 * (u / 2) + 16 * g + 8 * (u % 2) : 32 * u + 8 * g;
+    __device__ __forceinline__ void take(const WeightsArgs& a, const Unit& u, const Seq& q, int head, const int (&page)[NT]) {
+        if (u.past)
+            committed(a, u, head, page);
+        else
+            drafted(a, u, q, head);
     }
-
-    __device__ __forceinline__ void committed(const WeightsArgs& a, const Unit& u, int head, const int (&page)[4]) {
+    __device__ __forceinline__ void committed(const WeightsArgs& a, const Unit& u, int head, const int (&page)[NT]) {
         constexpr int kB = TYPE == RAC_CACHE_FP8 ? 1 : 2;
         const int lane = (int)threadIdx.x & 63, g = lane >> 4;
         const uint64_t plane = ((uint64_t)a.dim << a.log_page) * kB;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int j = u.tile * kKeys + 16 * t + (lane & 15);
+        for (int t = 0; t < NT; ++t) {
+            const int j = u.key0 + 16 * t + (lane & 15);
             const uint8_t* const at = a.pool + (((uint64_t)(page[t] < 0 ? 0 : page[t]) * a.layers + a.layer) * 2 * a.heads + head) * plane +
                                       (uint64_t)((j & ((1 << a.log_page) - 1)) * a.dim * kB);
             if constexpr (TYPE == RAC_CACHE_FP8) {
 #pragma unroll
                 for (int s = 0; s < kSteps; s += 2) {
-                    const int c = channel(s, g);
+                    const int c = channel<TYPE>(s, g);
                     u32x4 x = {0u, 0u, 0u, 0u};
                     if (c < a.dim && page[t] >= 0) x = *reinterpret_cast<const u32x4*>(at + c);
                     k[t][s] = widen8(x[0], x[1]);
@@ -220,7 +210,7 @@ struct Keys {
             } else {
 #pragma unroll
                 for (int s = 0; s < kSteps; ++s) {
-                    const int c = channel(s, g);
+                    const int c = channel<TYPE>(s, g);
                     k[t][s] = u32x4{0u, 0u, 0u, 0u};
                     if (c < a.dim && page[t] >= 0) k[t][s] = *reinterpret_cast<const u32x4*>(at + 2 * c);
                 }
@@ -230,12 +220,12 @@ struct Keys {
     __device__ __forceinline__ void drafted(const WeightsArgs& a, const Unit& u, const Seq& q, int head) {
         const int lane = (int)threadIdx.x & 63, g = lane >> 4;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int j = u.tile * kKeys + 16 * t + (lane & 15);
+        for (int t = 0; t < NT; ++t) {
+            const int j = u.key0 + 16 * t + (lane & 15);
             const uint16_t* const at = a.k + (int64_t)(q.d0 + j) * a.kv_stride + (int64_t)head * a.dim;
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
-                const int c = channel(s, g);
+                const int c = channel<TYPE>(s, g);
                 k[t][s] = u32x4{0u, 0u, 0u, 0u};
                 if (c < a.dim && j < q.n) k[t][s] = *reinterpret_cast<const u32x4*>(at + c);
             }
@@ -243,156 +233,357 @@ struct Keys {
     }
 };
 
-// 16 rows: their queries, and their lse in powers of two (infinity: nothing to give).
-template <int TYPE, int DP>
-struct Queries {
-    static constexpr int kSteps = DP / 32;
-    u32x4 q[kSteps];
-    float lse2;
-    int node;   // -1: no row
-    bool none;  // a row that gives nothing
+template <int NT>
+struct KeySums {
+    f32x4 s[NT];
 
-    __device__ __forceinline__ void take(const WeightsArgs& a, const Seq& s, int head, int tile) {
-        const int lane = (int)threadIdx.x & 63, r = tile * kRowTile + (lane & 15);
-        const bool is = r < s.m * a.group;
-        const int n = a.group == 1 ? r : (int)__umulhi((uint32_t)r, a.by_group);
-        node = is ? n : -1;
-        lse2 = INFINITY;
-        const int h = head * a.group + r - n * a.group;
-        const int64_t row = s.q0 + n;
-        if (is) lse2 = a.lse[row * (a.heads * a.group) + h] * 1.44269504f;
-        none = lse2 == -INFINITY;
-        const uint16_t* const at = a.q + row * a.q_stride + (int64_t)h * a.dim;
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int u = 0; u < kSteps; ++u) {
-            const int c = Keys<TYPE, DP>::channel(u, lane >> 4);
-            q[u] = u32x4{0u, 0u, 0u, 0u};
-            if (is && c < a.dim) q[u] = *reinterpret_cast<const u32x4*>(at + c);
+        for (int t = 0; t < NT; ++t) s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    // Of 16 rows that see every key (what does not exist is not stored).
+    __device__ __forceinline__ void add(const f32x4 (&x)[NT], float c2, float lse2) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) s[t][y] = s[t][y] + __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][y], c2, -lse2));
+    }
+    // bits: the keys that this lane's row sees.
+    __device__ __forceinline__ void add_some(const f32x4 (&x)[NT], float c2, float lse2, uint64_t bits) {
+        const int g = ((int)threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const uint32_t b = (uint32_t)(bits >> (16 * t)) >> (4 * g);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][y], c2, -lse2));
+                s[t][y] = s[t][y] + ((b >> y) & 1u ? e : 0.0f);
+            }
         }
     }
+    // Over the 16 lanes of a key: halves of the sums change places, until every lane has
+    // one, that of key key_of_lane().
+    __device__ __forceinline__ float join() const {
+        const int lane = (int)threadIdx.x & 63;
+        float v[4 * NT];
+#pragma unroll
+        for (int i = 0; i < 4 * NT; ++i) v[i] = s[i / 4][i % 4];
+#pragma unroll
+        for (int o = 8; o > 0; o /= 2) {
+            if (o >= 4 * NT) {
+#pragma unroll
+                for (int i = 0; i < 4 * NT; ++i) v[i] = v[i] + __shfl_xor(v[i], o);
+                continue;
+            }
+            const bool high = lane & o;
+#pragma unroll
+            for (int i = 0; i < o; ++i) {
+                const float keep = high ? v[i + o] : v[i], give = high ? v[i] : v[i + o];
+                v[i] = keep + __shfl_xor(give, o);
+            }
+        }
+        return v[0];
+    }
+    static __device__ __forceinline__ int key_of_lane() {
+        const int lane = (int)threadIdx.x & 63, i = lane & (4 * NT - 1) & 15;
+        return 16 * (i >> 2) + 4 * (lane >> 4) + (i & 3);
+    }
+    // (with fewer than 16 sums several lanes have the same)
+    static __device__ __forceinline__ bool first_lane() { return ((int)threadIdx.x & 15) < 4 * NT; }
 };
 
-// Bound by the bytes of the committed keys where sequences have few rows, and by the
-// exponentials (a quarter of the matrix cores' rate for 128 channels) where they
-// have many.
-template <int TYPE, int DP>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : DP == 128 ? 2 : 3) void weights_kernel(WeightsArgs a) {
-    extern __shared__ int32_t starts[];  // base [seqs + 1], slot [seqs]
-    int32_t* const base = starts;
-    int32_t* const slot = starts + a.seqs + 1;
-    const int size = lay_out<false>(a, base, slot);
-    const int lane = (int)threadIdx.x & 63;
-    const int total = base[a.seqs], step = (int)gridDim.x * kWavesEach;
-    for (int64_t w = (int64_t)blockIdx.x * kWavesEach + __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64); w < total; w += step) {
-        const int s = __builtin_amdgcn_readfirstlane(seq_at(base, a.seqs, (int)w));
+// ---------------------------------------------------------------------------
+// Few rows a head.  A wavefront takes 32 keys and goes through heads and tiles of 16 rows.
+// With SHARE (sums of all heads) the wavefronts of a workgroup have the same keys and
+// divide heads and rows; else each has a unit of its own.
+//
+// Bound by the bytes of the committed keys.
+constexpr int kFewKeys = 32, kFewRows = 16;
+
+template <int TYPE, int DP, bool SHARE>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 4) void weights_few_kernel(WeightsArgs a) {
+    constexpr int NT = kFewKeys / 16, kSteps = DP / 32;
+    extern __shared__ int32_t base[];  // [seqs + 1]
+    __shared__ float shared_sums[2][kWavesEach][kFewKeys];
+    lay_out<kFewKeys, kFewRows>(a, base);
+    const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x / 64);
+    const int total = base[a.seqs];
+    int turn = 0;
+    for (int64_t w = SHARE ? blockIdx.x : (int64_t)blockIdx.x * kWavesEach + wave; w < total;
+         w += SHARE ? gridDim.x : gridDim.x * kWavesEach) {
+        const int s = uniform(seq_at(base, a.seqs, (int)w));
         const Seq q = seq_of(a, s);
-        const Units us = units_of(a, q);
-        const int items = us.rows * a.item_heads, parts = uniform(parts_of(items, size));
-        const int i = uniform((int)w - base[s]), of = uniform(i / parts), part = i - of * parts;
-        const Unit u = unit_at(a, s, us, of);
-        int page[4];
+        const Units us = units_of<kFewKeys, kFewRows>(a, q);
+        const Unit u = unit_at<kFewKeys>(a, s, us, uniform((int)w - base[s]));
+        int page[NT];
         const uint64_t exist = exist_in(a, u, q, page);
         const float c2 = TYPE == RAC_CACHE_FP8 && u.past ? a.scale2 * a.k_scale : a.scale2;
         const bool look = !u.past || a.window > 0;  // whether rows differ in what they see
-        f32x4 sum[4];
+        KeySums<NT> sums;
+        sums.clear();
+        const int items = us.rows * a.item_heads;
+        int at = SHARE ? items * wave / kWavesEach : 0;
+        const int end = SHARE ? items * (wave + 1) / kWavesEach : items;
+        while (at < end) {
+            const int head = u.head >= 0 ? u.head : us.rows == 1 ? at : uniform(at / us.rows), h0 = u.head >= 0 ? 0 : head * us.rows;
+            const int stop = h0 + us.rows < end ? h0 + us.rows : end;
+            Keys<TYPE, DP, NT> keys;
+            keys.take(a, u, q, head, page);
+            for (; at < stop; ++at) {
+                const int r = (at - h0) * kFewRows + (lane & 15);
+                const int n = a.group == 1 ? r : (int)__umulhi((uint32_t)r, a.by_group), h = head * a.group + r - n * a.group;
+                const bool is = r < q.m * a.group;
+                const int64_t row = q.q0 + n;
+                float lse2 = -INFINITY;  // (a row that gives nothing)
+                if (is) lse2 = a.lse[row * (a.heads * a.group) + h] * 1.44269504f;
+                u32x4 qs[kSteps];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) sum[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        const int even = uniform(items / parts), more = items - even * parts;
-        const int i0 = part * even + (part < more ? part : more), i1 = i0 + even + (part < more);
-        for (int at = i0; at < i1;) {
-            const int head = u.head >= 0 ? u.head : uniform(at / us.rows), h0 = u.head >= 0 ? 0 : head * us.rows;
-            const int end = h0 + us.rows < i1 ? h0 + us.rows : i1;
-            Keys<TYPE, DP> keys;
-            if (u.past)
-                keys.committed(a, u, head, page);
-            else
-                keys.drafted(a, u, q, head);
-            Queries<TYPE, DP> next;
-            next.take(a, q, head, at - h0);
-            for (; at < end; ++at) {
-                const Queries<TYPE, DP> now = next;
-                if (at + 1 < end) next.take(a, q, head, at + 1 - h0);
-                uint64_t bits = now.none ? 0 : exist;
-                if (look && now.node >= 0 && !now.none) {
-                    const Sight see = sight_of(a, q, now.node);
-                    const int k0 = u.tile * kKeys;
-                    if (u.past) {
-                        bits &= ~low64(see.from - k0);
-                    } else {
-                        bits &= low64(see.end - k0) & ~low64(see.first - k0);
-                        if (a.mask && bits) bits &= a.mask[(int64_t)(q.q0 + now.node) * a.mask_words + u.tile];
-                    }
+                for (int y = 0; y < kSteps; ++y) {
+                    const int c = channel<TYPE>(y, lane >> 4);
+                    qs[y] = u32x4{0u, 0u, 0u, 0u};
+                    if (is && c < a.dim) qs[y] = *reinterpret_cast<const u32x4*>(a.q + row * a.q_stride + (int64_t)h * a.dim + c);
                 }
-                if (!__any(now.node >= 0 && bits)) continue;
-                const bool all = !__any(now.node < 0 || bits != exist);
-                const float ref = now.lse2;
+                uint64_t bits = lse2 == -INFINITY ? 0 : exist;
+                if (look && bits) bits &= sees(a, q, u, n, sight_of(a, q, n));
+                if (!__any(bits != 0)) continue;
+                f32x4 x[NT];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+                for (int t = 0; t < NT; ++t) {
+                    x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int y = 0; y < DP / 32; ++y) x = mma<TYPE>(keys.k[t][y], now.q[y], x);
-                    if (all) {
-#pragma unroll
-                        for (int y = 0; y < 4; ++y)
-                            sum[t][y] = sum[t][y] + __builtin_amdgcn_exp2f(__builtin_fmaf(x[y], c2, -ref));
-                    } else {
-                        const uint32_t b = (uint32_t)(bits >> (16 * t)) >> (4 * (lane >> 4));
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[y], c2, -ref));
-                            sum[t][y] = sum[t][y] + (now.node >= 0 && (b >> y) & 1u ? e : 0.0f);
-                        }
-                    }
+                    for (int y = 0; y < kSteps; ++y) x[t] = mma<TYPE>(keys.k[t][y], qs[y], x[t]);
                 }
+                sums.add_some(x, c2, lse2, bits);
             }
         }
-        // over the 16 lanes of a key: halves of the sums change places, until every lane has one
-        float v[16];
+        float v = sums.join();
+        const int key = KeySums<NT>::key_of_lane();
+        if constexpr (SHARE) {
+            if (KeySums<NT>::first_lane()) shared_sums[turn][wave][key] = v;
+            __syncthreads();
+            if (threadIdx.x < kFewKeys) {
+                v = 0.0f;
 #pragma unroll
-        for (int t = 0; t < 16; ++t) v[t] = sum[t / 4][t % 4];
-#pragma unroll
-        for (int o = 8; o > 0; o /= 2) {
-            const bool high = lane & o;
-#pragma unroll
-            for (int t = 0; t < o; ++t) {
-                const float keep = high ? v[t + o] : v[t], give = high ? v[t] : v[t + o];
-                v[t] = keep + __shfl_xor(give, o);
+                for (int y = 0; y < kWavesEach; ++y) v = v + shared_sums[turn][y][threadIdx.x];
+                add_to(a, u, q, exist, (int)threadIdx.x, v);
             }
-        }
-        const int key = 16 * ((lane & 15) >> 2) + 4 * (lane >> 4) + (lane & 3);
-        if (parts == 1) {
-            add_to(a, u, q, exist, key, v[0]);
-        } else {
-            const int64_t to = (int64_t)slot[s] + i;
-            if (to < a.slots) a.parts[to * kKeys + key] = v[0];
+            turn ^= 1;  // (what is read here is written again only after the next barrier)
+        } else if (KeySums<NT>::first_lane()) {
+            add_to(a, u, q, exist, key, v);
         }
     }
 }
 
-// Adds the parts of the units that were cut, in order: a wavefront a unit, a lane a key.
+// ---------------------------------------------------------------------------
+// Many rows a head.  A workgroup takes 256 keys, 64 a wavefront, and goes through blocks
+// of 64 rows, which it shares in LDS: the next block's loads are under way during the
+// products of this one.  A unit is cut into parts of at most `size` blocks, which about
+// kWant workgroups share out, and the parts are joined.
+//
+// Bound by the exponentials: for 128 channels and 16 rows by 64 keys the matrix cores are
+// busy for 256 cycles and the vector unit for 384, 256 of them exponentials.
+constexpr int kManyKeys = 256, kManyRows = 64, kWant = 2048;
+constexpr int kSlots = 2 * kWant;  // (a unit that is cut has fewer than twice its blocks over the size parts)
+
+// base[s]: where the parts of a sequence (with JOIN: its units that were cut) begin, slot[s]
+// its partial results.  Returns the size of a part.
+template <bool JOIN>
+__device__ __forceinline__ int lay_out_parts(const WeightsArgs& a, int32_t* base, int32_t* slot) {
+    __shared__ int64_t sums[kWavesEach];
+    const int each = (a.seqs + kThreads - 1) / kThreads, s0 = (int)threadIdx.x * each;
+    const int s1 = s0 + each < a.seqs ? s0 + each : a.seqs;
+    struct Share {
+        int64_t units;
+        int items;
+    };
+    const auto share = [&](int s) {
+        const Units u = units_of<kManyKeys, kManyRows>(a, seq_of(a, s));
+        return Share{(int64_t)(u.committed + u.drafted) * a.unit_heads, u.rows * a.item_heads};
+    };
+    int64_t work = 0, all;
+    Share one{0, 0};  // (with one sequence a thread it is kept)
+    for (int s = s0; s < s1; ++s) {
+        one = share(s);
+        work += one.units * one.items;
+    }
+    sum_before(work, sums, &all);
+    const int64_t even = all / kWant + 1;
+    const int size = even < (1 << 30) ? (int)even : 1 << 30;
+    const auto parts = [&](int items) { return items > size ? (items + size - 1) / size : 1; };
+    int64_t mine = 0, split = 0;
+    for (int s = s0; s < s1; ++s) {
+        if (each > 1) one = share(s);
+        const int p = parts(one.items);
+        mine += JOIN ? p > 1 ? one.units : 0 : one.units * p;
+        split += p > 1 ? one.units * p : 0;
+    }
+    int64_t b = sum_before(mine, sums, &all), ignored, at = sum_before(split, sums, &ignored);
+    for (int s = s0; s < s1; ++s) {
+        if (each > 1) one = share(s);
+        const int p = parts(one.items);
+        base[s] = held_int(b);
+        slot[s] = held_int(at);
+        b += JOIN ? p > 1 ? one.units : 0 : one.units * p;
+        at += p > 1 ? one.units * p : 0;
+    }
+    if (threadIdx.x == 0) base[a.seqs] = held_int(all);
+    __syncthreads();
+    return size;
+}
+
+template <int TYPE, int DP>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void weights_many_kernel(WeightsArgs a) {
+    constexpr int NT = 4, kSteps = DP / 32, kPieces = DP / 8, kLoads = kManyRows * kPieces / kThreads;
+    extern __shared__ int32_t starts[];  // base [seqs + 1], slot [seqs]
+    __shared__ u32x4 block[2][kManyRows * kPieces];
+    __shared__ float lses[2][kManyRows];
+    __shared__ Sight sights[2][kManyRows];
+    int32_t* const base = starts;
+    int32_t* const slot = starts + a.seqs + 1;
+    const int size = lay_out_parts<false>(a, base, slot);
+    const int t = (int)threadIdx.x, lane = t & 63, wave = uniform(t / 64);
+    const int total = base[a.seqs];
+    for (int w = (int)blockIdx.x; w < total; w += (int)gridDim.x) {
+        const int s = uniform(seq_at(base, a.seqs, w));
+        const Seq q = seq_of(a, s);
+        const Units us = units_of<kManyKeys, kManyRows>(a, q);
+        const int rows = q.m * a.group, all_items = us.rows * a.item_heads;
+        const int parts = all_items > size ? uniform((all_items + size - 1) / size) : 1;
+        const int i = uniform(w - base[s]), of = uniform(i / parts), part = i - of * parts;
+        Unit u = unit_at<kManyKeys>(a, s, us, of);
+        // (without a mask no row ahead of the first drafted key sees any)
+        int skip = 0;
+        if (!u.past && !a.mask) {
+            const int64_t first = (int64_t)(u.key0 - (q.n - q.m)) * a.group / kManyRows;
+            skip = first <= 0 ? 0 : first < us.rows ? (int)first : us.rows;
+        }
+        const int blocks = us.rows - skip, items = blocks * a.item_heads;
+        const int even = uniform(items / parts), more = items - even * parts;
+        const int i0 = part * even + (part < more ? part : more), i1 = i0 + even + (part < more);
+        u.key0 += 64 * wave;
+        int page[NT];
+        const uint64_t exist = exist_in(a, u, q, page);
+        const float c2 = TYPE == RAC_CACHE_FP8 && u.past ? a.scale2 * a.k_scale : a.scale2;
+        const bool look = !u.past || a.window > 0;  // whether rows differ in what they see
+        KeySums<NT> sums;
+        sums.clear();
+        u32x4 ahead[kLoads];
+        float lse_ahead = 0.0f;
+        Sight sight_ahead{0, 0, 0};
+        const auto head_of = [&](int item) { return u.head >= 0 ? u.head : blocks > 0 ? uniform(item / blocks) : 0; };
+        const auto fetch = [&](int item) {
+            const int head = head_of(item), r0 = (skip + item - (u.head >= 0 ? 0 : head * blocks)) * kManyRows;
+            const auto row_at = [&](int r, int& node, int& h) {
+                node = a.group == 1 ? r : (int)__umulhi((uint32_t)r, a.by_group);
+                h = head * a.group + r - node * a.group;
+            };
+#pragma unroll
+            for (int y = 0; y < kLoads; ++y) {
+                const int piece = t + y * kThreads, r = r0 + piece / kPieces, c = piece % kPieces * 8;
+                int node, h;
+                row_at(r, node, h);
+                ahead[y] = u32x4{0u, 0u, 0u, 0u};
+                if (r < rows && c < a.dim)
+                    ahead[y] = *reinterpret_cast<const u32x4*>(a.q + (int64_t)(q.q0 + node) * a.q_stride + (int64_t)h * a.dim + c);
+            }
+            if (t < kManyRows) {
+                int node, h;
+                row_at(r0 + t, node, h);
+                lse_ahead = -INFINITY;  // (a row that gives nothing)
+                if (r0 + t < rows) {
+                    lse_ahead = a.lse[(int64_t)(q.q0 + node) * (a.heads * a.group) + h] * 1.44269504f;
+                    if (look) sight_ahead = sight_of(a, q, node);
+                }
+            }
+        };
+        const auto put = [&](int to) {
+#pragma unroll
+            for (int y = 0; y < kLoads; ++y) {
+                const uint32_t piece = t + y * kThreads;
+                block[to][piece_at<DP>(piece / kPieces, piece % kPieces)] = ahead[y];
+            }
+            if (t < kManyRows) {
+                lses[to][t] = lse_ahead;
+                if (look) sights[to][t] = sight_ahead;
+            }
+        };
+        if (i0 < i1) {
+            fetch(i0);
+            put(0);
+        }
+        Keys<TYPE, DP, NT> keys;
+        int of_head = -1, now = 0;
+        for (int at = i0; at < i1; ++at, now ^= 1) {
+            __syncthreads();
+            const int head = head_of(at), r0 = (skip + at - (u.head >= 0 ? 0 : head * blocks)) * kManyRows;
+            if (at + 1 < i1) fetch(at + 1);
+            if (head != of_head) {
+                keys.take(a, u, q, head, page);
+                of_head = head;
+            }
+            if (exist) {
+#pragma unroll
+                for (int rt = 0; rt < kManyRows / 16; ++rt) {
+                    const int in = 16 * rt + (lane & 15);
+                    const float lse2 = lses[now][in];
+                    uint64_t bits = lse2 == -INFINITY ? 0 : exist;
+                    if (look && bits) {
+                        const int r = r0 + in, node = a.group == 1 ? r : (int)__umulhi((uint32_t)r, a.by_group);
+                        bits &= sees(a, q, u, node, sights[now][in]);
+                    }
+                    if (!__any(bits != 0)) continue;
+                    f32x4 x[NT];
+#pragma unroll
+                    for (int y = 0; y < kSteps; ++y) {
+                        const u32x4 qs = block[now][piece_at<DP>(in, channel<TYPE>(y, lane >> 4) / 8)];
+#pragma unroll
+                        for (int k = 0; k < NT; ++k) x[k] = mma<TYPE>(keys.k[k][y], qs, y ? x[k] : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+                    }
+                    if (__any(bits != exist))
+                        sums.add_some(x, c2, lse2, bits);
+                    else
+                        sums.add(x, c2, lse2);
+                }
+            }
+            if (at + 1 < i1) put(now ^ 1);
+        }
+        __syncthreads();  // (the next unit's first block takes the place of one that is read)
+        const float v = sums.join();
+        const int key = KeySums<NT>::key_of_lane();
+        if (parts == 1) {
+            add_to(a, u, q, exist, key, v);
+        } else {
+            const int64_t to = (int64_t)slot[s] + i;
+            if (to < kSlots) a.parts[to * kManyKeys + 64 * wave + key] = v;
+        }
+    }
+}
+
+// Adds the parts of the units that were cut, in order: a workgroup a unit, a thread a key.
 __global__ __launch_bounds__(kThreads) void weights_join_kernel(WeightsArgs a) {
     extern __shared__ int32_t starts[];
     int32_t* const base = starts;
     int32_t* const slot = starts + a.seqs + 1;
-    const int size = lay_out<true>(a, base, slot);
-    const int lane = (int)threadIdx.x & 63;
-    const int total = base[a.seqs], step = (int)gridDim.x * kWavesEach;
-    for (int64_t w = (int64_t)blockIdx.x * kWavesEach + __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64); w < total; w += step) {
-        const int s = __builtin_amdgcn_readfirstlane(seq_at(base, a.seqs, (int)w));
+    const int size = lay_out_parts<true>(a, base, slot);
+    const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x / 64);
+    const int total = base[a.seqs];
+    for (int w = (int)blockIdx.x; w < total; w += (int)gridDim.x) {
+        const int s = uniform(seq_at(base, a.seqs, w));
         const Seq q = seq_of(a, s);
-        const Units us = units_of(a, q);
-        const int parts = uniform(parts_of(us.rows * a.item_heads, size)), i = uniform((int)w - base[s]);
-        const Unit u = unit_at(a, s, us, i);
+        const Units us = units_of<kManyKeys, kManyRows>(a, q);
+        const int items = us.rows * a.item_heads, parts = uniform((items + size - 1) / size), i = uniform(w - base[s]);
+        Unit u = unit_at<kManyKeys>(a, s, us, i);
+        u.key0 += 64 * wave;
         int page[4];
         const uint64_t exist = exist_in(a, u, q, page);
         const int64_t from = (int64_t)slot[s] + (int64_t)i * parts;
-        if (from + parts > a.slots) continue;
+        if (from + parts > kSlots) continue;
         float v = 0.0f;
         constexpr int kAtOnce = 8;
         for (int p = 0; p < parts; p += kAtOnce) {
             float x[kAtOnce];
 #pragma unroll
-            for (int y = 0; y < kAtOnce; ++y) x[y] = p + y < parts ? a.parts[(from + p + y) * kKeys + lane] : 0.0f;
+            for (int y = 0; y < kAtOnce; ++y) x[y] = p + y < parts ? a.parts[(from + p + y) * kManyKeys + threadIdx.x] : 0.0f;
 #pragma unroll
             for (int y = 0; y < kAtOnce; ++y) v = v + x[y];
         }
@@ -433,19 +624,25 @@ __global__ __launch_bounds__(kThreads) void weights_append_kernel(AppendArgs a) 
 // ---------------------------------------------------------------------------
 // Host side
 
-constexpr int kSlots = 2 * kWant;  // (a unit that is cut has fewer than twice its items over the size parts)
-
 bool weights_valid(const rac_cache_config* c, const rac_tree_config* t) {
     return cache_valid(c) && t && t->q_heads >= 1 && t->q_heads % c->kv_heads == 0 && t->q_heads / c->kv_heads <= 64 &&
            t->rows >= 0 && t->rows <= (1 << 20) && t->max_rows >= 0 && t->max_draft >= 0 && t->window >= 0 &&
            t->scale >= 0.0f && t->scale < __builtin_inff();
 }
 
+// The kernel of a call: from 64 rows a key-value head on that of many rows; below it the
+// wavefronts share a unit's heads and rows where there are enough of them.
+enum Form { kMany, kShare, kAlone };
+
+template <int TYPE, int DP>
+const void* kernel_of(Form form) {
+    return form == kMany    ? reinterpret_cast<const void*>(weights_many_kernel<TYPE, DP>)
+           : form == kShare ? reinterpret_cast<const void*>(weights_few_kernel<TYPE, DP, true>)
+                            : reinterpret_cast<const void*>(weights_few_kernel<TYPE, DP, false>);
+}
 template <int TYPE>
-const void* kernel_of(int dim) {
-    return dim <= 64    ? reinterpret_cast<const void*>(weights_kernel<TYPE, 64>)
-           : dim <= 128 ? reinterpret_cast<const void*>(weights_kernel<TYPE, 128>)
-                        : reinterpret_cast<const void*>(weights_kernel<TYPE, 256>);
+const void* kernel_of(Form form, int dim) {
+    return dim <= 64 ? kernel_of<TYPE, 64>(form) : dim <= 128 ? kernel_of<TYPE, 128>(form) : kernel_of<TYPE, 256>(form);
 }
 
 rac_status start(const void* kernel, dim3 grid, void* args, size_t lds, hipStream_t st) {
@@ -458,7 +655,7 @@ rac_status start(const void* kernel, dim3 grid, void* args, size_t lds, hipStrea
 extern "C" {
 
 size_t rac_tree_weights_workspace(const rac_cache_config* cfg, const rac_tree_config* tree) {
-    return weights_valid(cfg, tree) && (int64_t)tree->rows * tree->q_heads < (int64_t(1) << 26) ? (size_t)kSlots * kKeys * 4 : 0;
+    return weights_valid(cfg, tree) && (int64_t)tree->rows * tree->q_heads < (int64_t(1) << 26) ? (size_t)kSlots * kManyKeys * 4 : 0;
 }
 
 rac_status rac_tree_weights(const rac_cache_config* cfg, const rac_tree_config* tree, int32_t layer, int32_t sets,
@@ -514,15 +711,17 @@ rac_status rac_tree_weights(const rac_cache_config* cfg, const rac_tree_config* 
     a.first_set = sets > 1 ? layer * cfg->kv_heads : 0;
     a.unit_heads = sets > 1 ? cfg->kv_heads : 1;
     a.item_heads = cfg->kv_heads / a.unit_heads;
-    a.slots = kSlots;
     a.by_group = (uint32_t)(((uint64_t(1) << 32) + a.group - 1) / a.group);
     a.scale2 = (tree->scale > 0.0f ? tree->scale : 1.0f / sqrtf((float)cfg->head_dim)) * 1.4426950408889634f;
     a.k_scale = cfg->k_scale;
-    const void* kernel = cfg->type == RAC_CACHE_BF16   ? kernel_of<RAC_CACHE_BF16>(cfg->head_dim)
-                         : cfg->type == RAC_CACHE_FP16 ? kernel_of<RAC_CACHE_FP16>(cfg->head_dim)
-                                                       : kernel_of<RAC_CACHE_FP8>(cfg->head_dim);
+    const int64_t most = (int64_t)(tree->max_rows < tree->rows ? tree->max_rows : tree->rows) * a.group;
+    const Form form = most >= kManyRows ? kMany : (most + kFewRows - 1) / kFewRows * a.item_heads >= kWavesEach ? kShare : kAlone;
+    const void* kernel = cfg->type == RAC_CACHE_BF16   ? kernel_of<RAC_CACHE_BF16>(form, cfg->head_dim)
+                         : cfg->type == RAC_CACHE_FP16 ? kernel_of<RAC_CACHE_FP16>(form, cfg->head_dim)
+                                                       : kernel_of<RAC_CACHE_FP8>(form, cfg->head_dim);
     const size_t lds = (size_t)(2 * cfg->seqs + 1) * 4;
-    const rac_status st = start(kernel, dim3(1024), &a, lds, stream);
+    if (form != kMany) return start(kernel, dim3(cfg->head_dim > 128 ? 512 : 1024), &a, lds, stream);
+    const rac_status st = start(kernel, dim3(cfg->head_dim > 128 ? 256 : 512), &a, lds, stream);
     return st != RAC_OK ? st : start(reinterpret_cast<const void*>(weights_join_kernel), dim3(512), &a, lds, stream);
 }
 

@@ -92,7 +92,7 @@ def calls_of_the_gpu_tests():
             for alike in (0, 1):
                 calls.append(("backward", [9, 3001, 9, 0, type], [entropy, alike]))
         for dim in (64, 128, 256):
-            for shape in ((8, 20, 2), (2, 300, 130), (2, 21, 1)):
+            for shape in ((8, 20, 2), (8, 30, 6), (2, 300, 130)):
                 calls.append(("weights", [2, 2, dim, 16, 100, 13, 20, type], [shape[0], shape[1], shape[2], shape[2]]))
     calls.append(("append", [2, 3, 16, 8, 200, 5, 20], None))
     for cfg in ([2, 3, 32, 16, 100, 14, 20], [1, 1, 16, 8, 900, 1100, 10], [1, 2, 16, 64, 2000, 3, 1200]):
