@@ -263,25 +263,26 @@ struct KeySums {
     }
     // Over the 16 lanes of a key: halves of the sums change places, until every lane has
     // one, that of key key_of_lane().
+    template <int O>
+    static __device__ __forceinline__ void halve(float (&v)[4 * NT]) {
+        if constexpr (O >= 4 * NT) {
+#pragma unroll
+            for (int i = 0; i < 4 * NT; ++i) v[i] = v[i] + __shfl_xor(v[i], O);
+        } else {
+            const bool high = threadIdx.x & O;
+#pragma unroll
+            for (int i = 0; i < O; ++i) {
+                const float keep = high ? v[i + O] : v[i], give = high ? v[i] : v[i + O];
+                v[i] = keep + __shfl_xor(give, O);
+            }
+        }
+        if constexpr (O > 1) halve<O / 2>(v);
+    }
     __device__ __forceinline__ float join() const {
-        const int lane = (int)threadIdx.x & 63;
         float v[4 * NT];
 #pragma unroll
         for (int i = 0; i < 4 * NT; ++i) v[i] = s[i / 4][i % 4];
-#pragma unroll
-        for (int o = 8; o > 0; o /= 2) {
-            if (o >= 4 * NT) {
-#pragma unroll
-                for (int i = 0; i < 4 * NT; ++i) v[i] = v[i] + __shfl_xor(v[i], o);
-                continue;
-            }
-            const bool high = lane & o;
-#pragma unroll
-            for (int i = 0; i < o; ++i) {
-                const float keep = high ? v[i + o] : v[i], give = high ? v[i] : v[i + o];
-                v[i] = keep + __shfl_xor(give, o);
-            }
-        }
+        halve<8>(v);
         return v[0];
     }
     static __device__ __forceinline__ int key_of_lane() {
@@ -382,7 +383,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 4) void weights_few_kerne
 //
 // Bound by the exponentials: for 128 channels and 16 rows by 64 keys the matrix cores are
 // busy for 256 cycles and the vector unit for 384, 256 of them exponentials.
-constexpr int kManyKeys = 256, kManyRows = 64, kWant = 2048;
+constexpr int kManyKeys = 256, kManyRows = 64, kWant = 3000;
 constexpr int kSlots = 2 * kWant;  // (a unit that is cut has fewer than twice its blocks over the size parts)
 
 // base[s]: where the parts of a sequence (with JOIN: its units that were cut) begin, slot[s]
@@ -438,6 +439,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void weights_many_kern
     __shared__ u32x4 block[2][kManyRows * kPieces];
     __shared__ float lses[2][kManyRows];
     __shared__ Sight sights[2][kManyRows];
+    __shared__ alignas(4) uint8_t whole[2][kWavesEach];  // whether all rows that a wavefront brought give something
     int32_t* const base = starts;
     int32_t* const slot = starts + a.seqs + 1;
     const int size = lay_out_parts<false>(a, base, slot);
@@ -467,82 +469,103 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void weights_many_kern
         const bool look = !u.past || a.window > 0;  // whether rows differ in what they see
         KeySums<NT> sums;
         sums.clear();
+        // Four threads bring a row: of the next block, on its way.  (Where that is: its head, and
+        // its first row.)
         u32x4 ahead[kLoads];
         float lse_ahead = 0.0f;
         Sight sight_ahead{0, 0, 0};
-        const auto head_of = [&](int item) { return u.head >= 0 ? u.head : blocks > 0 ? uniform(item / blocks) : 0; };
-        const auto fetch = [&](int item) {
-            const int head = head_of(item), r0 = (skip + item - (u.head >= 0 ? 0 : head * blocks)) * kManyRows;
-            const auto row_at = [&](int r, int& node, int& h) {
-                node = a.group == 1 ? r : (int)__umulhi((uint32_t)r, a.by_group);
-                h = head * a.group + r - node * a.group;
-            };
+        int next_head = u.head >= 0 ? u.head : blocks > 0 ? uniform(i0 / blocks) : 0;
+        int next_row = (skip + i0 - (u.head >= 0 ? 0 : next_head * blocks)) * kManyRows;
+        const auto node_of = [&](int r) { return a.group == 1 ? r : (int)__umulhi((uint32_t)r, a.by_group); };
+        const auto fetch = [&] {
+            const int r = next_row + t / 4, node = node_of(r), h = next_head * a.group + r - node * a.group;
+            const uint16_t* const from = a.q + (int64_t)(q.q0 + node) * a.q_stride + (int64_t)h * a.dim;
+            const bool is = r < rows;
 #pragma unroll
             for (int y = 0; y < kLoads; ++y) {
-                const int piece = t + y * kThreads, r = r0 + piece / kPieces, c = piece % kPieces * 8;
-                int node, h;
-                row_at(r, node, h);
+                const int c = 8 * (t % 4 + 4 * y);
                 ahead[y] = u32x4{0u, 0u, 0u, 0u};
-                if (r < rows && c < a.dim)
-                    ahead[y] = *reinterpret_cast<const u32x4*>(a.q + (int64_t)(q.q0 + node) * a.q_stride + (int64_t)h * a.dim + c);
+                if (is && c < a.dim) ahead[y] = *reinterpret_cast<const u32x4*>(from + c);
             }
-            if (t < kManyRows) {
-                int node, h;
-                row_at(r0 + t, node, h);
-                lse_ahead = -INFINITY;  // (a row that gives nothing)
-                if (r0 + t < rows) {
-                    lse_ahead = a.lse[(int64_t)(q.q0 + node) * (a.heads * a.group) + h] * 1.44269504f;
-                    if (look) sight_ahead = sight_of(a, q, node);
-                }
-            }
+            lse_ahead = -INFINITY;  // (a row that gives nothing)
+            if (is) lse_ahead = a.lse[(int64_t)(q.q0 + node) * (a.heads * a.group) + h] * 1.44269504f;
+            if (look && is) sight_ahead = sight_of(a, q, node);
         };
         const auto put = [&](int to) {
 #pragma unroll
-            for (int y = 0; y < kLoads; ++y) {
-                const uint32_t piece = t + y * kThreads;
-                block[to][piece_at<DP>(piece / kPieces, piece % kPieces)] = ahead[y];
+            for (int y = 0; y < kLoads; ++y) block[to][piece_at<DP>((uint32_t)t / 4, (uint32_t)(t % 4 + 4 * y))] = ahead[y];
+            if (t % 4 == 0) {
+                lses[to][t / 4] = lse_ahead;
+                if (look) sights[to][t / 4] = sight_ahead;
             }
-            if (t < kManyRows) {
-                lses[to][t] = lse_ahead;
-                if (look) sights[to][t] = sight_ahead;
-            }
+            const bool all = __all(lse_ahead != -INFINITY);
+            if (lane == 0) whole[to][wave] = all;
         };
         if (i0 < i1) {
-            fetch(i0);
+            fetch();
             put(0);
         }
+        uint32_t piece[kSteps];  // of this lane's row in a tile of 16
+#pragma unroll
+        for (int y = 0; y < kSteps; ++y) piece[y] = piece_at<DP>((uint32_t)lane & 15u, (uint32_t)(channel<TYPE>(y, lane >> 4) / 8));
         Keys<TYPE, DP, NT> keys;
         int of_head = -1, now = 0;
         for (int at = i0; at < i1; ++at, now ^= 1) {
             __syncthreads();
-            const int head = head_of(at), r0 = (skip + at - (u.head >= 0 ? 0 : head * blocks)) * kManyRows;
-            if (at + 1 < i1) fetch(at + 1);
+            const int head = next_head, r0 = next_row;
+            next_row += kManyRows;
+            if (next_row >= us.rows * kManyRows) {
+                next_row = skip * kManyRows;
+                ++next_head;
+            }
+            if (at + 1 < i1) fetch();
             if (head != of_head) {
                 keys.take(a, u, q, head, page);
                 of_head = head;
             }
-            if (exist) {
+            const uint32_t given = *reinterpret_cast<const uint32_t*>(whole[now]);
+            const u32x4* const tile = block[now];
+            const auto products = [&](int rt, f32x4 (&x)[NT]) {
 #pragma unroll
+                for (int y = 0; y < kSteps; ++y) {
+                    const u32x4 qs = tile[rt * 16 * kPieces + piece[y]];
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) x[k] = mma<TYPE>(keys.k[k][y], qs, y ? x[k] : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+                }
+            };
+            // (without a mask what a row sees moves on with the rows: the first and the last of the
+            // block tell whether all see every key, or none any)
+            bool plain = !look, none = exist == 0;
+            if (look && !a.mask && !none) {
+                const int last_row = r0 + kManyRows < rows ? r0 + kManyRows - 1 : rows - 1;
+                const Sight first = sight_of(a, q, uniform(node_of(r0))), last = sight_of(a, q, uniform(node_of(last_row)));
+                if (u.past) {
+                    plain = last.from <= u.key0;
+                    none = first.from >= u.key0 + 64;
+                } else {
+                    plain = last.first <= u.key0 && first.end >= (u.key0 + 64 < q.n ? u.key0 + 64 : q.n);
+                    none = last.end <= u.key0 || first.first >= u.key0 + 64;
+                }
+            }
+            if (none) {
+            } else if (plain && given == 0x01010101u) {
+#pragma unroll
+                for (int rt = 0; rt < kManyRows / 16; ++rt) {
+                    f32x4 x[NT];
+                    products(rt, x);
+                    sums.add(x, c2, lses[now][16 * rt + (lane & 15)]);
+                }
+            } else {
+#pragma unroll 1
                 for (int rt = 0; rt < kManyRows / 16; ++rt) {
                     const int in = 16 * rt + (lane & 15);
                     const float lse2 = lses[now][in];
                     uint64_t bits = lse2 == -INFINITY ? 0 : exist;
-                    if (look && bits) {
-                        const int r = r0 + in, node = a.group == 1 ? r : (int)__umulhi((uint32_t)r, a.by_group);
-                        bits &= sees(a, q, u, node, sights[now][in]);
-                    }
+                    if (look && bits) bits &= sees(a, q, u, node_of(r0 + in), sights[now][in]);
                     if (!__any(bits != 0)) continue;
                     f32x4 x[NT];
-#pragma unroll
-                    for (int y = 0; y < kSteps; ++y) {
-                        const u32x4 qs = block[now][piece_at<DP>(in, channel<TYPE>(y, lane >> 4) / 8)];
-#pragma unroll
-                        for (int k = 0; k < NT; ++k) x[k] = mma<TYPE>(keys.k[k][y], qs, y ? x[k] : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-                    }
-                    if (__any(bits != exist))
-                        sums.add_some(x, c2, lse2, bits);
-                    else
-                        sums.add(x, c2, lse2);
+                    products(rt, x);
+                    sums.add_some(x, c2, lse2, bits);
                 }
             }
             if (at + 1 < i1) put(now ^ 1);
