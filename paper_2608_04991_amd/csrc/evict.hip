@@ -21,6 +21,13 @@ struct EvictRecord {
     int32_t base;     // where its pages begin in the list of free ones, -1: refused
 };
 
+// What stays of the places in [lo, hi): those above the bar, and the first `left` at it.
+struct Choice {
+    int32_t lo, hi, left;
+    uint32_t bar;
+    bool ties;  // whether not all of those at the bar stay
+};
+
 struct EvictArgs {
     uint8_t* pool;
     int32_t* table;
@@ -38,8 +45,12 @@ struct EvictArgs {
     int32_t* list;        // [seqs][sets][positions]: holes from the front, what fills them from the back
     int32_t* holes;       // [seqs][sets]
     uint64_t* hole_bits;  // [seqs][sets][words]
+    int32_t* digits;      // [seqs][sets][3][2048], counts of weights' digits, and
+    int32_t* tally;       // [seqs][sets][split][4], of parts, and
+    Choice* chosen;       // [seqs][sets], where a sequence has several parts
     int64_t positions, words;
-    int32_t layers, heads, row_bytes, log_page, pages, seqs, max_pages, sets, first, recent, parts;
+    int32_t split, part, digit;
+    int32_t layers, heads, row_bytes, log_page, pages, seqs, max_pages, sets, first, recent, parts, end_parts;
 
     __device__ __forceinline__ int64_t sums(int s, int set) const { return ((int64_t)s * sets + set); }
     // The position of a place.
@@ -65,166 +76,317 @@ __device__ __forceinline__ uint32_t rank_of(float x) {
 }
 
 // ---------------------------------------------------------------------------
-// First launch: a workgroup a sequence and set.  The places of the sequence; the
-// weight that divides what stays from what goes, digit by digit from the top (counts of
-// 2048 values in LDS); and, in one ordered pass, the holes and what fills them.
+// First: the places of a sequence; the weight that divides what stays from what goes,
+// digit by digit from the top (counts of 2048 values in LDS); and, in one ordered pass, the
+// holes and what fills them.
 constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64, kDigit = 2048;
+constexpr int kSteps = 8, kChunk = kPickThreads * kSteps;  // places a thread and a workgroup has at once
 
-__global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a) {
-    __shared__ int32_t count[kDigit];
-    __shared__ int32_t sums[kPickWaves], more[kPickWaves], found[3];
-    const int t = (int)threadIdx.x, lane = t & 63, wv = t / 64, page = 1 << a.log_page;
+__device__ __forceinline__ Choice choice_of(const EvictArgs& a, const EvictRecord& r) {
+    const int recent = r.n - r.border;
+    Choice c{a.first < r.border ? a.first : r.border, r.m - recent, 0, 0, false};
+    c.left = r.border - c.lo;
+    if (c.left == 0) c.bar = ~0u;  // (no weight has this rank)
+    return c;
+}
+
+// The record and the pages of a sequence, by a workgroup.
+__device__ EvictRecord see(const EvictArgs& a, int s, int set, int32_t* sums) {
+    const int t = (int)threadIdx.x, page = 1 << a.log_page;
+    EvictRecord r{};
+    r.length = clamp_int(a.lengths[s], 0, a.max_pages << a.log_page);
+    const int keep = a.keep[s], used = (r.length + page - 1) >> a.log_page;
+    const int32_t* const row = a.table + (int64_t)s * a.max_pages;
+    __syncthreads();
+    // how many positions have a page
+    int mine = 0, all;
+    for (int d = t; d < used; d += kPickThreads) mine += (uint32_t)row[d] < (uint32_t)a.pages;
+    scan_workgroup<kPickWaves>(mine, sums, &all);
+    r.pages = all;
+    r.gaps = all != used;
+    const int tail = r.length & (page - 1);
+    const bool whole = tail == 0 || (uint32_t)row[used - 1] >= (uint32_t)a.pages;
+    r.m = (all << a.log_page) - (whole ? 0 : page - tail);
+    r.cut = keep >= 0 && r.m > keep;
+    r.n = r.cut ? keep : r.m;
+    r.border = r.n - (a.recent < r.n ? a.recent : r.n);
+    if (set == 0 && t == 0) a.record[s] = r;
+    if (!r.cut) return r;
+    if (set == 0 || r.gaps) {  // (with gaps every set needs the places: they write the same)
+        int at = 0;
+        for (int d0 = 0; d0 < used; d0 += kPickThreads) {
+            const int p = d0 + t < used ? row[d0 + t] : -1;
+            const bool is = (uint32_t)p < (uint32_t)a.pages;
+            const int to = at + scan_workgroup<kPickWaves>(is, sums, &all);
+            if (is) {
+                a.old_page[(int64_t)s * a.max_pages + to] = p;
+                a.old_at[(int64_t)s * a.max_pages + to] = d0 + t;
+            }
+            at += all;
+        }
+        __syncthreads();
+    }
+    return r;
+}
+
+// The places of a thread in the chunk at p0, 64 kSteps in a row to a wavefront.
+__device__ __forceinline__ int place_of(int p0, int y) {
+    return p0 + (int)threadIdx.x / 64 * 64 * kSteps + 64 * y + ((int)threadIdx.x & 63);
+}
+
+__device__ __forceinline__ void load_places(const EvictArgs& a, const EvictRecord& r, int s, const float* w, const Choice& c,
+                                            int p0, uint32_t (&k)[kSteps]) {
+    int at[kSteps];
+    float x[kSteps];
+#pragma unroll
+    for (int y = 0; y < kSteps; ++y) {  // (those outside read a place inside, and are not counted)
+        const int p = place_of(p0, y);
+        at[y] = p < c.lo ? c.lo : p < c.hi ? p : c.hi - 1;
+    }
+    if (r.gaps)
+#pragma unroll
+        for (int y = 0; y < kSteps; ++y) at[y] = a.position(r, s, at[y]);
+#pragma unroll
+    for (int y = 0; y < kSteps; ++y) x[y] = w[at[y]];
+#pragma unroll
+    for (int y = 0; y < kSteps; ++y) k[y] = rank_of(x[y]);
+}
+
+// Counts the values of a digit, among those whose higher digits are the bar's.
+__device__ __forceinline__ void count_places(const Choice& c, int digit, int p0, const uint32_t (&k)[kSteps], int32_t* count) {
+    const int lane = (int)threadIdx.x & 63, shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
+    const uint32_t high = digit == 0 ? 0 : ~0u << (shift + bits), mask = (1u << bits) - 1;
+#pragma unroll
+    for (int y = 0; y < kSteps; ++y) {
+        const int p = place_of(p0, y);
+        const bool in = p >= c.lo && p < c.hi && ((k[y] ^ c.bar) & high) == 0;
+        const uint64_t who = __ballot(in);
+        if (!who) continue;
+        // (weights that are alike, zeros for one, would queue up at one counter)
+        const uint32_t v = (k[y] >> shift) & mask, one = __builtin_amdgcn_readlane(v, __builtin_ctzll(who));
+        if (__ballot(in && v == one) == who) {
+            if (lane == __builtin_ctzll(who)) atomicAdd(count + one, __popcll(who));
+        } else if (in) {
+            atomicAdd(count + v, 1);
+        }
+    }
+}
+
+// The digit at which the counts from the top reach what is left.
+__device__ void take_digit(Choice& c, int digit, const int32_t* count, int32_t* sums, int32_t* found) {
+    const int t = (int)threadIdx.x, shift = digit == 0 ? 21 : digit == 1 ? 10 : 0;
+    int all;
+    const int c1 = count[kDigit - 1 - 2 * t], c0 = count[kDigit - 2 - 2 * t];
+    const int above = scan_workgroup<kPickWaves>(c0 + c1, sums, &all);
+    if (above < c.left && c.left <= above + c1) {
+        found[0] = kDigit - 1 - 2 * t;
+        found[1] = above;
+        found[2] = c1;
+    } else if (above + c1 < c.left && c.left <= above + c1 + c0) {
+        found[0] = kDigit - 2 - 2 * t;
+        found[1] = above + c1;
+        found[2] = c0;
+    }
+    __syncthreads();
+    c.bar |= (uint32_t)found[0] << shift;
+    c.left -= found[1];
+    c.ties = found[2] > c.left;
+    __syncthreads();
+}
+
+// Holes before the border and what stays behind it, of the places in [begin, end), in
+// order, after nh, nf and (at the bar) nt of earlier ones; k has them if there is one chunk only.
+__device__ void order_places(const EvictArgs& a, const EvictRecord& r, int s, int set, const Choice& c, int begin, int end,
+                             bool held, uint32_t (&k)[kSteps], int& nh, int& nf, int& nt, int32_t* sums, int32_t* more) {
+    const int lane = (int)threadIdx.x & 63, wv = (int)threadIdx.x / 64;
     const uint64_t below = (uint64_t(1) << lane) - 1;
+    const float* const w = a.weight + a.sums(s, set) * a.positions;
+    int32_t* const list = a.list + a.sums(s, set) * a.positions;
+    uint64_t* const bits = a.hole_bits + a.sums(s, set) * a.words;
+    for (int p0 = begin; p0 < end; p0 += kChunk) {
+        if (!held) load_places(a, r, s, w, c, p0, k);
+        uint64_t hole[kSteps], fill[kSteps];
+        int h = 0, f = 0, before = nt;
+        if (c.ties) {
+            int e = 0;
+#pragma unroll
+            for (int y = 0; y < kSteps; ++y) {
+                const int p = place_of(p0, y);
+                e += __popcll(__ballot(p >= c.lo && p < c.hi && k[y] == c.bar));
+            }
+            __syncthreads();
+            if (lane == 0) sums[wv] = e;
+            __syncthreads();
+            for (int x = 0; x < kPickWaves; ++x) {
+                before += x < wv ? sums[x] : 0;
+                nt += sums[x];
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < kSteps; ++y) {
+            const int p = place_of(p0, y);
+            const bool at_bar = p >= c.lo && p < c.hi && k[y] == c.bar;
+            bool stays = p < c.lo || k[y] > c.bar || at_bar;
+            if (c.ties) {
+                const uint64_t tie = __ballot(at_bar);
+                stays &= !at_bar || before + __popcll(tie & below) < c.left;
+                before += __popcll(tie);
+            }
+            hole[y] = __ballot(p < r.border && !stays);
+            fill[y] = __ballot(p >= r.border && p < c.hi && stays);
+            h += __popcll(hole[y]);
+            f += __popcll(fill[y]);
+        }
+        __syncthreads();
+        if (lane == 0) {
+            sums[wv] = h;
+            more[wv] = f;
+        }
+        __syncthreads();
+        int ah = nh, af = nf;
+        for (int x = 0; x < kPickWaves; ++x) {
+            ah += x < wv ? sums[x] : 0;
+            af += x < wv ? more[x] : 0;
+            nh += sums[x];
+            nf += more[x];
+        }
+#pragma unroll
+        for (int y = 0; y < kSteps; ++y) {
+            const int p = place_of(p0, y), q = p - lane;
+            if ((hole[y] >> lane) & 1) list[ah + __popcll(hole[y] & below)] = p;
+            if ((fill[y] >> lane) & 1) list[a.positions - 1 - (af + __popcll(fill[y] & below))] = p;
+            if (lane == 0 && q < r.border) bits[q / 64] = hole[y];
+            ah += __popcll(hole[y]);
+            af += __popcll(fill[y]);
+        }
+    }
+}
+
+// A workgroup a sequence and set does it all.
+__global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a) {
+    __shared__ int32_t count[kDigit], sums[kPickWaves], more[kPickWaves], found[3];
+    const int t = (int)threadIdx.x, s = (int)blockIdx.y;
+    for (int set = (int)blockIdx.x; set < a.sets; set += (int)gridDim.x) {
+        const EvictRecord r = see(a, s, set, sums);
+        if (!r.cut) continue;
+        const float* const w = a.weight + a.sums(s, set) * a.positions;
+        Choice c = choice_of(a, r);
+        uint32_t k[kSteps];
+        const bool held = c.hi <= kChunk;
+        if (held) load_places(a, r, s, w, c, 0, k);
+        for (int digit = 0; digit < (c.left > 0 ? 3 : 0); ++digit) {
+            for (int i = t; i < kDigit; i += kPickThreads) count[i] = 0;
+            __syncthreads();
+            for (int p0 = 0; p0 < c.hi; p0 += kChunk) {
+                if (!held) load_places(a, r, s, w, c, p0, k);
+                count_places(c, digit, p0, k, count);
+            }
+            __syncthreads();
+            take_digit(c, digit, count, sums, found);
+        }
+        int nh = 0, nf = 0, nt = 0;
+        order_places(a, r, s, set, c, 0, c.hi, held, k, nh, nf, nt, sums, more);
+        if (t == 0) a.holes[a.sums(s, set)] = nh;
+    }
+}
+
+// Long sequences of few sets: `split` workgroups each, of `part` places, and a launch for
+// each of these steps.  The counts are whole numbers, so that their order is no matter.
+__global__ __launch_bounds__(kPickThreads) void evict_see_kernel(EvictArgs a) {
+    __shared__ int32_t sums[kPickWaves];
     const int s = (int)blockIdx.y;
     for (int set = (int)blockIdx.x; set < a.sets; set += (int)gridDim.x) {
-        EvictRecord r{};
-        r.length = clamp_int(a.lengths[s], 0, a.max_pages << a.log_page);
-        const int keep = a.keep[s], used = (r.length + page - 1) >> a.log_page;
-        const int32_t* const row = a.table + (int64_t)s * a.max_pages;
+        see(a, s, set, sums);
+        for (int i = (int)threadIdx.x; i < 3 * kDigit; i += kPickThreads) a.digits[a.sums(s, set) * 3 * kDigit + i] = 0;
+    }
+}
+
+// The choice after some digits, from the counts of all parts.
+__device__ Choice choice_after(const EvictArgs& a, const EvictRecord& r, int s, int set, int digits, int32_t* sums, int32_t* found) {
+    Choice c = choice_of(a, r);
+    for (int digit = 0; digit < (c.left > 0 ? digits : 0); ++digit)
+        take_digit(c, digit, a.digits + (a.sums(s, set) * 3 + digit) * kDigit, sums, found);
+    return c;
+}
+
+__global__ __launch_bounds__(kPickThreads) void evict_count_kernel(EvictArgs a) {
+    __shared__ int32_t count[kDigit], sums[kPickWaves], found[3];
+    const int t = (int)threadIdx.x, s = (int)blockIdx.y;
+    const EvictRecord r = a.record[s];
+    if (!r.cut) return;
+    for (int i = (int)blockIdx.x; i < a.sets * a.split; i += (int)gridDim.x) {
+        const int set = i / a.split, begin = (i - set * a.split) * a.part;
+        const Choice c = choice_after(a, r, s, set, a.digit, sums, found);
+        const int end = begin + a.part < c.hi ? begin + a.part : c.hi;
+        if (c.left == 0 || begin >= end) continue;
+        for (int x = t; x < kDigit; x += kPickThreads) count[x] = 0;
         __syncthreads();
-        // how many positions have a page
-        int mine = 0, all;
-        for (int d = t; d < used; d += kPickThreads) mine += (uint32_t)row[d] < (uint32_t)a.pages;
-        scan_workgroup<kPickWaves>(mine, sums, &all);
-        r.pages = all;
-        r.gaps = all != used;
-        const int tail = r.length & (page - 1);
-        const bool whole = tail == 0 || (uint32_t)row[used - 1] >= (uint32_t)a.pages;
-        r.m = (all << a.log_page) - (whole ? 0 : page - tail);
-        r.cut = keep >= 0 && r.m > keep;
-        r.n = r.cut ? keep : r.m;
-        const int recent = a.recent < r.n ? a.recent : r.n, first = a.first < r.n - recent ? a.first : r.n - recent;
-        r.border = r.n - recent;
-        if (set == 0 && t == 0) a.record[s] = r;
-        if (!r.cut) continue;
-        if (set == 0 || r.gaps) {  // (with gaps every set needs the places: they write the same)
-            int at = 0;
-            for (int d0 = 0; d0 < used; d0 += kPickThreads) {
-                const int p = d0 + t < used ? row[d0 + t] : -1;
-                const bool is = (uint32_t)p < (uint32_t)a.pages;
-                const int to = at + scan_workgroup<kPickWaves>(is, sums, &all);
-                if (is) {
-                    a.old_page[(int64_t)s * a.max_pages + to] = p;
-                    a.old_at[(int64_t)s * a.max_pages + to] = d0 + t;
-                }
-                at += all;
-            }
-            __syncthreads();
-        }
-        const float* const w = a.weight + a.sums(s, set) * a.positions;
-        const int lo = first, hi = r.m - recent;  // the places to choose from
-        int left = r.n - recent - first;          // how many of them stay
-        uint32_t bar = ~0u;                       // (no weight has this rank)
-        bool ties = false;                        // whether not all of those at the bar stay
-        if (left > 0) {
-            bar = 0;
-            for (int digit = 0; digit < 3; ++digit) {
-                const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
-                for (int i = t; i < kDigit; i += kPickThreads) count[i] = 0;
-                __syncthreads();
-                for (int p0 = lo; p0 < hi; p0 += kPickThreads) {
-                    const int p = p0 + t;
-                    bool in = p < hi;
-                    uint32_t v = 0;
-                    if (in) {
-                        const uint32_t k = rank_of(w[a.position(r, s, p)]);
-                        in = digit == 0 || (k >> (shift + bits)) == (bar >> (shift + bits));
-                        v = (k >> shift) & ((1u << bits) - 1);
-                    }
-                    // (weights that are alike, zeros for one, would queue up at one counter)
-                    const uint64_t who = __ballot(in);
-                    if (!who) continue;
-                    const uint32_t one = __builtin_amdgcn_readlane(v, __builtin_ctzll(who));
-                    const uint64_t same = __ballot(in && v == one);
-                    if (lane == __builtin_ctzll(who)) atomicAdd(count + one, __popcll(same));
-                    if (in && v != one) atomicAdd(count + v, 1);
-                }
-                __syncthreads();
-                // the digit at which the counts from the top reach `left`
-                const int c1 = count[kDigit - 1 - 2 * t], c0 = count[kDigit - 2 - 2 * t];
-                const int above = scan_workgroup<kPickWaves>(c0 + c1, sums, &all);
-                if (above < left && left <= above + c1) {
-                    found[0] = kDigit - 1 - 2 * t;
-                    found[1] = above;
-                    found[2] = c1;
-                } else if (above + c1 < left && left <= above + c1 + c0) {
-                    found[0] = kDigit - 2 - 2 * t;
-                    found[1] = above + c1;
-                    found[2] = c0;
-                }
-                __syncthreads();
-                bar |= (uint32_t)found[0] << shift;
-                left -= found[1];
-                ties = found[2] > left;
-                __syncthreads();
-            }
-        }
-        // in the order of places: holes before the border, what stays behind it
-        int32_t* const list = a.list + a.sums(s, set) * a.positions;
-        uint64_t* const bits = a.hole_bits + a.sums(s, set) * a.words;
-        constexpr int kSteps = 4;
-        int nh = 0, nf = 0, nt = 0;
-        for (int p0 = 0; p0 < hi; p0 += kPickThreads * kSteps) {
-            uint64_t hole[kSteps], fill[kSteps], tie[kSteps];
+        for (int p0 = begin; p0 < end; p0 += kChunk) {
             uint32_t k[kSteps];
-            int h = 0, f = 0, e = 0;
+            load_places(a, r, s, a.weight + a.sums(s, set) * a.positions, c, p0, k);
+            count_places(c, a.digit, p0, k, count);
+        }
+        __syncthreads();
+        for (int x = t; x < kDigit; x += kPickThreads)
+            if (count[x]) atomicAdd(a.digits + (a.sums(s, set) * 3 + a.digit) * kDigit + x, count[x]);
+        __syncthreads();
+    }
+}
+
+// How many holes and fills a part has, and how many at the bar on either side of the border.
+__global__ __launch_bounds__(kPickThreads) void evict_tally_kernel(EvictArgs a) {
+    __shared__ int32_t sums[kPickWaves], found[3];
+    const int t = (int)threadIdx.x, s = (int)blockIdx.y;
+    const EvictRecord r = a.record[s];
+    if (!r.cut) return;
+    for (int i = (int)blockIdx.x; i < a.sets * a.split; i += (int)gridDim.x) {
+        const int set = i / a.split, begin = (i - set * a.split) * a.part;
+        const Choice c = choice_after(a, r, s, set, 3, sums, found);
+        const int end = begin + a.part < c.hi ? begin + a.part : c.hi;
+        if (t == 0 && begin == 0) a.chosen[a.sums(s, set)] = c;
+        int of[4] = {0, 0, 0, 0};
+        for (int p0 = begin; p0 < end; p0 += kChunk) {
+            uint32_t k[kSteps];
+            load_places(a, r, s, a.weight + a.sums(s, set) * a.positions, c, p0, k);
 #pragma unroll
             for (int y = 0; y < kSteps; ++y) {
-                const int p = p0 + wv * 64 * kSteps + 64 * y + lane;
-                k[y] = 0;
-                if (p >= lo && p < hi) k[y] = rank_of(w[a.position(r, s, p)]);
-            }
-#pragma unroll
-            for (int y = 0; y < kSteps; ++y) {
-                const int p = p0 + wv * 64 * kSteps + 64 * y + lane;
-                tie[y] = __ballot(p >= lo && p < hi && k[y] == bar);
-                e += __popcll(tie[y]);
-            }
-            int before = nt;
-            if (ties) {
-                __syncthreads();
-                if (lane == 0) sums[wv] = e;
-                __syncthreads();
-                for (int x = 0; x < kPickWaves; ++x) {
-                    before += x < wv ? sums[x] : 0;
-                    nt += sums[x];
-                }
-            }
-#pragma unroll
-            for (int y = 0; y < kSteps; ++y) {
-                const int p = p0 + wv * 64 * kSteps + 64 * y + lane;
-                const bool at_bar = (tie[y] >> lane) & 1;
-                const bool stays = p < lo || k[y] > bar || (at_bar && (!ties || before + __popcll(tie[y] & below) < left));
-                before += __popcll(tie[y]);
-                hole[y] = __ballot(p < r.border && !stays);
-                fill[y] = __ballot(p >= r.border && p < hi && stays);
-                h += __popcll(hole[y]);
-                f += __popcll(fill[y]);
-            }
-            __syncthreads();
-            if (lane == 0) {
-                sums[wv] = h;
-                more[wv] = f;
-            }
-            __syncthreads();
-            int ah = nh, af = nf;
-            for (int x = 0; x < kPickWaves; ++x) {
-                ah += x < wv ? sums[x] : 0;
-                af += x < wv ? more[x] : 0;
-                nh += sums[x];
-                nf += more[x];
-            }
-#pragma unroll
-            for (int y = 0; y < kSteps; ++y) {
-                const int q = p0 + wv * 64 * kSteps + 64 * y, p = q + lane;
-                if ((hole[y] >> lane) & 1) list[ah + __popcll(hole[y] & below)] = p;
-                if ((fill[y] >> lane) & 1) list[a.positions - 1 - (af + __popcll(fill[y] & below))] = p;
-                if (lane == 0 && q < r.border) bits[q / 64] = hole[y];
-                ah += __popcll(hole[y]);
-                af += __popcll(fill[y]);
+                const int p = place_of(p0, y);
+                const bool in = p >= c.lo && p < c.hi, early = p < r.border, at_bar = in && k[y] == c.bar, above = k[y] > c.bar;
+                of[0] += in && early && !at_bar && !above;
+                of[1] += in && !early && above;
+                of[2] += early && at_bar;
+                of[3] += !early && at_bar;
             }
         }
-        if (t == 0) a.holes[a.sums(s, set)] = nh;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            int all;
+            scan_workgroup<kPickWaves>(of[x], sums, &all);
+            if (t == 0) a.tally[(a.sums(s, set) * a.split + i - set * a.split) * 4 + x] = all;
+        }
+    }
+}
+
+__global__ __launch_bounds__(kPickThreads) void evict_order_kernel(EvictArgs a) {
+    __shared__ int32_t sums[kPickWaves], more[kPickWaves];
+    const int s = (int)blockIdx.y;
+    const EvictRecord r = a.record[s];
+    if (!r.cut) return;
+    for (int i = (int)blockIdx.x; i < a.sets * a.split; i += (int)gridDim.x) {
+        const int set = i / a.split, part = i - set * a.split, begin = part * a.part;
+        const Choice c = a.chosen[a.sums(s, set)];
+        const int end = begin + a.part < c.hi ? begin + a.part : c.hi;
+        int nh = 0, nf = 0, nt = 0;
+        for (int x = 0; x < part; ++x) {
+            const int32_t* const of = a.tally + (a.sums(s, set) * a.split + x) * 4;
+            const int ties = of[2] + of[3], stay = clamp_int(c.left - nt, 0, ties), early = stay < of[2] ? stay : of[2];
+            nh += of[0] + of[2] - early;
+            nf += of[1] + stay - early;
+            nt += ties;
+        }
+        uint32_t k[kSteps];
+        if (begin < end) order_places(a, r, s, set, c, begin, end, false, k, nh, nf, nt, sums, more);
+        if (threadIdx.x == 0 && part == a.split - 1) a.holes[a.sums(s, set)] = nh;
     }
 }
 
@@ -365,10 +527,15 @@ struct Lane {
 __device__ void move_unit(const EvictArgs& a, const EvictRecord& r, int s, int lh, int part) {
     const int layer = lh / a.heads, head = lh - layer * a.heads, set = a.sets > 1 ? lh : 0, page = 1 << a.log_page;
     const Lane l(a.row_bytes, kMoveThreads);
-    if (!l.on) return;
     const int32_t* const list = a.list + a.sums(s, set) * a.positions;
     const int32_t* const old_page = a.old_page + (int64_t)s * a.max_pages;
     const int holes = a.holes[a.sums(s, set)];
+    if (!r.gaps && (a.sets > 1 || lh == 0)) {  // the sums, once a set
+        float* const w = a.weight + a.sums(s, set) * a.positions;
+        for (int64_t e = (int64_t)part * kMoveThreads + threadIdx.x; e < holes; e += (int64_t)a.parts * kMoveThreads)
+            w[list[e]] = w[list[a.positions - 1 - e]];
+    }
+    if (!l.on) return;
     constexpr int kAtOnce = 4;
     for (int64_t e0 = part * l.step + l.first; e0 < holes; e0 += (int64_t)a.parts * l.step * kAtOnce) {
         u32x4 x[kAtOnce];
@@ -410,23 +577,26 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Last launch, what the moves had to be ahead of: the last tokens shift, a workgroup a
-// (sequence, layer, head), read ahead of where they are written; the sums of weights,
-// a workgroup a (sequence, set); table, counts and lengths, a workgroup a sequence.
-constexpr int kEndThreads = 256;
+// Last launch, what the moves had to be ahead of: the last tokens shift; the sums of
+// weights move; table, counts and lengths.  Where the last tokens shift by less than their
+// number, one workgroup a (sequence, layer, head) reads ahead of where it writes; else
+// `parts` of them share the rows.  The sums' tail becomes zeros, by `parts` workgroups too.
+constexpr int kEndThreads = 512;
 
-__device__ void shift_recent(const EvictArgs& a, const EvictRecord& r, int s, int layer, int head) {
-    const int by = r.m - r.n;
+__device__ void shift_recent(const EvictArgs& a, const EvictRecord& r, int s, int layer, int head, int part) {
+    const int by = r.m - r.n, parts = by >= r.n - r.border ? a.end_parts : 1;
+    if (part >= parts) return;
     const Lane l(a.row_bytes, kEndThreads);
     const int32_t* const old_page = a.old_page + (int64_t)s * a.max_pages;
     constexpr int kAtOnce = 4;
-    for (int p0 = r.border; p0 < r.n; p0 += l.step * kAtOnce) {
+    for (int64_t p0 = r.border + (int64_t)part * l.step * kAtOnce; p0 < r.n; p0 += (int64_t)parts * l.step * kAtOnce) {
         u32x4 x[kAtOnce];
         uint8_t* to[kAtOnce];
 #pragma unroll
         for (int y = 0; y < kAtOnce; ++y) {
-            const int p = p0 + y * l.step + l.first, from = p + by;
-            if (!l.on || p >= r.n) continue;
+            const int64_t at = p0 + y * l.step + l.first;
+            if (!l.on || at >= r.n) continue;
+            const int p = (int)at, from = p + by;
             x[y] = *reinterpret_cast<const u32x4*>(a.row_of(old_page[from >> a.log_page], layer, l.side, head, from) + l.byte);
             to[y] = a.row_of(a.page_now(r, s, p >> a.log_page), layer, l.side, head, p) + l.byte;
         }
@@ -470,11 +640,22 @@ __device__ void move_sums(const EvictArgs& a, const EvictRecord& r, int s, int s
         __syncthreads();
         for (int e = t; e < holes; e += kEndThreads) source[list[e]] = a.position(r, s, list[a.positions - 1 - e]);
     }
-    if (r.gaps) shift_sums(w, 0, r.m, [&](int i) { return a.position(r, s, i); });
-    for (int e = t; e < holes; e += kEndThreads) w[list[e]] = w[list[a.positions - 1 - e]];
-    __syncthreads();
+    if (r.gaps) {  // (else the move kernel has filled the holes)
+        shift_sums(w, 0, r.m, [&](int i) { return a.position(r, s, i); });
+        for (int e = t; e < holes; e += kEndThreads) w[list[e]] = w[list[a.positions - 1 - e]];
+        __syncthreads();
+    }
     shift_sums(w, r.border, r.n - r.border, [&](int i) { return r.border + by + i; });
-    for (int p = r.n + t; p < r.length; p += kEndThreads) w[p] = 0.0f;
+    // (the last tokens' former places; with gaps, all from n on)
+    for (int p = (r.gaps || r.m - (r.n - r.border) < r.n ? r.n : r.m - (r.n - r.border)) + t; p < r.length; p += kEndThreads) w[p] = 0.0f;
+}
+
+// Zeros between the cut and the last tokens' former places: what was there has moved.
+__device__ void clear_sums(const EvictArgs& a, const EvictRecord& r, int s, int set, int part) {
+    if (r.gaps) return;  // (the one that moves the sums clears all of it)
+    float* const w = a.weight + a.sums(s, set) * a.positions;
+    const int end = r.m - (r.n - r.border);
+    for (int64_t p = r.n + (int64_t)part * kEndThreads + threadIdx.x; p < end; p += (int64_t)a.end_parts * kEndThreads) w[p] = 0.0f;
 }
 
 __device__ void enter_pages(const EvictArgs& a, const EvictRecord& r, int s) {
@@ -496,16 +677,21 @@ __device__ void enter_pages(const EvictArgs& a, const EvictRecord& r, int s) {
 }
 
 __global__ __launch_bounds__(kEndThreads) void evict_end_kernel(EvictArgs a) {
-    const int s = (int)blockIdx.y, units = a.layers * a.heads;
+    const int s = (int)blockIdx.y, units = a.layers * a.heads * a.end_parts, clears = a.sets * a.end_parts;
     const EvictRecord r = a.record[s];
     if (!r.cut || r.base < 0) return;
-    for (int i = (int)blockIdx.x; i < units + a.sets + 1; i += (int)gridDim.x) {
-        if (i < units)
-            shift_recent(a, r, s, i / a.heads, i % a.heads);
-        else if (i < units + a.sets)
-            move_sums(a, r, s, i - units);
-        else
+    for (int i = (int)blockIdx.x; i < units + clears + a.sets + 1; i += (int)gridDim.x) {
+        if (i < units) {
+            const int unit = i / a.end_parts;
+            shift_recent(a, r, s, unit / a.heads, unit % a.heads, i - unit * a.end_parts);
+        } else if (i < units + clears) {
+            const int set = (i - units) / a.end_parts;
+            clear_sums(a, r, s, set, i - units - set * a.end_parts);
+        } else if (i < units + clears + a.sets) {
+            move_sums(a, r, s, i - units - clears);
+        } else {
             enter_pages(a, r, s);
+        }
     }
 }
 
@@ -518,6 +704,8 @@ bool evict_valid(const rac_cache_config* c, const rac_evict_config* e) {
     return cache_valid(c) && e && sets_valid(c, e->sets) && e->first >= 0 && e->first <= (1 << 30) && e->recent >= 0 &&
            e->recent <= (1 << 30);
 }
+
+constexpr int64_t kSplitChunks = 4;
 
 // The scratch, in order; returns its bytes.
 uint64_t lay_out(const rac_cache_config* c, EvictArgs& a, uint8_t* ws) {
@@ -535,6 +723,9 @@ uint64_t lay_out(const rac_cache_config* c, EvictArgs& a, uint8_t* ws) {
     take(a.list, sums * a.positions);
     take(a.holes, sums);
     take(a.hole_bits, sums * a.words);
+    take(a.digits, a.split > 1 ? sums * 3 * kDigit : 0);
+    take(a.tally, a.split > 1 ? sums * a.split * 4 : 0);
+    take(a.chosen, a.split > 1 ? sums : 0);
     return at;
 }
 
@@ -543,6 +734,11 @@ EvictArgs args_of(const rac_cache_config* c, const rac_evict_config* e) {
     a.positions = (int64_t)c->max_pages * c->page_tokens;
     a.words = (a.positions + 63) / 64;
     a.sets = e->sets;
+    const int64_t units = (int64_t)c->seqs * a.sets, chunks = (a.positions + kChunk - 1) / kChunk;
+    int64_t split = 512 / units;
+    split = chunks < kSplitChunks || split < 2 ? 1 : split < chunks ? split : chunks;
+    a.part = (int32_t)((chunks + split - 1) / split) * kChunk;
+    a.split = (int32_t)((a.positions + a.part - 1) / a.part);
     return a;
 }
 
@@ -598,11 +794,22 @@ rac_status rac_cache_evict(const rac_cache_config* cfg, const rac_evict_config* 
     // (a few workgroups for every compute unit where the sequences and heads are few)
     const int64_t units = (int64_t)cfg->layers * cfg->kv_heads, parts = 2048 / (units * cfg->seqs);
     a.parts = (int32_t)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
-    rac_status st = launch(evict_pick_kernel, evict->sets, cfg->seqs, kPickThreads, a, stream);
+    const int64_t ends = 512 / (units * cfg->seqs);
+    a.end_parts = (int32_t)(ends < 1 ? 1 : ends > 32 ? 32 : ends);
+    rac_status st;
+    if (a.split == 1) {
+        st = launch(evict_pick_kernel, evict->sets, cfg->seqs, kPickThreads, a, stream);
+    } else {
+        const int64_t each = (int64_t)evict->sets * a.split;
+        st = launch(evict_see_kernel, evict->sets, cfg->seqs, kPickThreads, a, stream);
+        for (; st == RAC_OK && a.digit < 3; ++a.digit) st = launch(evict_count_kernel, each, cfg->seqs, kPickThreads, a, stream);
+        if (st == RAC_OK) st = launch(evict_tally_kernel, each, cfg->seqs, kPickThreads, a, stream);
+        if (st == RAC_OK) st = launch(evict_order_kernel, each, cfg->seqs, kPickThreads, a, stream);
+    }
     if (st == RAC_OK) st = launch(evict_demand_kernel, 1, cfg->seqs, kDemandThreads, a, stream);
     if (st == RAC_OK) st = launch(evict_plan_kernel, 1, 1, kPlanThreads, a, stream);
     if (st == RAC_OK) st = launch(evict_move_kernel, units * a.parts, cfg->seqs, kMoveThreads, a, stream);
-    if (st == RAC_OK) st = launch(evict_end_kernel, units + evict->sets + 1, cfg->seqs, kEndThreads, a, stream);
+    if (st == RAC_OK) st = launch(evict_end_kernel, (units + evict->sets) * a.end_parts + evict->sets + 1, cfg->seqs, kEndThreads, a, stream);
     return st;
 }
 

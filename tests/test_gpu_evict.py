@@ -150,6 +150,23 @@ def test_long_sequences(sets):
 
 
 @pytest.mark.parametrize("sets", [1, 2])
+@pytest.mark.parametrize("ties", [0, 2, 100])
+def test_parts_of_sequences(ties, sets):
+    """Long caches, whose sequences several workgroups share, or none: cuts, borders and rows of weights that are alike
+    in any part; short sequences in long caches; places without a page."""
+    for width in (1000, 1500, 2100, 4200):  # positions: to 20000, 28000, and past the length from which parts are made
+        cases = (([19999, 8192, 8193, 1], [9000, 8191, 1, 0]), ([width * 16 - 40, 16384, 100, 0], [16384, 16000, 37, -1]),
+                 ([width * 16 - 16, 12000, 12000, 12000], [width * 16 - 17, 12000, 11999, 3]))
+        for i, (lengths, keep) in enumerate(cases):
+            if max(lengths) > width * 16:
+                continue
+            first, recent = ((0, 0), (5, 3000), (8200, 77))[i]
+            say(f"[gpu] evict {lengths} to {keep} in {width} pages, first {first}, recent {recent}, ties {ties}, sets {sets}")
+            gaps = ((0, 0), (0, 600), (1, 3), (1, 700)) if i < 2 and lengths[1] > 11300 else ()
+            Cache(lengths, 16, 1, 2, 16, 2, sets, width=width, seed=i, ties=ties, gaps=gaps).evict(keep, first, recent)
+
+
+@pytest.mark.parametrize("sets", [1, 2])
 @pytest.mark.parametrize("page", [8, 16, 64])
 def test_shared_pages_are_replaced(page, sets):
     """Forks of one sequence: what the others hold stays, byte for byte."""
