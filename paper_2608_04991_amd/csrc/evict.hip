@@ -80,7 +80,7 @@ __device__ __forceinline__ uint32_t rank_of(float x) {
 // digit by digit from the top (counts of 2048 values in LDS); and, in one ordered pass, the
 // holes and what fills them.
 constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64, kDigit = 2048;
-constexpr int kSteps = 8, kChunk = kPickThreads * kSteps;  // places a thread and a workgroup has at once
+constexpr int kSteps = 4, kChunk = kPickThreads * kSteps;  // places a thread and a workgroup has at once
 
 __device__ __forceinline__ Choice choice_of(const EvictArgs& a, const EvictRecord& r) {
     const int recent = r.n - r.border;
@@ -581,7 +581,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
 // weights move; table, counts and lengths.  Where the last tokens shift by less than their
 // number, one workgroup a (sequence, layer, head) reads ahead of where it writes; else
 // `parts` of them share the rows.  The sums' tail becomes zeros, by `parts` workgroups too.
-constexpr int kEndThreads = 512;
+constexpr int kEndThreads = 256;
 
 __device__ void shift_recent(const EvictArgs& a, const EvictRecord& r, int s, int layer, int head, int part) {
     const int by = r.m - r.n, parts = by >= r.n - r.border ? a.end_parts : 1;
@@ -705,7 +705,7 @@ bool evict_valid(const rac_cache_config* c, const rac_evict_config* e) {
            e->recent <= (1 << 30);
 }
 
-constexpr int64_t kSplitChunks = 4;
+constexpr int64_t kSplitChunks = 8;
 
 // The scratch, in order; returns its bytes.
 uint64_t lay_out(const rac_cache_config* c, EvictArgs& a, uint8_t* ws) {
@@ -735,7 +735,7 @@ EvictArgs args_of(const rac_cache_config* c, const rac_evict_config* e) {
     a.words = (a.positions + 63) / 64;
     a.sets = e->sets;
     const int64_t units = (int64_t)c->seqs * a.sets, chunks = (a.positions + kChunk - 1) / kChunk;
-    int64_t split = 512 / units;
+    int64_t split = 256 / units;
     split = chunks < kSplitChunks || split < 2 ? 1 : split < chunks ? split : chunks;
     a.part = (int32_t)((chunks + split - 1) / split) * kChunk;
     a.split = (int32_t)((a.positions + a.part - 1) / a.part);
@@ -794,7 +794,7 @@ rac_status rac_cache_evict(const rac_cache_config* cfg, const rac_evict_config* 
     // (a few workgroups for every compute unit where the sequences and heads are few)
     const int64_t units = (int64_t)cfg->layers * cfg->kv_heads, parts = 2048 / (units * cfg->seqs);
     a.parts = (int32_t)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
-    const int64_t ends = 512 / (units * cfg->seqs);
+    const int64_t ends = 256 / (units * cfg->seqs);
     a.end_parts = (int32_t)(ends < 1 ? 1 : ends > 32 ? 32 : ends);
     rac_status st;
     if (a.split == 1) {
