@@ -844,9 +844,14 @@ bool logprob_valid(const rac_logprob_config* c) {
            c->type <= RAC_TYPE_FP32 && (c->scale == 0.0f || (c->scale >= 0x1p-40f && c->scale <= 0x1p40f));
 }
 
-// How rows are cut.  Few rows: so that every compute unit has work, into parts of at
-// least two blocks a thread.  With alternatives: into parts that a workgroup of 256
-// threads, or 512, holds in registers.
+// How rows are cut.  Without alternatives: few rows so that every compute unit has work,
+// into parts of at least two blocks a thread (4 rows of 32000 in bf16 6.3 us, with four
+// blocks 7.1; 256 rows of 131072 19.4 us in four parts, 27.8 in two).  With them: into as few
+// parts as workgroups of 512 threads hold in registers, for an own look at alternatives and a
+// join cost more than the bytes (a row of 32000, 8 alternatives: 9.0 us, in seven parts 11.1;
+// 128 rows 10.0 and 14.6).  256 threads do if the part fits (128 rows of 32000 in eight parts
+// 14.6 us, with 512 threads 19.7).  Longer rows are read twice, as if none were wanted (held
+// in registers 600 rows of 131072 take 56 us, read twice 75).
 struct LogprobCut {
     int parts, part_blocks, threads;
     bool held;
@@ -861,7 +866,7 @@ LogprobCut cut_of(const rac_logprob_config* c) {
     const int64_t hold = (blocks + kHeld * 512 - 1) / (kHeld * 512);
     LogprobCut r{};
     r.held = c->top > 0 && hold <= kMostParts;
-    if (r.held && parts < hold) parts = hold;
+    if (r.held) parts = hold;
     r.parts = (int)parts;
     r.part_blocks = (int)((blocks + parts - 1) / parts);
     r.threads = r.held && r.part_blocks > kHeld * 256 ? 512 : 256;
