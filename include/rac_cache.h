@@ -207,7 +207,8 @@ rac_status rac_cache_copy(const rac_cache_config* cfg, const void* src_pool, con
  *
  * Alignments as in rac_tree_attention, weights 4-byte.  RAC_ERR_INVALID (also sets
  * other than 1 or layers * kv_heads), _ALIGN, _UNSUPPORTED (as there, and seqs * sets *
- * positions of 2^36 and more) and _CAPACITY.  Two kernel launches. */
+ * positions of 2^36 and more) and _CAPACITY.  One kernel launch, two where a key-value
+ * head may have 64 rows and more. */
 size_t rac_tree_weights_workspace(const rac_cache_config* cfg, const rac_tree_config* tree);
 
 rac_status rac_tree_weights(const rac_cache_config* cfg, const rac_tree_config* tree, int32_t layer, int32_t sets,
@@ -247,8 +248,8 @@ rac_status rac_cache_weights_commit(const rac_cache_config* cfg, int32_t sets, c
  * state.  A sequence's pages that it shares with nobody are changed in place; pages past the
  * cut are let go.  No other byte of the pool changes.
  *
- * pool 16-byte aligned, workspace 256-byte, the others 4-byte.  Five kernel launches at
- * most.  RAC_ERR_INVALID, _ALIGN, _UNSUPPORTED (seqs * sets * positions of 2^36 and more)
+ * pool 16-byte aligned, workspace 256-byte, the others 4-byte.  Five kernel launches, ten where
+ * workgroups share long sequences.  RAC_ERR_INVALID, _ALIGN, _UNSUPPORTED (seqs * sets * positions of 2^36 and more)
  * and _CAPACITY. */
 typedef struct {
     int32_t sets;   /* 1, or layers * kv_heads                                      */

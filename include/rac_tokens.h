@@ -94,8 +94,8 @@ rac_status rac_rotary(const rac_rotary_config* cfg, const int32_t* pos, const do
  * alternative: where a row has fewer, the rest have id -1 and -infinity.  A row of
  * such logits only has an lse of -infinity, entropy 0, and log probabilities of
  * -infinity; so does one whose lse lies below the range of fp32.  A token outside the
- * vocabulary, or a row outside the rows, scores 0 (padding).  A NaN or +infinity makes its row's lse, entropy and log
- * probabilities NaN; a NaN is no alternative.
+ * vocabulary, or a row outside the rows, scores 0 (padding).  A NaN or +infinity makes
+ * its row's lse, entropy and log probabilities NaN; a NaN is no alternative.
  *
  * Sums are fp32, whatever the type. */
 typedef struct {
@@ -124,7 +124,7 @@ typedef struct {
 size_t rac_logprobs_workspace(const rac_logprob_config* cfg);
 
 /* int32 and fp32 arrays 4-byte aligned, workspace 256-byte.  One kernel launch, one
- * more where few rows are cut into parts and one with token_rows.  RAC_ERR_INVALID,
+ * more where rows are cut into parts and one with token_rows.  RAC_ERR_INVALID,
  * _ALIGN and _CAPACITY (workspace). */
 rac_status rac_logprobs(const rac_logprob_config* cfg, const rac_logprob_tensors* t, void* workspace,
                         size_t workspace_bytes, rac_stream_t stream);

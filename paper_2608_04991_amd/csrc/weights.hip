@@ -298,7 +298,10 @@ struct KeySums {
 // With SHARE (sums of all heads) the wavefronts of a workgroup have the same keys and
 // divide heads and rows; else each has a unit of its own.
 //
-// Bound by the bytes of the committed keys.
+// Bound by the bytes of the committed keys: one token of 32 sequences of 4001 to 16383 in
+// bf16, 8 heads of 128 channels, 591 MB in 117 us, 5.0 TB/s (a large copy reaches 4.9).  200
+// short drafts in a window of 1000, 24 MB in 8 bits, take 17 us: three units or less for a
+// wavefront, and the latency of their pages, keys and rows one after the other.
 constexpr int kFewKeys = 32, kFewRows = 16;
 
 template <int TYPE, int DP, bool SHARE>
@@ -382,7 +385,9 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 4) void weights_few_kerne
 // kWant workgroups share out, and the parts are joined.
 //
 // Bound by the exponentials: for 128 channels and 16 rows by 64 keys the matrix cores are
-// busy for 256 cycles and the vector unit for 384, 256 of them exponentials.
+// busy for 256 cycles and the vector unit for 384, 256 of them exponentials.  Chunks of 701
+// to 2048 rows over 1003 to 6001 tokens, 28 heads on 4 of 128 channels: 170 GFLOP in 300 us,
+// 565 TF/s (a large matrix product reaches 1360), and 8 us for the join.
 constexpr int kManyKeys = 256, kManyRows = 64, kWant = 3000;
 constexpr int kSlots = 2 * kWant;  // (a unit that is cut has fewer than twice its blocks over the size parts)
 
@@ -615,7 +620,7 @@ __global__ __launch_bounds__(kThreads) void weights_join_kernel(WeightsArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// The sums of appended tokens: a lane a token, a wavefront a set.
+// The sums of appended tokens: a lane a token, a wavefront a set.  The time of a launch, 2 us.
 struct AppendArgs {
     const int32_t* lengths;
     const int32_t* committed;
@@ -654,7 +659,11 @@ bool weights_valid(const rac_cache_config* c, const rac_tree_config* t) {
 }
 
 // The kernel of a call: from 64 rows a key-value head on that of many rows; below it the
-// wavefronts share a unit's heads and rows where there are enough of them.
+// wavefronts share a unit's heads and rows where there are enough of them.  16 sequences of
+// 1000 to 8000, 8 heads of 128 channels: the few and the many rows' kernel take 32 and 46 us
+// with 16 rows a head, 41 and 47 with 32, 48 and 49 with 48, 55 and 47 with 64, 84 and 58 with
+// 128.  Shared and alone: sums of all heads, 4 sequences 13 and 21 us, 16 with 16 rows a head
+// 32 and 34; sums for every head 58 and 32.
 enum Form { kMany, kShare, kAlone };
 
 template <int TYPE, int DP>
