@@ -61,7 +61,7 @@ struct EvictArgs {
     __device__ __forceinline__ int page_now(const EvictRecord& r, int s, int d) const {
         const int64_t at = (int64_t)s * max_pages + d;
         const int f = fresh[at];
-        return f < 0 ? old_page[at] : free_list[r.base + f];
+        return *(f < 0 ? old_page + at : free_list + r.base + f);
     }
     __device__ __forceinline__ uint8_t* row_of(int page, int layer, int side, int head, int place) const {
         const uint64_t plane = ((uint64_t)page * layers + layer) * 2 * heads + (uint64_t)side * heads + head;
@@ -78,7 +78,7 @@ __device__ __forceinline__ uint32_t rank_of(float x) {
 // ---------------------------------------------------------------------------
 // First: the places of a sequence; the weight that divides what stays from what goes,
 // digit by digit from the top (counts of 2048 values in LDS); and, in one ordered pass, the
-// holes and what fills them.  Bound by the latency of one workgroup's passes: 14 us for
+// holes and what fills them.  Bound by the latency of one workgroup's passes: 15 us for
 // sequences of up to 4000 (kSteps 8: 17 us), and 9 us more for every 8192 places of a long one.
 constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64, kDigit = 2048;
 constexpr int kSteps = 4, kChunk = kPickThreads * kSteps;  // places a thread and a workgroup has at once
@@ -101,7 +101,17 @@ __device__ EvictRecord see(const EvictArgs& a, int s, int set, int32_t* sums) {
     __syncthreads();
     // how many positions have a page
     int mine = 0, all;
-    for (int d = t; d < used; d += kPickThreads) mine += (uint32_t)row[d] < (uint32_t)a.pages;
+    constexpr int kEach = 8;  // entries a thread has at once
+    for (int64_t d0 = 0; d0 < used; d0 += kPickThreads * kEach) {
+        int p[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int64_t d = d0 + t + i * kPickThreads;
+            p[i] = row[d < used ? d : used - 1];
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) mine += d0 + t + i * kPickThreads < used && (uint32_t)p[i] < (uint32_t)a.pages;
+    }
     scan_workgroup<kPickWaves>(mine, sums, &all);
     r.pages = all;
     r.gaps = all != used;
@@ -115,15 +125,35 @@ __device__ EvictRecord see(const EvictArgs& a, int s, int set, int32_t* sums) {
     if (!r.cut) return r;
     if (set == 0 || r.gaps) {  // (with gaps every set needs the places: they write the same)
         int at = 0;
-        for (int d0 = 0; d0 < used; d0 += kPickThreads) {
-            const int p = d0 + t < used ? row[d0 + t] : -1;
-            const bool is = (uint32_t)p < (uint32_t)a.pages;
-            const int to = at + scan_workgroup<kPickWaves>(is, sums, &all);
-            if (is) {
-                a.old_page[(int64_t)s * a.max_pages + to] = p;
-                a.old_at[(int64_t)s * a.max_pages + to] = d0 + t;
+        for (int64_t d0 = 0; d0 < used; d0 += kPickThreads * kEach) {
+            const int lane = t & 63;
+            const int64_t own = d0 + t / 64 * (64 * kEach) + lane;
+            int p[kEach], count = 0;
+            uint64_t is[kEach];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) p[i] = row[own + 64 * i < used ? own + 64 * i : used - 1];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                is[i] = __ballot(own + 64 * i < used && (uint32_t)p[i] < (uint32_t)a.pages);
+                count += __popcll(is[i]);
             }
-            at += all;
+            __syncthreads();
+            if (lane == 0) sums[t / 64] = count;
+            __syncthreads();
+            int64_t to = (int64_t)s * a.max_pages + at;
+            for (int x = 0; x < kPickWaves; ++x) {
+                to += x < t / 64 ? sums[x] : 0;
+                at += sums[x];
+            }
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int64_t k = to + __popcll(is[i] & ((uint64_t(1) << lane) - 1));
+                if ((is[i] >> lane) & 1) {
+                    a.old_page[k] = p[i];
+                    a.old_at[k] = (int)own + 64 * i;
+                }
+                to += __popcll(is[i]);
+            }
         }
         __syncthreads();
     }
@@ -393,8 +423,9 @@ __global__ __launch_bounds__(kPickThreads) void evict_order_kernel(EvictArgs a) 
 }
 
 // ---------------------------------------------------------------------------
-// Then: a workgroup a sequence finds the shared pages that change in any set.  3 to 4 us.
-constexpr int kDemandThreads = 256;
+// Then: a workgroup a sequence finds the shared pages that change in any set.  Latency:
+// 4 to 5 us, 8 for 3000 pages of a sequence (with 256 threads 15).
+constexpr int kDemandThreads = 1024;
 
 __global__ __launch_bounds__(kDemandThreads) void evict_demand_kernel(EvictArgs a) {
     __shared__ int32_t sums[kDemandThreads / 64];
@@ -506,7 +537,8 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
 // stay where they are.  `parts` workgroups a (sequence, layer, head).
 //
 // Bound by the bytes that move, each read and written once, and below some 20 MB by the
-// chain of loads that leads to them: 10 to 11 us for 4000 rows of 8 heads or 24 of 32 sequences.
+// chain of loads that leads to them: 10 to 11 us for 4000 rows of 8 heads or 24 of 32 sequences,
+// 32 us for 20000 rows of 6 heads, 38 MB (with a quarter of the workgroups and a branch at each load 53).
 constexpr int kMoveThreads = 256;
 
 // A thread's part of the rows that move: 16 bytes of a row's keys or values, always the
@@ -545,8 +577,8 @@ __device__ void move_unit(const EvictArgs& a, const EvictRecord& r, int s, int l
         uint8_t* to[kAtOnce];
 #pragma unroll
         for (int y = 0; y < kAtOnce; ++y) {
-            const int64_t e = e0 + (int64_t)y * a.parts * l.step;
-            if (e >= holes) continue;
+            int64_t e = e0 + (int64_t)y * a.parts * l.step;
+            e = e < holes ? e : holes - 1;  // (loads without branches; what is too much is not stored)
             const int from = list[a.positions - 1 - e], hole = list[e];
             x[y] = *reinterpret_cast<const u32x4*>(a.row_of(old_page[from >> a.log_page], layer, l.side, head, from) + l.byte);
             to[y] = a.row_of(a.page_now(r, s, hole >> a.log_page), layer, l.side, head, hole) + l.byte;
@@ -584,7 +616,8 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
 // weights move; table, counts and lengths.  Where the last tokens shift by less than their
 // number, one workgroup a (sequence, layer, head) reads ahead of where it writes; else
 // `end_parts` of them share the rows.  The sums' tail becomes zeros, by `end_parts` workgroups
-// too.  Bound by latency as well: 15 us for 32 sequences, 10 for 131k places of 8 heads.
+// too; so are the tokens' sources and the table.  Bound by latency as well: 14 us for 32
+// sequences, 6 for 131k places of 8 heads or one sequence of 20000 pages.
 constexpr int kEndThreads = 256;
 
 __device__ void shift_recent(const EvictArgs& a, const EvictRecord& r, int s, int layer, int head, int part) {
@@ -599,8 +632,7 @@ __device__ void shift_recent(const EvictArgs& a, const EvictRecord& r, int s, in
 #pragma unroll
         for (int y = 0; y < kAtOnce; ++y) {
             const int64_t at = p0 + y * l.step + l.first;
-            if (!l.on || at >= r.n) continue;
-            const int p = (int)at, from = p + by;
+            const int p = at < r.n ? (int)at : r.n - 1, from = p + by;  // (as above)
             x[y] = *reinterpret_cast<const u32x4*>(a.row_of(old_page[from >> a.log_page], layer, l.side, head, from) + l.byte);
             to[y] = a.row_of(a.page_now(r, s, p >> a.log_page), layer, l.side, head, p) + l.byte;
         }
@@ -638,12 +670,6 @@ __device__ void move_sums(const EvictArgs& a, const EvictRecord& r, int s, int s
     float* const w = a.weight + of;
     const int32_t* const list = a.list + of;
     const int holes = a.holes[a.sums(s, set)], by = r.m - r.n;
-    if (a.source) {
-        int32_t* const source = a.source + of;
-        for (int p = t; p < r.n; p += kEndThreads) source[p] = a.position(r, s, p < r.border ? p : p + by);
-        __syncthreads();
-        for (int e = t; e < holes; e += kEndThreads) source[list[e]] = a.position(r, s, list[a.positions - 1 - e]);
-    }
     if (r.gaps) {  // (else the move kernel has filled the holes)
         shift_sums(w, 0, r.m, [&](int i) { return a.position(r, s, i); });
         for (int e = t; e < holes; e += kEndThreads) w[list[e]] = w[list[a.positions - 1 - e]];
@@ -654,37 +680,48 @@ __device__ void move_sums(const EvictArgs& a, const EvictRecord& r, int s, int s
     for (int p = (r.gaps || r.m - (r.n - r.border) < r.n ? r.n : r.m - (r.n - r.border)) + t; p < r.length; p += kEndThreads) w[p] = 0.0f;
 }
 
-// Zeros between the cut and the last tokens' former places: what was there has moved.
+// Where the tokens were, and zeros between the cut and the last ones' former places: what was
+// there has moved.
 __device__ void clear_sums(const EvictArgs& a, const EvictRecord& r, int s, int set, int part) {
+    if (a.source) {
+        int32_t* const source = a.source + a.sums(s, set) * a.positions;
+        const int32_t* const list = a.list + a.sums(s, set) * a.positions;
+        const uint64_t* const bits = a.hole_bits + a.sums(s, set) * a.words;
+        const int first = part * kEndThreads + (int)threadIdx.x, step = a.end_parts * kEndThreads;
+        for (int64_t p = first; p < r.n; p += step)
+            if (p >= r.border || !((bits[p / 64] >> (p % 64)) & 1))
+                source[p] = a.position(r, s, (int)p < r.border ? (int)p : (int)p + r.m - r.n);
+        for (int64_t e = first; e < a.holes[a.sums(s, set)]; e += step) source[list[e]] = a.position(r, s, list[a.positions - 1 - e]);
+    }
     if (r.gaps) return;  // (the one that moves the sums clears all of it)
     float* const w = a.weight + a.sums(s, set) * a.positions;
     const int end = r.m - (r.n - r.border);
     for (int64_t p = r.n + (int64_t)part * kEndThreads + threadIdx.x; p < end; p += (int64_t)a.end_parts * kEndThreads) w[p] = 0.0f;
 }
 
-__device__ void enter_pages(const EvictArgs& a, const EvictRecord& r, int s) {
-    const int t = (int)threadIdx.x, page = 1 << a.log_page;
+__device__ void enter_pages(const EvictArgs& a, const EvictRecord& r, int s, int part) {
+    const int page = 1 << a.log_page;
     const int used = (r.n + page - 1) >> a.log_page, before = (r.length + page - 1) >> a.log_page;
     int32_t* const row = a.table + (int64_t)s * a.max_pages;
-    for (int d = t; d < before; d += kEndThreads) {
+    for (int64_t d = part * kEndThreads + (int)threadIdx.x; d < before; d += a.end_parts * kEndThreads) {
         const int64_t at = (int64_t)s * a.max_pages + d;
         int now = -1;
         if (d < r.pages) {
             const int was = a.old_page[at];
-            now = d < used ? a.page_now(r, s, d) : -1;
+            now = d < used ? a.page_now(r, s, (int)d) : -1;
             if (now != was) atomicAdd(a.refs + was, -1);
             if (now >= 0 && now != was) a.refs[now] = 1;
         }
         row[d] = now;
     }
-    if (t == 0) a.lengths[s] = r.n;
+    if (part == 0 && threadIdx.x == 0) a.lengths[s] = r.n;
 }
 
 __global__ __launch_bounds__(kEndThreads) void evict_end_kernel(EvictArgs a) {
     const int s = (int)blockIdx.y, units = a.layers * a.heads * a.end_parts, clears = a.sets * a.end_parts;
     const EvictRecord r = a.record[s];
     if (!r.cut || r.base < 0) return;
-    for (int i = (int)blockIdx.x; i < units + clears + a.sets + 1; i += (int)gridDim.x) {
+    for (int i = (int)blockIdx.x; i < units + clears + a.sets + a.end_parts; i += (int)gridDim.x) {
         if (i < units) {
             const int unit = i / a.end_parts;
             shift_recent(a, r, s, unit / a.heads, unit % a.heads, i - unit * a.end_parts);
@@ -694,7 +731,7 @@ __global__ __launch_bounds__(kEndThreads) void evict_end_kernel(EvictArgs a) {
         } else if (i < units + clears + a.sets) {
             move_sums(a, r, s, i - units - clears);
         } else {
-            enter_pages(a, r, s);
+            enter_pages(a, r, s, i - units - clears - a.sets);
         }
     }
 }
@@ -803,7 +840,7 @@ rac_status rac_cache_evict(const rac_cache_config* cfg, const rac_evict_config* 
     // (a few workgroups for every compute unit where the sequences and heads are few: a round of
     // 32 sequences 73 us, with four times as many 82; the cut of 131k places 79 us, with a quarter 82)
     const int64_t units = (int64_t)cfg->layers * cfg->kv_heads, parts = 2048 / (units * cfg->seqs);
-    a.parts = (int32_t)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    a.parts = (int32_t)(parts < 1 ? 1 : parts > 256 ? 256 : parts);
     const int64_t ends = 256 / (units * cfg->seqs);
     a.end_parts = (int32_t)(ends < 1 ? 1 : ends > 32 ? 32 : ends);
     rac_status st;
@@ -819,7 +856,7 @@ rac_status rac_cache_evict(const rac_cache_config* cfg, const rac_evict_config* 
     if (st == RAC_OK) st = launch(evict_demand_kernel, 1, cfg->seqs, kDemandThreads, a, stream);
     if (st == RAC_OK) st = launch(evict_plan_kernel, 1, 1, kPlanThreads, a, stream);
     if (st == RAC_OK) st = launch(evict_move_kernel, units * a.parts, cfg->seqs, kMoveThreads, a, stream);
-    if (st == RAC_OK) st = launch(evict_end_kernel, (units + evict->sets) * a.end_parts + evict->sets + 1, cfg->seqs, kEndThreads, a, stream);
+    if (st == RAC_OK) st = launch(evict_end_kernel, (units + evict->sets + 1) * a.end_parts + evict->sets, cfg->seqs, kEndThreads, a, stream);
     return st;
 }
 
