@@ -164,6 +164,22 @@ def test_ties_go_to_the_lower_word():
         assert c.ids[0].tolist() == list(range(64))
 
 
+@pytest.mark.parametrize("top", [1, 5, 64])
+@pytest.mark.parametrize("vocab", [64, 500, 697, 1500, 2047, 2048, 2049, 4090])
+def test_short_rows_with_alternatives(vocab, top):
+    """Rows of a block a thread or less: of random words, of ties with one another, and of few that are allowed."""
+    say(f"[gpu] short rows of {vocab}, {top} alternatives")
+    for dtype in (torch.bfloat16, torch.float32):
+        x = normal(7, vocab, dtype, vocab, apart=3)
+        x[1] = 0.0
+        x[2] = x[2].round()
+        x[3, : vocab - 20] = -math.inf
+        x[4] = 1.0
+        x[4, ::2] = 2.0
+        x[5] = torch.arange(vocab, device="cuda").float().neg().to(dtype)
+        Call(x, some_tokens(7, vocab, 2), 0.0, top).check()
+
+
 def test_many_large_words_in_few_places():
     """More words than the bar of the threads' largest lets be ranked: of different value,
     all at the places of a few threads, and above many that tie."""
