@@ -149,12 +149,16 @@ __device__ __forceinline__ uint64_t exist_in(const WeightsArgs& a, const Unit& u
     return r;
 }
 
-// Adds a sum of key u.key0 + key.
+// Where the sum of key u.key0 + key is.
+__device__ __forceinline__ float* sum_of(const WeightsArgs& a, const Unit& u, const Seq& q, int key) {
+    const int64_t set = a.first_set + (u.head > 0 && a.sets > 1 ? u.head : 0), j = (int64_t)u.key0 + key;
+    return u.past ? a.weight + ((int64_t)u.seq * a.sets + set) * a.positions + j : a.draft_weight + set * a.draft_rows + q.d0 + j;
+}
+
+// Adds to it, if there is such a key.
 __device__ __forceinline__ void add_to(const WeightsArgs& a, const Unit& u, const Seq& q, uint64_t exist, int key, float v) {
     if (!((exist >> key) & 1)) return;
-    const int64_t set = a.first_set + (u.head > 0 && a.sets > 1 ? u.head : 0), j = (int64_t)u.key0 + key;
-    float* const to = u.past ? a.weight + ((int64_t)u.seq * a.sets + set) * a.positions + j
-                             : a.draft_weight + set * a.draft_rows + q.d0 + j;
+    float* const to = sum_of(a, u, q, key);
     *to = *to + v;
 }
 
@@ -323,6 +327,15 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 4) void weights_few_kerne
         const uint64_t exist = exist_in(a, u, q, page);
         const float c2 = TYPE == RAC_CACHE_FP8 && u.past ? a.scale2 * a.k_scale : a.scale2;
         const bool look = !u.past || a.window > 0;  // whether rows differ in what they see
+        // (what is to be added to, ahead of the work)
+        const int key = SHARE ? (int)threadIdx.x % kFewKeys : KeySums<NT>::key_of_lane();
+        const bool adds = (SHARE ? threadIdx.x < kFewKeys : KeySums<NT>::first_lane()) && ((exist >> key) & 1);
+        float* to = nullptr;
+        float before = 0.0f;
+        if (adds) {
+            to = sum_of(a, u, q, key);
+            before = *to;
+        }
         KeySums<NT> sums;
         sums.clear();
         const int items = us.rows * a.item_heads;
@@ -361,20 +374,15 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 4) void weights_few_kerne
             }
         }
         float v = sums.join();
-        const int key = KeySums<NT>::key_of_lane();
         if constexpr (SHARE) {
-            if (KeySums<NT>::first_lane()) shared_sums[turn][wave][key] = v;
+            if (KeySums<NT>::first_lane()) shared_sums[turn][wave][KeySums<NT>::key_of_lane()] = v;
             __syncthreads();
-            if (threadIdx.x < kFewKeys) {
-                v = 0.0f;
+            v = 0.0f;
 #pragma unroll
-                for (int y = 0; y < kWavesEach; ++y) v = v + shared_sums[turn][y][threadIdx.x];
-                add_to(a, u, q, exist, (int)threadIdx.x, v);
-            }
+            for (int y = 0; y < kWavesEach; ++y) v = v + shared_sums[turn][y][key];
             turn ^= 1;  // (what is read here is written again only after the next barrier)
-        } else if (KeySums<NT>::first_lane()) {
-            add_to(a, u, q, exist, key, v);
         }
+        if (adds) *to = before + v;
     }
 }
 
