@@ -303,7 +303,7 @@ struct KeySums {
 // divide heads and rows; else each has a unit of its own.
 //
 // Bound by the bytes of the committed keys: one token of 32 sequences of 4001 to 16383 in
-// bf16, 8 heads of 128 channels, 591 MB in 117 us, 5.0 TB/s (a large copy reaches 4.9).  200
+// bf16, 8 heads of 128 channels, 591 MB in 115 us, 5.1 TB/s (a large copy reaches 4.9).  200
 // short drafts in a window of 1000, 24 MB in 8 bits, take 17 us: three units or less for a
 // wavefront, and the latency of their pages, keys and rows one after the other.
 constexpr int kFewKeys = 32, kFewRows = 16;
