@@ -683,52 +683,54 @@ __global__ __launch_bounds__(kLogThreads) void logprob_join_kernel(LogprobArgs a
     __shared__ uint64_t best[kMostTop];
     __shared__ int count;
     const int t = (int)threadIdx.x, all = a.parts * a.top;
-    const int64_t r = blockIdx.x;
-    const Scored<TYPE> scored(a, r);
-    constexpr int kAtOnce = kMostParts * kMostTop / kLogThreads;
-    uint64_t key[kAtOnce], bar = 0;
-    if (a.top > 0) {
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const Scored<TYPE> scored(a, r);
+        constexpr int kAtOnce = kMostParts * kMostTop / kLogThreads;
+        uint64_t key[kAtOnce], bar = 0;
+        if (a.top > 0) {
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            key[i] = 0;
-            if (i * kLogThreads < all && t + i * kLogThreads < all) key[i] = a.part_top[r * all + t + i * kLogThreads];
+            for (int i = 0; i < kAtOnce; ++i) {
+                key[i] = 0;
+                if (i * kLogThreads < all && t + i * kLogThreads < all) key[i] = a.part_top[r * all + t + i * kLogThreads];
+            }
+            if ((t & 63) < a.parts) bar = a.part_top[r * all + (t & 63) * a.top + a.each - 1];
         }
-        if ((t & 63) < a.parts) bar = a.part_top[r * all + (t & 63) * a.top + a.each - 1];
-    }
-    Sums x{-INFINITY, 0.0f, 0.0f};
-    if ((t & 63) < a.parts) {
-        const float4 v = *reinterpret_cast<const float4*>(a.part_sums + 4 * (r * a.parts + (t & 63)));
-        x = Sums{v.x, v.y, v.z};
-    }
-    x.join_wave(a.scale2);
-    if (t == kLogThreads - 64) finish_row<TYPE>(a, r, x, scored);
-    if (a.top == 0) return;
-    int above = 0;
-    for (int p = 0; p < a.parts; ++p) {
-        const uint64_t y = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(bar >> 32), p) << 32 |
-                           (uint32_t)__builtin_amdgcn_readlane((int)bar, p);
-        above += y > bar || (y == bar && p < (t & 63));
-    }
-    const int at = __builtin_ctzll(__ballot((t & 63) < a.parts && above == (a.top + a.each - 1) / a.each - 1));
-    bar = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(bar >> 32), at) << 32 |
-          (uint32_t)__builtin_amdgcn_readlane((int)bar, at);
-    if (t < kMostTop) best[t] = 0;
-    if (t == 0) count = 0;
-    __syncthreads();
+        Sums x{-INFINITY, 0.0f, 0.0f};
+        if ((t & 63) < a.parts) {
+            const float4 v = *reinterpret_cast<const float4*>(a.part_sums + 4 * (r * a.parts + (t & 63)));
+            x = Sums{v.x, v.y, v.z};
+        }
+        x.join_wave(a.scale2);
+        if (t == kLogThreads - 64) finish_row<TYPE>(a, r, x, scored);
+        if (a.top == 0) continue;
+        int above = 0;
+        for (int p = 0; p < a.parts; ++p) {
+            const uint64_t y = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(bar >> 32), p) << 32 |
+                               (uint32_t)__builtin_amdgcn_readlane((int)bar, p);
+            above += y > bar || (y == bar && p < (t & 63));
+        }
+        const int at = __builtin_ctzll(__ballot((t & 63) < a.parts && above == (a.top + a.each - 1) / a.each - 1));
+        bar = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(bar >> 32), at) << 32 |
+              (uint32_t)__builtin_amdgcn_readlane((int)bar, at);
+        if (t < kMostTop) best[t] = 0;
+        if (t == 0) count = 0;
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i)
-        if (key[i] && key[i] >= bar) keys[atomicAdd(&count, 1)] = key[i];  // (any order: they are ranked)
-    __syncthreads();
-    const int n = count;
-    for (int i = t; i < n; i += kLogThreads) {
-        const uint64_t k = keys[i];
-        int rank = 0;
+        for (int i = 0; i < kAtOnce; ++i)
+            if (key[i] && key[i] >= bar) keys[atomicAdd(&count, 1)] = key[i];  // (any order: they are ranked)
+        __syncthreads();
+        const int n = count;
+        for (int i = t; i < n; i += kLogThreads) {
+            const uint64_t k = keys[i];
+            int rank = 0;
 #pragma unroll 8
-        for (int j = 0; j < n; ++j) rank += keys[j] > k;
-        if (rank < a.top) best[rank] = k;
+            for (int j = 0; j < n; ++j) rank += keys[j] > k;
+            if (rank < a.top) best[rank] = k;
+        }
+        __syncthreads();
+        if (t < a.top) finish_top(a, r, t, best[t], x.lse(a.scale));
+        __syncthreads();
     }
-    __syncthreads();
-    if (t < a.top) finish_top(a, r, t, best[t], x.lse(a.scale));
 }
 
 // The log probabilities of tokens that name their rows, from the rows' lse: a thread each.
@@ -826,7 +828,7 @@ __global__ __launch_bounds__(kLogThreads) void logprob_backward_kernel(GradientA
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 uint64_t up256(uint64_t v) { return (v + 255u) & ~uint64_t(255); }
 int type_bytes(int type) { return type == RAC_TYPE_FP32 ? 4 : 2; }
-constexpr int64_t kMostGroups = 1 << 20;  // workgroups of a launch (they go on with further rows)
+constexpr int64_t kMostGroups = 1 << 20;  // workgroups of a launch: a kernel of a call's rows goes on with further ones
 
 template <class A>
 rac_status launch(void (*kernel)(A), int64_t x, int64_t y, int threads, const A& args, hipStream_t st) {
