@@ -93,9 +93,11 @@ rac_status rac_rotary(const rac_rotary_config* cfg, const int32_t* pos, const do
  * A logit of -infinity (a masked word) has no part in the sums and is no
  * alternative: where a row has fewer, the rest have id -1 and -infinity.  A row of
  * such logits only has an lse of -infinity, entropy 0, and log probabilities of
- * -infinity; so does one whose lse lies below the range of fp32.  A token outside the
- * vocabulary, or a row outside the rows, scores 0 (padding).  A NaN or +infinity makes
- * its row's lse, entropy and log probabilities NaN; a NaN is no alternative.
+ * -infinity; so does one whose lse lies below the range of fp32, but for its entropy.  A
+ * token outside the vocabulary, or a row outside the rows, scores 0 (padding).  A NaN or
+ * +infinity makes its row's lse, entropy and log probabilities NaN; a NaN is no alternative.
+ * An lse above the range of fp32 (finite logits, a scale above 1) is NaN, and so are
+ * the row's log probabilities.
  *
  * Sums are fp32, whatever the type. */
 typedef struct {
@@ -135,7 +137,7 @@ rac_status rac_logprobs(const rac_logprob_config* cfg, const rac_logprob_tensors
  *   grad_logits[r][v] = c (g_l (v == tokens[r]) - p_v (g_l + g_e (ln p_v + entropy[r])))
  * with g_l = grad_logprob[r] (0 for a token outside the vocabulary) and g_e =
  * grad_entropy[r]; either array may be NULL (zeros), not both.  A masked word gets
- * g_l's part alone, a row of masked words zeros. */
+ * g_l's part alone, a row whose lse is -infinity zeros, one whose lse is NaN NaN. */
 typedef struct {
     const void* logits; /* as above                                                    */
     int64_t stride;

@@ -282,8 +282,10 @@ struct Sums {
         s = sum_wave(s);
         t = sum_wave(t);
     }
+    // (an infinity above the range would make every word's log probability one below it)
     __device__ __forceinline__ float lse(float scale) const {
-        return s == 0.0f ? -INFINITY : (float)((double)m * (double)scale + (double)log2f(s) * 0.6931471805599453);
+        const float x = (float)((double)m * (double)scale + (double)log2f(s) * 0.6931471805599453);
+        return s == 0.0f ? -INFINITY : x == INFINITY ? NAN : x;
     }
     __device__ __forceinline__ float entropy() const {
         if (s == 0.0f) return 0.0f;
