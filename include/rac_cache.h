@@ -191,7 +191,9 @@ rac_status rac_cache_copy(const rac_cache_config* cfg, const void* src_pool, con
  *   draft_weight : fp32 [sets][draft_rows], the drafted tokens'
  * A round is rac_tree_attention and rac_tree_weights for every layer, rac_cache_commit,
  * rac_cache_weights_commit, and rac_cache_evict.  rac_cache_fork knows nothing of
- * weights: those of a sequence are those of its parent, a copy of rows. */
+ * weights: those of a sequence are those of its parent, a copy of rows.  The predictor's step
+ * below keeps its queries and lse to itself, so rac_tree_weights cannot follow it: its
+ * cache is bounded by rac_cache_fork's keep_from. */
 
 /* Adds to the sums of layer `layer` what the rows of rac_tree_attention's call give
  * to every key they see, with t, tree and cfg as there (t->v and t->out are not looked

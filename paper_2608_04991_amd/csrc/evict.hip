@@ -424,7 +424,9 @@ __global__ __launch_bounds__(kPickThreads) void evict_order_kernel(EvictArgs a) 
 
 // ---------------------------------------------------------------------------
 // Then: a workgroup a sequence finds the shared pages that change in any set.  Latency:
-// 4 to 5 us, 8 for 3000 pages of a sequence (with 256 threads 15).
+// 4 to 5 us with few sets, 8 for 3000 pages of a sequence (with 256 threads 15).  A thread goes
+// through the sets of a page until one has changed it, a load each: where no set changes any of
+// 188 shared pages of three forks the whole call takes 36 us with one set, 176 with 256.
 constexpr int kDemandThreads = 1024;
 
 __global__ __launch_bounds__(kDemandThreads) void evict_demand_kernel(EvictArgs a) {
@@ -617,7 +619,10 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
 // number, one workgroup a (sequence, layer, head) reads ahead of where it writes; else
 // `end_parts` of them share the rows.  The sums' tail becomes zeros, by `end_parts` workgroups
 // too; so are the tokens' sources and the table.  Bound by latency as well: 14 us for 32
-// sequences, 6 for 131k places of 8 heads or one sequence of 20000 pages.
+// sequences, 6 for 131k places of 8 heads or one sequence of 20000 pages.  Many last tokens that
+// shift by few take their steps one after the other, 32 tokens of 128 channels each: whole calls
+// that let 24 of 16408 tokens go, 4 layers of 8 heads, 55 us with 64 last ones, 147 with 2000 and
+// 426 with 8192; of 32 such sequences 78, 478 and 1686.
 constexpr int kEndThreads = 256;
 
 __device__ void shift_recent(const EvictArgs& a, const EvictRecord& r, int s, int layer, int head, int part) {

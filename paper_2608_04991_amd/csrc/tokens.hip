@@ -79,7 +79,7 @@ struct Block {
 // of a binary64 product, off by 2^-53 of the turns at most.
 //
 // Bound by the bytes of queries and keys, read and written once: 4099 rows of 28 + 4 heads
-// of 128 channels, 64 of them turned, 67 MB, in 16.0 us, 4.2 TB/s (a large copy reaches 4.9).
+// of 128 channels, 64 of them turned, 67 MB, in 16.7 us, 4.0 TB/s (a large copy reaches 4.9).
 // A level of 8 rows of 8 + 8 heads takes 3 us, the time of a launch.
 struct RotaryArgs {
     const int32_t* pos;
@@ -560,7 +560,11 @@ struct Top {
                     return n < top;
                 });
             if (t == 0 && count < top) count = n < top ? n : top;
-        } else {  // (a few threads have most of the large ones) one after the other
+        } else {
+            // A few threads have most of the large ones, as of a mask that allows one range of words:
+            // one alternative after the other, a look at all blocks each.  Rows of 131072 in bf16 of
+            // which 2000 words in a row are allowed, 64 alternatives: 393 us a row and 2.9 ms for 681
+            // of them, with every word allowed 16 and 76; 8 alternatives 67 and 462 us.
             uint64_t last = ~uint64_t(0);
             n = 0;
             for (; n < top; ++n) {
@@ -623,9 +627,10 @@ __device__ __forceinline__ void finish_top(const LogprobArgs& a, int64_t row, in
 // A workgroup a row, or a part of one: one pass with a running reference and sums.  With
 // alternatives the blocks stay in registers for the second look where they fit (HELD).
 //
-// Bound by the logits' bytes, 4099 rows of 100003 in bf16: 820 MB in 149 us, 5.5 TB/s.  With
-// alternatives of short rows by what follows the loads, the bar, the look and the ranking of
-// candidates, for which a workgroup waits on itself: 681 rows of 32768, 45 MB, in 19 us.
+// Bound by the logits' bytes, 4099 rows of 100003 in bf16: 820 MB in 151 us, 5.4 TB/s (call
+// after call; under a profiler, with gaps between them, 162 in the median).  With alternatives
+// of short rows by what follows the loads, the bar, the look and the ranking of candidates, for
+// which a workgroup waits on itself: 681 rows of 32768, 45 MB, in 20 us.
 template <int TYPE, bool ENTROPY, bool TOP, int T, bool HELD>
 __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
     using B = Block<TYPE>;
@@ -678,7 +683,7 @@ __global__ __launch_bounds__(T) void logprob_kernel(LogprobArgs a) {
 // Joins the parts of a row: a wavefront has the sums.  With d alternatives of each of
 // top / d parts there are enough: so the top / d-th largest of the parts' d-th ones bounds
 // the row's from below, and the few keys that reach it are ranked by counting.  Bound by
-// the loads' latency and its own barriers: 4 us for 8 parts and 20 alternatives.
+// the loads' latency and its own barriers: 4 to 5 us for 8 parts and 20 alternatives.
 template <int TYPE>
 __global__ __launch_bounds__(kLogThreads) void logprob_join_kernel(LogprobArgs a) {
     __shared__ uint64_t keys[kMostParts * kMostTop];
@@ -749,8 +754,9 @@ __global__ __launch_bounds__(kLogThreads) void logprob_pick_kernel(LogprobArgs a
 // Gradients: every logit read and every gradient written once, at the same place.  With u
 // = c x - lse and p = e^u the gradient of a logit is c (g_l ([it is the token] - p) - g_h p (u + H)).
 //
-// Bound by those bytes: 4096 rows of 131072 in bf16, 2.15 GB, in 350 us, 6.1 TB/s; 64 rows
-// of 32003 in fp32, 16 MB, in 5.6 us.  Without ALIKE the elements are stored one by one: 767 us.
+// Bound by those bytes: 4096 rows of 131072 in bf16, 2.15 GB, in 358 us, 6.0 TB/s; 64 rows
+// of 32003 in fp32, 16 MB, in 6.2 us.  Without ALIKE the elements are stored one by one, for
+// what a thread has read are parts of two of the gradient's 16 bytes: 786 us.
 struct GradientArgs {
     const uint8_t* logits;
     uint8_t* grad;

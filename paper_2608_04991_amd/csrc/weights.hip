@@ -303,7 +303,7 @@ struct KeySums {
 // divide heads and rows; else each has a unit of its own.
 //
 // Bound by the bytes of the committed keys: one token of 32 sequences of 4001 to 16383 in
-// bf16, 8 heads of 128 channels, 591 MB in 115 us, 5.1 TB/s (a large copy reaches 4.9).  200
+// bf16, 8 heads of 128 channels, 591 MB in 114 us, 5.2 TB/s (a large copy reaches 4.9).  200
 // short drafts in a window of 1000, 24 MB in 8 bits, take 17 us: three units or less for a
 // wavefront, and the latency of their pages, keys and rows one after the other.
 constexpr int kFewKeys = 32, kFewRows = 16;
@@ -392,10 +392,15 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 4) void weights_few_kerne
 // products of this one.  A unit is cut into parts of at most `size` blocks, which about
 // kWant workgroups share out, and the parts are joined.
 //
-// Bound by the exponentials: for 128 channels and 16 rows by 64 keys the matrix cores are
-// busy for 256 cycles and the vector unit for 384, 256 of them exponentials.  Chunks of 701
-// to 2048 rows over 1003 to 6001 tokens, 28 heads on 4 of 128 channels: 170 GFLOP in 300 us,
-// 565 TF/s (a large matrix product reaches 1360), and 8 us for the join.
+// Chunks of 701 to 2048 rows over 1003 to 6001 tokens, 28 heads on 4 of 128 channels: 170
+// GFLOP in 302 us, 563 TF/s (a large matrix product reaches 1360), and 9 us for the join; under
+// a profiler 323.  No unit alone is the bound.  For 16 rows by 64 keys the matrix cores are busy
+// for 256 cycles, and the vector unit has 16 exponentials of 8 cycles and 32 factors and sums of
+// 4; counted are 506 of its cycles, 64 of them the issue of matrix instructions, for 46 vector
+// instructions more than these.  Of the 1021 cycles that a tile takes that is 25% and 50%; the
+// wavefronts, two a SIMD, wait for 40% of theirs.  With a mask and a window every committed tile
+// is masked key by key: 16 trees of 130 nodes, 32 heads on 8, in a window of 4096 take 222 us,
+// without the mask 176.
 constexpr int kManyKeys = 256, kManyRows = 64, kWant = 3000;
 constexpr int kSlots = 2 * kWant;  // (a unit that is cut has fewer than twice its blocks over the size parts)
 
